@@ -11,6 +11,8 @@
  *   shiftattn_decode            one-token-per-sequence attention, split over the context (fused KV append)
  *   shiftattn_mixed             a unified batch of chunks and decode rows in one call
  *   shiftattn_unpack_head2seq   receive side of the head->sequence all-to-all (SP mode only)
+ *   shiftattn_{kv_write,prefill,decode,mixed}_scaled   the same over an FP8 cache with a scale for each block and head
+ *   shiftattn_tables_append / shiftattn_tables_truncate   block tables and slot maps from request lengths, on the GPU
  *
  * and, next to the exchange, the two projections fused with its layouts (bf16, or FP8 E4M3 operands):
  *
@@ -53,6 +55,19 @@
  * finite 448).  A stored element stands for code_value * k_scale (K) or code_value * v_scale (V).
  * The writer computes x / scale in float32 and rounds to the nearest code, ties to the even code,
  * magnitudes beyond 448 saturating; NaN gives a NaN code.  q, k_new, v_new and out keep `dtype`.
+ *
+ * FP8 KV cache with block scales (kv_format = SHIFTATTN_KV_FP8_E4M3_BLOCKS, the calls named _scaled): the same codes in the same
+ * arrangement, and beside them kv_scales[num_blocks][num_kv_heads][2] (float32, 8-byte aligned): the scale of a block's K and of
+ * its V for each head, a power of two.  k_scale and v_scale are not read.  Nothing has to be calibrated: the append
+ * chooses the scales.  With needed(x) the least power of two between 2^-100 and 2^119 that brings the largest finite magnitude
+ * of x to at most 448, and x the tokens of a block that a call appends at offsets o, o + 1, .. of it:
+ *   o = 0: the block starts anew, its scale becomes needed(x); codes in its other slots are no longer valid (nor need they, or
+ *          the scale, have been set before).
+ *   o > 0: its scale becomes the larger of needed(x) and the one it has; if that is larger than before, the codes in front of
+ *          offset o are multiplied by old / new and rounded again (exact but for those that become subnormal), in slots behind
+ *          the appended tokens the codes stay.
+ * A code is the nearest one to x / scale as above; infinities saturate.  What one call appends to a block must stand next to each
+ * other in the call's rows, in slot order: one stretch of rows for each block (as the rows of a chunk are), each slot once.
  */
 #ifndef SHIFTATTN_H
 #define SHIFTATTN_H
@@ -73,7 +88,7 @@ enum {
 };
 
 enum { SHIFTATTN_BF16 = 0, SHIFTATTN_F32 = 1 };
-enum { SHIFTATTN_KV_SAME = 0 /* cache elements have `dtype` */, SHIFTATTN_KV_FP8_E4M3 = 1 };
+enum { SHIFTATTN_KV_SAME = 0 /* cache elements have `dtype` */, SHIFTATTN_KV_FP8_E4M3 = 1, SHIFTATTN_KV_FP8_E4M3_BLOCKS = 2 };
 
 /* One sequence<->head exchange among P ranks (Algorithm 1: P is the SP degree of the base
  * configuration; h and h_kv are the heads a source rank holds, i.e. model heads / TP). */
@@ -102,7 +117,7 @@ typedef struct shiftattn_attn {
     int64_t q_stride;           /* elements between consecutive tokens of q;   0 = hq_l*D (dense)  */
     int64_t kv_stride;          /* same for k_new and v_new;                   0 = hkv_l*D         */
     int64_t out_stride;         /* same for out;                               0 = hq_l*D          */
-    int32_t kv_format;          /* SHIFTATTN_KV_SAME | SHIFTATTN_KV_FP8_E4M3 (needs head_dim % 16 == 0) */
+    int32_t kv_format;          /* SHIFTATTN_KV_SAME | SHIFTATTN_KV_FP8_E4M3[_BLOCKS] (need head_dim % 16 == 0) */
     float k_scale;              /* FP8 cache only: value of a K element = code value * k_scale, > 0 */
     float v_scale;              /* FP8 cache only: same for V                                      */
     int32_t reserved;           /* must be 0                                                       */
@@ -308,6 +323,70 @@ int shiftattn_mixed(const void *q, const void *k_new, const void *v_new, const i
                     int32_t max_q_len, int32_t max_prefill_seq_len, int32_t num_decode_seqs,
                     int32_t max_decode_seq_len, void *out, void *workspace, size_t workspace_bytes,
                     const shiftattn_attn *a, void *stream);
+
+/* ---- The same over a cache with block scales (a->kv_format = SHIFTATTN_KV_FP8_E4M3_BLOCKS; see the top of this file) ----
+ * kv_scales (device, in/out): float32 [num_blocks][num_kv_heads][2], written by the append, read by attention.
+ * All else as in the calls above, whose workspace queries serve these too (through a->kv_format).  The calls above refuse such a
+ * descriptor, and these any other. */
+int shiftattn_kv_write_scaled(const void *k_new, const void *v_new, const int64_t *slot_mapping, int32_t n_tokens,
+                              void *kv_cache, float *kv_scales, const shiftattn_attn *a, void *stream);
+int shiftattn_prefill_scaled(const void *q, const void *k_new, const void *v_new, const int64_t *slot_mapping,
+                             void *kv_cache, float *kv_scales, const int32_t *block_table, const int32_t *cu_seqlens_q,
+                             const int32_t *seq_lens, int32_t num_seqs, int32_t total_q, int32_t max_q_len,
+                             int32_t max_seq_len, void *out, void *workspace, size_t workspace_bytes,
+                             const shiftattn_attn *a, void *stream);
+int shiftattn_decode_scaled(const void *q, const void *k_new, const void *v_new, const int64_t *slot_mapping,
+                            void *kv_cache, float *kv_scales, const int32_t *block_table, const int32_t *seq_lens,
+                            int32_t num_seqs, int32_t max_seq_len, void *out, void *workspace, size_t workspace_bytes,
+                            const shiftattn_attn *a, void *stream);
+int shiftattn_mixed_scaled(const void *q, const void *k_new, const void *v_new, const int64_t *slot_mapping,
+                           void *kv_cache, float *kv_scales, const int32_t *block_table, const int32_t *cu_seqlens_q,
+                           const int32_t *seq_lens, int32_t num_prefill_seqs, int32_t total_prefill_q, int32_t max_q_len,
+                           int32_t max_prefill_seq_len, int32_t num_decode_seqs, int32_t max_decode_seq_len, void *out,
+                           void *workspace, size_t workspace_bytes, const shiftattn_attn *a, void *stream);
+
+/* ---- Block tables and slot maps on the GPU ---------------------------------------------------------------------------
+ * What the calls above take beside their tensors, kept in device memory and brought from one step to the next there: an engine
+ * that replays its steps from a graph, or does not want to wait for lengths to reach the host, gives its sequences cache
+ * blocks and takes them back with these two calls.  The arrays are the caller's; a zeroed free_count and a free_blocks filled
+ * with 0 .. num_blocks - 1 (then free_count = num_blocks) is all the set-up there is. */
+typedef struct shiftattn_tables {
+    int32_t num_seqs;           /* sequences of the batch, in the order of shiftattn_mixed: chunks, then decode rows          */
+    int32_t max_blocks_per_seq; /* row length of block_table                                                                 */
+    int32_t num_blocks;         /* length of free_blocks                                                                     */
+    int32_t reserved;           /* must be 0                                                                                 */
+    int32_t *seq_lens;          /* device, in/out [num_seqs]: tokens in the cache; <= 0: none                                */
+    int32_t *block_table;       /* device, in/out [num_seqs][max_blocks_per_seq]                                             */
+    int32_t *free_blocks;       /* device, in/out [num_blocks]: a stack of free block ids, free_blocks[free_count - 1] on top */
+    int32_t *free_count;        /* device, in/out [1]: its height (taken as between 0 and num_blocks)                        */
+} shiftattn_tables;
+
+/* tables_append: gives every sequence the blocks that its new tokens need and says where the tokens go.
+ *   new_lens (device, in)       : int32 [num_seqs], new tokens per sequence (< 0: 0); decode rows bring one or none
+ *   num_prefill_seqs (host)     : the first so many sequences are chunks, the others decode rows
+ *   total_prefill_q (host)      : rows that the chunks have together; rows: length of slot_mapping, at least total_prefill_q and
+ *                                 one row for each decode sequence (more: padding to a multiple of the SP degree)
+ *   cu_seqlens_q (device, out)  : int32 [num_prefill_seqs + 1]
+ *   slot_mapping (device, out)  : int64 [rows]; row cu_seqlens_q[s] + i is token i of chunk s, row total_prefill_q + j the token
+ *                                 of the j-th decode sequence; -1 in every other row
+ *   taken (device, out)         : int32 [num_seqs], the new tokens for which there was room: new_lens[s] or 0
+ *   seq_lens grows by taken; the caller's decode sequences without a token keep their length and get slot -1.
+ *   A sequence is refused (taken 0, nothing of it changes) if its tokens exceed its row of block_table, a decode sequence that
+ *   brings more than one, a chunk if the rows of the chunks up to and with it (those refused for the first reason apart) exceed
+ *   total_prefill_q, and any that needs blocks if the blocks needed up to and with it (of those not refused so far) exceed
+ *   free_count.  Blocks leave the stack from the top in the order of sequences and tokens.
+ * tables_truncate: sequence s keeps its first keep_lens[s] tokens (device, in, int32 [num_seqs]) and gives the blocks behind them
+ *   back: 0 for a finished or preempted one, fewer than it has for rejected speculative tokens; negative, or not below
+ *   seq_lens[s]: unchanged.  The blocks go back in the order that undoes an append (sequence 0's first block ends on top), so that
+ *   a truncate to the lengths before an append restores the stack.  Entries of block_table are left as they are.
+ * workspace (device, scratch): shiftattn_tables_workspace_bytes(num_seqs) bytes, 4-byte aligned (SIZE_MAX for a negative
+ *   count).  Calls that share a workspace or the tables must not overlap. */
+size_t shiftattn_tables_workspace_bytes(int32_t num_seqs);
+int shiftattn_tables_append(const shiftattn_tables *t, const int32_t *new_lens, int32_t num_prefill_seqs,
+                            int32_t total_prefill_q, int32_t rows, int32_t *cu_seqlens_q, int64_t *slot_mapping,
+                            int32_t *taken, void *workspace, size_t workspace_bytes, void *stream);
+int shiftattn_tables_truncate(const shiftattn_tables *t, const int32_t *keep_lens, void *workspace,
+                              size_t workspace_bytes, void *stream);
 
 /* Workspace sizes (host only, no GPU work).  Return 0 when no workspace is needed; SIZE_MAX on
  * invalid arguments. */

@@ -45,6 +45,12 @@ class Attn(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class Tables(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("max_blocks_per_seq", ctypes.c_int32), ("num_blocks", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("seq_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("free_blocks", ctypes.c_void_p), ("free_count", ctypes.c_void_p)]
+
+
 class PrefillPlan(ctypes.Structure):
     _fields_ = [("tile_columns", ctypes.c_int32), ("wave_columns", ctypes.c_int32), ("key_ranges", ctypes.c_int32),
                 ("tiles_per_wg", ctypes.c_int32), ("decode_wgs", ctypes.c_int32)]
@@ -55,7 +61,7 @@ class ProjPlan(ctypes.Structure):
                                               "lead_tokens", "tile_features", "tile_tokens")]
 
 
-KV_SAME, KV_FP8_E4M3 = 0, 1
+KV_SAME, KV_FP8_E4M3, KV_FP8_E4M3_BLOCKS = 0, 1, 2
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -122,6 +128,14 @@ def lib() -> ctypes.CDLL:
         L.shiftattn_set_option.argtypes = [i32, i32]
         L.shiftattn_get_option.argtypes = [i32]
         L.shiftattn_get_option.restype = i32
+        L.shiftattn_kv_write_scaled.argtypes = [vp, vp, i64p, i32, vp, vp, ap, vp]
+        L.shiftattn_prefill_scaled.argtypes = [vp, vp, vp, i64p, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, sz, ap, vp]
+        L.shiftattn_decode_scaled.argtypes = [vp, vp, vp, i64p, vp, vp, vp, vp, i32, i32, vp, vp, sz, ap, vp]
+        L.shiftattn_mixed_scaled.argtypes = [vp, vp, vp, i64p, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp, sz, ap, vp]
+        L.shiftattn_tables_workspace_bytes.argtypes = [i32]
+        L.shiftattn_tables_workspace_bytes.restype = sz
+        L.shiftattn_tables_append.argtypes = [ctypes.POINTER(Tables), vp, i32, i32, i32, vp, i64p, vp, vp, sz, vp]
+        L.shiftattn_tables_truncate.argtypes = [ctypes.POINTER(Tables), vp, vp, sz, vp]
         L.shiftattn_last_error.restype = ctypes.c_char_p
         _calls = importlib.import_module("._calls", __package__)
         _calls.bind(_workspace, *[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _calls.names])
@@ -303,15 +317,17 @@ def unpack_o_proj_fp8(recv_codes: torch.Tensor, a_scales: torch.Tensor, w_codes:
 
 def attn_desc(q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Tensor, softmax_scale: float,
               k_new: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, k_scale: float = 1.0,
-              v_scale: float = 1.0) -> Attn:
+              v_scale: float = 1.0, kv_scales: Optional[torch.Tensor] = None) -> Attn:
     """Descriptor from tensor shapes.  kv_cache is [num_blocks, hkv_l, 2, 16*D] in q's type, or uint8 for an
-    FP8 E4M3 cache (then k_scale / v_scale give the value of a code)."""
-    return Attn.from_buffer_copy(_native().attn_desc(q, kv_cache, block_table, softmax_scale, k_new, out, k_scale, v_scale))
+    FP8 E4M3 cache: then k_scale / v_scale give the value of a code, or kv_scales, float32 [num_blocks, hkv_l, 2], a scale for
+    each block and head (which the append chooses; the same tensor goes to every call)."""
+    return Attn.from_buffer_copy(_native().attn_desc(q, kv_cache, block_table, softmax_scale, k_new, out, k_scale, v_scale, kv_scales))
 
 
 def kv_write(k_new: torch.Tensor, v_new: torch.Tensor, slot_mapping: torch.Tensor, kv_cache: torch.Tensor,
-             k_scale: float = 1.0, v_scale: float = 1.0) -> None:
-    _check(_native().kv_write(k_new, v_new, slot_mapping, kv_cache, k_scale, v_scale))
+             k_scale: float = 1.0, v_scale: float = 1.0, kv_scales: Optional[torch.Tensor] = None) -> None:
+    """K/V rows [n_tokens, hkv_l, D] to their slots.  With kv_scales: FP8 codes with a scale for each block, which the call chooses."""
+    _check(_native().kv_write(k_new, v_new, slot_mapping, kv_cache, k_scale, v_scale, kv_scales))
 
 
 def prefill_workspace_bytes(num_seqs: int, total_q: int, max_q_len: int, max_seq_len: int, a: Attn) -> int:
@@ -326,19 +342,20 @@ def prefill(q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Tensor, 
             seq_lens: torch.Tensor, max_q_len: int, max_seq_len: int, out: torch.Tensor, softmax_scale: float,
             k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
             slot_mapping: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, k_scale: float = 1.0,
-            v_scale: float = 1.0) -> None:
+            v_scale: float = 1.0, kv_scales: Optional[torch.Tensor] = None) -> None:
     """Causal attention of prefill chunks; q/out [total_q, hq_l, D] (row-strided views allowed)."""
     _check(_native().prefill(q, kv_cache, block_table, cu_seqlens_q, seq_lens, max_q_len, max_seq_len, out, softmax_scale, k_new, v_new,
-                             slot_mapping, workspace, k_scale, v_scale))
+                             slot_mapping, workspace, k_scale, v_scale, kv_scales))
 
 
 def decode(q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
            max_seq_len: int, out: torch.Tensor, softmax_scale: float, k_new: Optional[torch.Tensor] = None,
            v_new: Optional[torch.Tensor] = None, slot_mapping: Optional[torch.Tensor] = None,
-           workspace: Optional[torch.Tensor] = None, k_scale: float = 1.0, v_scale: float = 1.0) -> None:
+           workspace: Optional[torch.Tensor] = None, k_scale: float = 1.0, v_scale: float = 1.0,
+           kv_scales: Optional[torch.Tensor] = None) -> None:
     """One new token per sequence; q/out [num_seqs, hq_l, D]."""
     _check(_native().decode(q, kv_cache, block_table, seq_lens, max_seq_len, out, softmax_scale, k_new, v_new, slot_mapping, workspace,
-                            k_scale, v_scale))
+                            k_scale, v_scale, kv_scales))
 
 
 STATIC_SCRATCH_BYTES = 16 << 20
@@ -350,7 +367,7 @@ def decode_static(q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Te
                   v_scale: float = 1.0) -> None:
     """decode() without a workspace: the library's own static device array takes the split partials."""
     _check(_native().decode_static(q, kv_cache, block_table, seq_lens, max_seq_len, out, softmax_scale, k_new, v_new, slot_mapping, None,
-                                   k_scale, v_scale))
+                                   k_scale, v_scale, None))
 
 
 def mixed_workspace_bytes(num_prefill_seqs: int, total_prefill_q: int, max_q_len: int, max_prefill_seq_len: int,
@@ -363,11 +380,33 @@ def mixed(q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Tensor, cu
           seq_lens: torch.Tensor, num_prefill_seqs: int, max_q_len: int, max_prefill_seq_len: int,
           max_decode_seq_len: int, out: torch.Tensor, softmax_scale: float, k_new: Optional[torch.Tensor] = None,
           v_new: Optional[torch.Tensor] = None, slot_mapping: Optional[torch.Tensor] = None,
-          workspace: Optional[torch.Tensor] = None, k_scale: float = 1.0, v_scale: float = 1.0) -> None:
+          workspace: Optional[torch.Tensor] = None, k_scale: float = 1.0, v_scale: float = 1.0,
+          kv_scales: Optional[torch.Tensor] = None) -> None:
     """Unified batch: the first num_prefill_seqs sequences are chunks (cu_seqlens_q [num_prefill_seqs + 1]), the
     others carry one row each; q/out hold the chunk rows first, then the decode rows."""
     _check(_native().mixed(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_prefill_seqs, max_q_len, max_prefill_seq_len,
-                           max_decode_seq_len, out, softmax_scale, k_new, v_new, slot_mapping, workspace, k_scale, v_scale))
+                           max_decode_seq_len, out, softmax_scale, k_new, v_new, slot_mapping, workspace, k_scale, v_scale, kv_scales))
+
+
+# ---- block tables and slot maps ----------------------------------------------------------------------------
+def tables_workspace_bytes(num_seqs: int) -> int:
+    return int(lib().shiftattn_tables_workspace_bytes(num_seqs))
+
+
+def tables_append(new_lens: torch.Tensor, num_prefill_seqs: int, total_prefill_q: int, seq_lens: torch.Tensor, block_table: torch.Tensor,
+                  free_blocks: torch.Tensor, free_count: torch.Tensor, cu_seqlens_q: torch.Tensor, slot_mapping: torch.Tensor,
+                  taken: torch.Tensor, workspace: Optional[torch.Tensor] = None) -> None:
+    """Gives every sequence the blocks that its new_lens [num_seqs] tokens need, from the stack free_blocks[:free_count]: seq_lens,
+    block_table and free_count move on, cu_seqlens_q [num_prefill_seqs + 1], slot_mapping [rows] (chunks' rows, one row per
+    decode sequence, -1 elsewhere) and taken [num_seqs] (0: refused for want of rows or blocks) are written."""
+    _check(_native().tables_append(new_lens, num_prefill_seqs, total_prefill_q, seq_lens, block_table, free_blocks, free_count, cu_seqlens_q,
+                                   slot_mapping, taken, workspace))
+
+
+def tables_truncate(keep_lens: torch.Tensor, seq_lens: torch.Tensor, block_table: torch.Tensor, free_blocks: torch.Tensor,
+                    free_count: torch.Tensor, workspace: Optional[torch.Tensor] = None) -> None:
+    """Every sequence keeps its first keep_lens[s] tokens (0: it is finished; negative: all) and gives the blocks behind them back."""
+    _check(_native().tables_truncate(keep_lens, seq_lens, block_table, free_blocks, free_count, workspace))
 
 
 # ---- numpy <-> device helpers for tests and benchmarks (storage only) ------------------------------------

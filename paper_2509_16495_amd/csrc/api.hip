@@ -134,7 +134,13 @@ int check_attn(const shiftattn_attn* a, AttnShape* s) {
         return fail(SHIFTATTN_EINVAL, "row strides must be multiples of 16 bytes");
     s->kv_elem = e;
     s->k_scale = s->v_scale = 1.f;
-    if (a->kv_format == SHIFTATTN_KV_FP8_E4M3) {
+    s->block_scales = false;
+    s->kv_scales = nullptr;
+    if (a->kv_format == SHIFTATTN_KV_FP8_E4M3_BLOCKS) {
+        if (a->head_dim % 16) return fail(SHIFTATTN_EUNSUPPORTED, "head_dim = %d: an FP8 cache needs a multiple of 16", a->head_dim);
+        s->kv_elem = 1;
+        s->block_scales = true;
+    } else if (a->kv_format == SHIFTATTN_KV_FP8_E4M3) {
         if (!(a->k_scale > 0.f) || !(a->v_scale > 0.f) || a->k_scale > 3.0e38f || a->v_scale > 3.0e38f)
             return fail(SHIFTATTN_EINVAL, "k_scale and v_scale of an FP8 cache must be positive and finite");
         if (a->head_dim % 16) return fail(SHIFTATTN_EUNSUPPORTED, "head_dim = %d: an FP8 cache needs a multiple of 16", a->head_dim);
@@ -148,6 +154,17 @@ int check_attn(const shiftattn_attn* a, AttnShape* s) {
     return 0;
 }
 
+// The scales of a call: those of the entry points named _scaled, for a cache that has them, and none for the others.
+int check_scales(bool scaled, float* kv_scales, AttnShape* s) {
+    if (scaled != s->block_scales)
+        return fail(SHIFTATTN_EINVAL, scaled ? "the cache of this call has a scale for each block: kv_format must be SHIFTATTN_KV_FP8_E4M3_BLOCKS"
+                                             : "a cache with a scale for each block goes to the calls named _scaled");
+    if (scaled && (!kv_scales || (reinterpret_cast<uintptr_t>(kv_scales) & 7)))
+        return fail(SHIFTATTN_EINVAL, "kv_scales is NULL or not 8-byte aligned");
+    s->kv_scales = kv_scales;
+    return 0;
+}
+
 int check_new_kv(const void* k_new, const void* v_new, const int64_t* slots, bool* present) {
     const int n = (k_new != nullptr) + (v_new != nullptr) + (slots != nullptr);
     if (n != 0 && n != 3) return fail(SHIFTATTN_EINVAL, "k_new, v_new and slot_mapping must be all NULL or all set");
@@ -158,10 +175,10 @@ int check_new_kv(const void* k_new, const void* v_new, const int64_t* slots, boo
 }
 
 bool use_prefill_mfma(const AttnShape& s, int num_seqs, int max_seq_len) {
-    return !force_generic() && prefill_mfma_supported(s, num_seqs, max_seq_len);
+    return !force_generic() && !s.block_scales && prefill_mfma_supported(s, num_seqs, max_seq_len);
 }
 bool use_decode_mfma(const AttnShape& s, int num_seqs, int max_seq_len) {
-    return !force_generic() && decode_mfma_supported(s, num_seqs, max_seq_len);
+    return !force_generic() && !s.block_scales && decode_mfma_supported(s, num_seqs, max_seq_len);
 }
 
 // Argument checks of a prefill / decode call that need no launch (shared with the mixed entry point, which must
@@ -193,6 +210,25 @@ int check_decode_args(const void* q, const void* kv_cache, const int32_t* block_
         return fail(SHIFTATTN_EINVAL, "q / out / kv_cache must be 16-byte aligned");
     if (static_cast<int64_t>(s.max_blocks) * kBlockSize < max_seq_len)
         return fail(SHIFTATTN_EINVAL, "max_blocks_per_seq = %d cannot hold max_seq_len = %d", s.max_blocks, max_seq_len);
+    return 0;
+}
+
+bool aligned_to(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+int check_tables(const shiftattn_tables* t, const void* workspace, size_t workspace_bytes) {
+    if (!t) return fail(SHIFTATTN_EINVAL, "tables descriptor is NULL");
+    if (t->num_seqs < 0 || t->max_blocks_per_seq < 0 || t->num_blocks < 0)
+        return fail(SHIFTATTN_EINVAL, "num_seqs = %d, max_blocks_per_seq = %d, num_blocks = %d", t->num_seqs, t->max_blocks_per_seq, t->num_blocks);
+    if (t->reserved != 0) return fail(SHIFTATTN_EINVAL, "reserved field must be 0");
+    if (!t->free_count || (t->num_seqs > 0 && (!t->seq_lens || (t->max_blocks_per_seq > 0 && !t->block_table))) ||
+        (t->num_blocks > 0 && !t->free_blocks))
+        return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (!aligned_to(t->seq_lens, 4) || !aligned_to(t->free_count, 4) || !aligned_to(t->block_table, 4) || !aligned_to(t->free_blocks, 4))
+        return fail(SHIFTATTN_EINVAL, "the tables' arrays must be 4-byte aligned");
+    const size_t need = tables_workspace(t->num_seqs);
+    if (!workspace || workspace_bytes < need || !aligned_to(workspace, 4))
+        return fail(SHIFTATTN_EWORKSPACE, "tables of %d sequences need %zu workspace bytes, got %zu", t->num_seqs, need,
+                    workspace ? workspace_bytes : static_cast<size_t>(0));
     return 0;
 }
 
@@ -229,6 +265,156 @@ int option_prefill_splits() { return g_options[SHIFTATTN_OPT_PREFILL_SPLITS].loa
 int option_prefill_pairing() { return g_options[SHIFTATTN_OPT_PREFILL_PAIRING].load(std::memory_order_relaxed); }
 int option_prefill_scaled_q() { return g_options[SHIFTATTN_OPT_PREFILL_SCALED_Q].load(std::memory_order_relaxed); }
 }  // namespace shiftattn
+
+// ---- the attention calls; scaled: the cache has a scale for each block, in kv_scales -----------------------------------
+namespace {
+
+int kv_write(bool scaled, float* kv_scales, const void* k_new, const void* v_new, const int64_t* slot_mapping, int32_t n_tokens,
+                       void* kv_cache, const shiftattn_attn* a, void* stream) {
+    AttnShape s;
+    if (int rc = check_attn(a, &s)) return rc;
+    if (n_tokens < 0) return fail(SHIFTATTN_EINVAL, "n_tokens = %d", n_tokens);
+    if (n_tokens == 0) return SHIFTATTN_OK;
+    if (int rc = check_scales(scaled, kv_scales, &s)) return rc;
+    if (!k_new || !v_new || !slot_mapping || !kv_cache) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(kv_cache))
+        return fail(SHIFTATTN_EINVAL, "k_new / v_new / kv_cache must be 16-byte aligned");
+    hipError_t e = launch_kv_write(k_new, v_new, slot_mapping, n_tokens, kv_cache, s, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "kv_write launch");
+}
+
+int prefill(bool scaled, float* kv_scales, const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
+                      const int32_t* block_table, const int32_t* cu_seqlens_q, const int32_t* seq_lens,
+                      int32_t num_seqs, int32_t total_q, int32_t max_q_len, int32_t max_seq_len, void* out,
+                      void* workspace, size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
+    AttnShape s;
+    if (int rc = check_attn(a, &s)) return rc;
+    if (int rc = check_scales(scaled, kv_scales, &s)) return rc;
+    bool new_kv;
+    if (int rc = check_new_kv(k_new, v_new, slot_mapping, &new_kv)) return rc;
+    if (int rc = check_prefill_args(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, max_q_len,
+                                    max_seq_len, out, s))
+        return rc;
+    if (num_seqs == 0 || total_q == 0) return SHIFTATTN_OK;
+    const bool mfma = use_prefill_mfma(s, num_seqs, max_seq_len);
+    const size_t need = mfma ? prefill_mfma_least_workspace(num_seqs, total_q, max_q_len, max_seq_len, s) : 0;
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+        return fail(SHIFTATTN_EWORKSPACE, "prefill needs %zu workspace bytes, got %zu", need,
+                    workspace ? workspace_bytes : static_cast<size_t>(0));
+    if (mfma)
+        if (int rc = ensure_device_ready()) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    if (new_kv) {
+        e = launch_kv_write(k_new, v_new, slot_mapping, total_q, kv_cache, s, st);
+        if (e != hipSuccess) return hip_fail(e, "kv_write launch");
+    }
+    if (mfma)
+        e = launch_prefill_mfma(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, max_q_len,
+                                max_seq_len, out, workspace, workspace && aligned16(workspace) ? workspace_bytes : 0, s, st);
+    else if (!force_generic() && prefill_f32_supported(s))
+        e = launch_prefill_f32(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, out, s, st);
+    else
+        e = launch_attn_generic(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, out, s, st);
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "prefill launch");
+}
+
+int decode(bool scaled, float* kv_scales, const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
+                     const int32_t* block_table, const int32_t* seq_lens, int32_t num_seqs, int32_t max_seq_len,
+                     void* out, void* workspace, size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
+    AttnShape s;
+    if (int rc = check_attn(a, &s)) return rc;
+    if (int rc = check_scales(scaled, kv_scales, &s)) return rc;
+    bool new_kv;
+    if (int rc = check_new_kv(k_new, v_new, slot_mapping, &new_kv)) return rc;
+    if (int rc = check_decode_args(q, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, out, s)) return rc;
+    if (num_seqs == 0) return SHIFTATTN_OK;
+    const bool mfma = use_decode_mfma(s, num_seqs, max_seq_len);
+    const size_t need = mfma ? decode_mfma_workspace(num_seqs, max_seq_len, s) : 0;
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+        return fail(SHIFTATTN_EWORKSPACE, "decode needs %zu workspace bytes, got %zu", need,
+                    workspace ? workspace_bytes : static_cast<size_t>(0));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    hipError_t e;
+    // the tuned kernel appends the new tokens itself where it can; otherwise a write kernel runs in front
+    const bool fused_append = new_kv && mfma && decode_mfma_appends(num_seqs, s);
+    if (new_kv && !fused_append) {
+        e = launch_kv_write(k_new, v_new, slot_mapping, num_seqs, kv_cache, s, st);
+        if (e != hipSuccess) return hip_fail(e, "kv_write launch");
+    }
+    if (mfma)
+        e = launch_decode_mfma(q, fused_append ? k_new : nullptr, fused_append ? v_new : nullptr,
+                               fused_append ? slot_mapping : nullptr, kv_cache, block_table, seq_lens, num_seqs, max_seq_len,
+                               out, workspace, s, st);
+    else
+        e = launch_attn_generic(q, kv_cache, block_table, nullptr, seq_lens, num_seqs, num_seqs, out, s, st);
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "decode launch");
+}
+
+int mixed(bool scaled, float* kv_scales, const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
+                    const int32_t* block_table, const int32_t* cu_seqlens_q, const int32_t* seq_lens,
+                    int32_t num_prefill_seqs, int32_t total_prefill_q, int32_t max_q_len, int32_t max_prefill_seq_len,
+                    int32_t num_decode_seqs, int32_t max_decode_seq_len, void* out, void* workspace,
+                    size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
+    AttnShape s;
+    if (int rc = check_attn(a, &s)) return rc;
+    if (int rc = check_scales(scaled, kv_scales, &s)) return rc;
+    if (num_prefill_seqs < 0 || total_prefill_q < 0 || max_q_len < 0 || max_prefill_seq_len < 0 || num_decode_seqs < 0 ||
+        max_decode_seq_len < 0)
+        return fail(SHIFTATTN_EINVAL, "negative size argument");
+    if (num_prefill_seqs == 0 && total_prefill_q != 0)
+        return fail(SHIFTATTN_EINVAL, "total_prefill_q = %d without prefill sequences", total_prefill_q);
+    bool new_kv;
+    if (int rc = check_new_kv(k_new, v_new, slot_mapping, &new_kv)) return rc;
+    const int64_t rows = static_cast<int64_t>(total_prefill_q) + num_decode_seqs;
+    if (rows > INT32_MAX) return fail(SHIFTATTN_EINVAL, "batch of %lld rows is too large", static_cast<long long>(rows));
+    if (rows == 0) return SHIFTATTN_OK;
+    if (!q || !kv_cache || !block_table || !seq_lens || !out || (num_prefill_seqs > 0 && !cu_seqlens_q))
+        return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    const size_t need_p = num_prefill_seqs > 0 && total_prefill_q > 0 && use_prefill_mfma(s, num_prefill_seqs, max_prefill_seq_len)
+                              ? prefill_mfma_least_workspace(num_prefill_seqs, total_prefill_q, max_q_len, max_prefill_seq_len, s) : 0;
+    const size_t need_d = shiftattn_decode_workspace_bytes(num_decode_seqs, max_decode_seq_len, a);
+    const size_t need = need_p > need_d ? need_p : need_d;
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+        return fail(SHIFTATTN_EWORKSPACE, "mixed batch needs %zu workspace bytes, got %zu", need,
+                    workspace ? workspace_bytes : static_cast<size_t>(0));
+    // everything the two parts would refuse is refused here, before the cache is touched
+    const size_t q_off = static_cast<size_t>(total_prefill_q) * s.q_stride * s.elem;
+    const size_t o_off = static_cast<size_t>(total_prefill_q) * s.out_stride * s.elem;
+    const int32_t* table_d = block_table + static_cast<size_t>(num_prefill_seqs) * s.max_blocks;
+    if (int rc = check_prefill_args(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_prefill_seqs, total_prefill_q,
+                                    max_q_len, max_prefill_seq_len, out, s))
+        return rc;
+    if (int rc = check_decode_args(static_cast<const char*>(q) + q_off, kv_cache, table_d, seq_lens + num_prefill_seqs,
+                                   num_decode_seqs, max_decode_seq_len, static_cast<char*>(out) + o_off, s))
+        return rc;
+    if (new_kv) {
+        if (!aligned16(kv_cache)) return fail(SHIFTATTN_EINVAL, "kv_cache must be 16-byte aligned");
+        hipError_t e = launch_kv_write(k_new, v_new, slot_mapping, static_cast<int>(rows), kv_cache, s,
+                                       static_cast<hipStream_t>(stream));
+        if (e != hipSuccess) return hip_fail(e, "kv_write launch");
+    }
+    if (workspace && aligned16(workspace) && use_prefill_mfma(s, num_prefill_seqs, max_prefill_seq_len) &&
+        use_decode_mfma(s, num_decode_seqs, max_decode_seq_len)) {
+        if (int rc = ensure_device_ready()) return rc;
+        hipError_t e = hipSuccess;
+        if (launch_prefill_and_decode(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_prefill_seqs, total_prefill_q, max_q_len,
+                                      max_prefill_seq_len, num_decode_seqs, max_decode_seq_len, out, workspace, workspace_bytes, s,
+                                      static_cast<hipStream_t>(stream), &e))
+            return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "mixed launch");
+    }
+    // the two kinds of rows go to the kernel built for each; both read the cache written above
+    if (int rc = prefill(scaled, kv_scales, q, nullptr, nullptr, nullptr, kv_cache, block_table, cu_seqlens_q, seq_lens,
+                                   num_prefill_seqs, total_prefill_q, max_q_len, max_prefill_seq_len, out, workspace,
+                                   workspace_bytes, a, stream))
+        return rc;
+    return decode(scaled, kv_scales, static_cast<const char*>(q) + q_off, nullptr, nullptr, nullptr, kv_cache, table_d,
+                            seq_lens + num_prefill_seqs,
+                            num_decode_seqs, max_decode_seq_len, static_cast<char*>(out) + o_off, workspace, workspace_bytes,
+                            a, stream);
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -516,19 +702,6 @@ int shiftattn_unpack_o_proj_fp8(const void* recv_codes, const float* a_scales, c
     return shiftattn_unpack_o_proj_fp8_ws(recv_codes, a_scales, w_codes, w_scales, out, T, T_pad, d_model, xc, nullptr, 0, stream);
 }
 
-int shiftattn_kv_write(const void* k_new, const void* v_new, const int64_t* slot_mapping, int32_t n_tokens,
-                       void* kv_cache, const shiftattn_attn* a, void* stream) {
-    AttnShape s;
-    if (int rc = check_attn(a, &s)) return rc;
-    if (n_tokens < 0) return fail(SHIFTATTN_EINVAL, "n_tokens = %d", n_tokens);
-    if (n_tokens == 0) return SHIFTATTN_OK;
-    if (!k_new || !v_new || !slot_mapping || !kv_cache) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
-    if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(kv_cache))
-        return fail(SHIFTATTN_EINVAL, "k_new / v_new / kv_cache must be 16-byte aligned");
-    hipError_t e = launch_kv_write(k_new, v_new, slot_mapping, n_tokens, kv_cache, s, static_cast<hipStream_t>(stream));
-    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "kv_write launch");
-}
-
 size_t shiftattn_prefill_workspace_bytes(int32_t num_seqs, int32_t total_q, int32_t max_q_len, int32_t max_seq_len,
                                          const shiftattn_attn* a) {
     AttnShape s;
@@ -542,72 +715,6 @@ size_t shiftattn_decode_workspace_bytes(int32_t num_seqs, int32_t max_seq_len, c
     if (check_attn(a, &s) || num_seqs < 0 || max_seq_len < 0) return SIZE_MAX;
     if (!use_decode_mfma(s, num_seqs, max_seq_len) || num_seqs == 0) return 0;
     return decode_mfma_workspace(num_seqs, max_seq_len, s);
-}
-
-int shiftattn_prefill(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
-                      const int32_t* block_table, const int32_t* cu_seqlens_q, const int32_t* seq_lens,
-                      int32_t num_seqs, int32_t total_q, int32_t max_q_len, int32_t max_seq_len, void* out,
-                      void* workspace, size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
-    AttnShape s;
-    if (int rc = check_attn(a, &s)) return rc;
-    bool new_kv;
-    if (int rc = check_new_kv(k_new, v_new, slot_mapping, &new_kv)) return rc;
-    if (int rc = check_prefill_args(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, max_q_len,
-                                    max_seq_len, out, s))
-        return rc;
-    if (num_seqs == 0 || total_q == 0) return SHIFTATTN_OK;
-    const bool mfma = use_prefill_mfma(s, num_seqs, max_seq_len);
-    const size_t need = mfma ? prefill_mfma_least_workspace(num_seqs, total_q, max_q_len, max_seq_len, s) : 0;
-    if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
-        return fail(SHIFTATTN_EWORKSPACE, "prefill needs %zu workspace bytes, got %zu", need,
-                    workspace ? workspace_bytes : static_cast<size_t>(0));
-    if (mfma)
-        if (int rc = ensure_device_ready()) return rc;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    hipError_t e;
-    if (new_kv) {
-        e = launch_kv_write(k_new, v_new, slot_mapping, total_q, kv_cache, s, st);
-        if (e != hipSuccess) return hip_fail(e, "kv_write launch");
-    }
-    if (mfma)
-        e = launch_prefill_mfma(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, max_q_len,
-                                max_seq_len, out, workspace, workspace && aligned16(workspace) ? workspace_bytes : 0, s, st);
-    else if (!force_generic() && prefill_f32_supported(s))
-        e = launch_prefill_f32(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, out, s, st);
-    else
-        e = launch_attn_generic(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, out, s, st);
-    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "prefill launch");
-}
-
-int shiftattn_decode(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
-                     const int32_t* block_table, const int32_t* seq_lens, int32_t num_seqs, int32_t max_seq_len,
-                     void* out, void* workspace, size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
-    AttnShape s;
-    if (int rc = check_attn(a, &s)) return rc;
-    bool new_kv;
-    if (int rc = check_new_kv(k_new, v_new, slot_mapping, &new_kv)) return rc;
-    if (int rc = check_decode_args(q, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, out, s)) return rc;
-    if (num_seqs == 0) return SHIFTATTN_OK;
-    const bool mfma = use_decode_mfma(s, num_seqs, max_seq_len);
-    const size_t need = mfma ? decode_mfma_workspace(num_seqs, max_seq_len, s) : 0;
-    if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
-        return fail(SHIFTATTN_EWORKSPACE, "decode needs %zu workspace bytes, got %zu", need,
-                    workspace ? workspace_bytes : static_cast<size_t>(0));
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    hipError_t e;
-    // the tuned kernel appends the new tokens itself where it can; otherwise a write kernel runs in front
-    const bool fused_append = new_kv && mfma && decode_mfma_appends(num_seqs, s);
-    if (new_kv && !fused_append) {
-        e = launch_kv_write(k_new, v_new, slot_mapping, num_seqs, kv_cache, s, st);
-        if (e != hipSuccess) return hip_fail(e, "kv_write launch");
-    }
-    if (mfma)
-        e = launch_decode_mfma(q, fused_append ? k_new : nullptr, fused_append ? v_new : nullptr,
-                               fused_append ? slot_mapping : nullptr, kv_cache, block_table, seq_lens, num_seqs, max_seq_len,
-                               out, workspace, s, st);
-    else
-        e = launch_attn_generic(q, kv_cache, block_table, nullptr, seq_lens, num_seqs, num_seqs, out, s, st);
-    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "decode launch");
 }
 
 int shiftattn_decode_static(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
@@ -661,66 +768,88 @@ int shiftattn_prefill_plan(int32_t num_prefill_seqs, int32_t total_prefill_q, in
     return SHIFTATTN_OK;
 }
 
+int shiftattn_kv_write(const void* k_new, const void* v_new, const int64_t* slot_mapping, int32_t n_tokens, void* kv_cache,
+                       const shiftattn_attn* a, void* stream) {
+    return kv_write(false, nullptr, k_new, v_new, slot_mapping, n_tokens, kv_cache, a, stream);
+}
+
+int shiftattn_kv_write_scaled(const void* k_new, const void* v_new, const int64_t* slot_mapping, int32_t n_tokens, void* kv_cache,
+                              float* kv_scales, const shiftattn_attn* a, void* stream) {
+    return kv_write(true, kv_scales, k_new, v_new, slot_mapping, n_tokens, kv_cache, a, stream);
+}
+
+int shiftattn_prefill(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
+                      const int32_t* block_table, const int32_t* cu_seqlens_q, const int32_t* seq_lens,
+                      int32_t num_seqs, int32_t total_q, int32_t max_q_len, int32_t max_seq_len, void* out,
+                      void* workspace, size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
+    return prefill(false, nullptr, q, k_new, v_new, slot_mapping, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q,
+                   max_q_len, max_seq_len, out, workspace, workspace_bytes, a, stream);
+}
+
+int shiftattn_prefill_scaled(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
+                             float* kv_scales, const int32_t* block_table, const int32_t* cu_seqlens_q, const int32_t* seq_lens,
+                             int32_t num_seqs, int32_t total_q, int32_t max_q_len, int32_t max_seq_len, void* out,
+                             void* workspace, size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
+    return prefill(true, kv_scales, q, k_new, v_new, slot_mapping, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q,
+                   max_q_len, max_seq_len, out, workspace, workspace_bytes, a, stream);
+}
+
+int shiftattn_decode(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
+                     const int32_t* block_table, const int32_t* seq_lens, int32_t num_seqs, int32_t max_seq_len,
+                     void* out, void* workspace, size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
+    return decode(false, nullptr, q, k_new, v_new, slot_mapping, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, out, workspace,
+                  workspace_bytes, a, stream);
+}
+
+int shiftattn_decode_scaled(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
+                            float* kv_scales, const int32_t* block_table, const int32_t* seq_lens, int32_t num_seqs, int32_t max_seq_len,
+                            void* out, void* workspace, size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
+    return decode(true, kv_scales, q, k_new, v_new, slot_mapping, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, out, workspace,
+                  workspace_bytes, a, stream);
+}
+
 int shiftattn_mixed(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
                     const int32_t* block_table, const int32_t* cu_seqlens_q, const int32_t* seq_lens,
                     int32_t num_prefill_seqs, int32_t total_prefill_q, int32_t max_q_len, int32_t max_prefill_seq_len,
                     int32_t num_decode_seqs, int32_t max_decode_seq_len, void* out, void* workspace,
                     size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
-    AttnShape s;
-    if (int rc = check_attn(a, &s)) return rc;
-    if (num_prefill_seqs < 0 || total_prefill_q < 0 || max_q_len < 0 || max_prefill_seq_len < 0 || num_decode_seqs < 0 ||
-        max_decode_seq_len < 0)
-        return fail(SHIFTATTN_EINVAL, "negative size argument");
-    if (num_prefill_seqs == 0 && total_prefill_q != 0)
-        return fail(SHIFTATTN_EINVAL, "total_prefill_q = %d without prefill sequences", total_prefill_q);
-    bool new_kv;
-    if (int rc = check_new_kv(k_new, v_new, slot_mapping, &new_kv)) return rc;
-    const int64_t rows = static_cast<int64_t>(total_prefill_q) + num_decode_seqs;
-    if (rows > INT32_MAX) return fail(SHIFTATTN_EINVAL, "batch of %lld rows is too large", static_cast<long long>(rows));
-    if (rows == 0) return SHIFTATTN_OK;
-    if (!q || !kv_cache || !block_table || !seq_lens || !out || (num_prefill_seqs > 0 && !cu_seqlens_q))
+    return mixed(false, nullptr, q, k_new, v_new, slot_mapping, kv_cache, block_table, cu_seqlens_q, seq_lens, num_prefill_seqs,
+                 total_prefill_q, max_q_len, max_prefill_seq_len, num_decode_seqs, max_decode_seq_len, out, workspace, workspace_bytes, a, stream);
+}
+
+int shiftattn_mixed_scaled(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,
+                           float* kv_scales, const int32_t* block_table, const int32_t* cu_seqlens_q, const int32_t* seq_lens,
+                           int32_t num_prefill_seqs, int32_t total_prefill_q, int32_t max_q_len, int32_t max_prefill_seq_len,
+                           int32_t num_decode_seqs, int32_t max_decode_seq_len, void* out, void* workspace,
+                           size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
+    return mixed(true, kv_scales, q, k_new, v_new, slot_mapping, kv_cache, block_table, cu_seqlens_q, seq_lens, num_prefill_seqs,
+                 total_prefill_q, max_q_len, max_prefill_seq_len, num_decode_seqs, max_decode_seq_len, out, workspace, workspace_bytes, a, stream);
+}
+
+size_t shiftattn_tables_workspace_bytes(int32_t num_seqs) { return num_seqs < 0 ? SIZE_MAX : tables_workspace(num_seqs); }
+
+int shiftattn_tables_append(const shiftattn_tables* t, const int32_t* new_lens, int32_t num_prefill_seqs, int32_t total_prefill_q, int32_t rows,
+                            int32_t* cu_seqlens_q, int64_t* slot_mapping, int32_t* taken, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_tables(t, workspace, workspace_bytes)) return rc;
+    if (num_prefill_seqs < 0 || num_prefill_seqs > t->num_seqs || total_prefill_q < 0 || rows < 0)
+        return fail(SHIFTATTN_EINVAL, "num_prefill_seqs = %d of %d, total_prefill_q = %d, rows = %d", num_prefill_seqs, t->num_seqs, total_prefill_q, rows);
+    if (static_cast<int64_t>(total_prefill_q) + t->num_seqs - num_prefill_seqs > rows)
+        return fail(SHIFTATTN_EINVAL, "rows = %d: %d rows of chunks and %d decode rows do not fit", rows, total_prefill_q, t->num_seqs - num_prefill_seqs);
+    if (!cu_seqlens_q || (rows > 0 && !slot_mapping) || (t->num_seqs > 0 && (!new_lens || !taken)))
         return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
-    const size_t need_p = num_prefill_seqs > 0 && total_prefill_q > 0 && use_prefill_mfma(s, num_prefill_seqs, max_prefill_seq_len)
-                              ? prefill_mfma_least_workspace(num_prefill_seqs, total_prefill_q, max_q_len, max_prefill_seq_len, s) : 0;
-    const size_t need_d = shiftattn_decode_workspace_bytes(num_decode_seqs, max_decode_seq_len, a);
-    const size_t need = need_p > need_d ? need_p : need_d;
-    if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
-        return fail(SHIFTATTN_EWORKSPACE, "mixed batch needs %zu workspace bytes, got %zu", need,
-                    workspace ? workspace_bytes : static_cast<size_t>(0));
-    // everything the two parts would refuse is refused here, before the cache is touched
-    const size_t q_off = static_cast<size_t>(total_prefill_q) * s.q_stride * s.elem;
-    const size_t o_off = static_cast<size_t>(total_prefill_q) * s.out_stride * s.elem;
-    const int32_t* table_d = block_table + static_cast<size_t>(num_prefill_seqs) * s.max_blocks;
-    if (int rc = check_prefill_args(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_prefill_seqs, total_prefill_q,
-                                    max_q_len, max_prefill_seq_len, out, s))
-        return rc;
-    if (int rc = check_decode_args(static_cast<const char*>(q) + q_off, kv_cache, table_d, seq_lens + num_prefill_seqs,
-                                   num_decode_seqs, max_decode_seq_len, static_cast<char*>(out) + o_off, s))
-        return rc;
-    if (new_kv) {
-        if (!aligned16(kv_cache)) return fail(SHIFTATTN_EINVAL, "kv_cache must be 16-byte aligned");
-        hipError_t e = launch_kv_write(k_new, v_new, slot_mapping, static_cast<int>(rows), kv_cache, s,
-                                       static_cast<hipStream_t>(stream));
-        if (e != hipSuccess) return hip_fail(e, "kv_write launch");
-    }
-    if (workspace && aligned16(workspace) && use_prefill_mfma(s, num_prefill_seqs, max_prefill_seq_len) &&
-        use_decode_mfma(s, num_decode_seqs, max_decode_seq_len)) {
-        if (int rc = ensure_device_ready()) return rc;
-        hipError_t e = hipSuccess;
-        if (launch_prefill_and_decode(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_prefill_seqs, total_prefill_q, max_q_len,
-                                      max_prefill_seq_len, num_decode_seqs, max_decode_seq_len, out, workspace, workspace_bytes, s,
-                                      static_cast<hipStream_t>(stream), &e))
-            return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "mixed launch");
-    }
-    // the two kinds of rows go to the kernel built for each; both read the cache written above
-    if (int rc = shiftattn_prefill(q, nullptr, nullptr, nullptr, kv_cache, block_table, cu_seqlens_q, seq_lens,
-                                   num_prefill_seqs, total_prefill_q, max_q_len, max_prefill_seq_len, out, workspace,
-                                   workspace_bytes, a, stream))
-        return rc;
-    return shiftattn_decode(static_cast<const char*>(q) + q_off, nullptr, nullptr, nullptr, kv_cache, table_d,
-                            seq_lens + num_prefill_seqs,
-                            num_decode_seqs, max_decode_seq_len, static_cast<char*>(out) + o_off, workspace, workspace_bytes,
-                            a, stream);
+    if (!aligned_to(slot_mapping, 8) || !aligned_to(new_lens, 4) || !aligned_to(cu_seqlens_q, 4) || !aligned_to(taken, 4))
+        return fail(SHIFTATTN_EINVAL, "slot_mapping must be 8-byte aligned, the int32 arrays 4-byte");
+    hipError_t e = launch_tables_append(*t, new_lens, num_prefill_seqs, total_prefill_q, rows, cu_seqlens_q, slot_mapping, taken, workspace,
+                                        static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "tables_append launch");
+}
+
+int shiftattn_tables_truncate(const shiftattn_tables* t, const int32_t* keep_lens, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_tables(t, workspace, workspace_bytes)) return rc;
+    if (t->num_seqs == 0) return SHIFTATTN_OK;
+    if (!keep_lens || !aligned_to(keep_lens, 4)) return fail(SHIFTATTN_EINVAL, "keep_lens is NULL or not 4-byte aligned");
+    hipError_t e = launch_tables_truncate(*t, keep_lens, workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "tables_truncate launch");
 }
 
 }  // extern "C"

@@ -28,6 +28,8 @@ struct AttnShape {
     int64_t q_stride, kv_stride, out_stride;  // in elements
     int kv_elem;                  // bytes per cache element: elem, or 1 for an FP8 E4M3 cache
     float k_scale, v_scale;       // FP8 cache: value = code value * scale (1 otherwise)
+    bool block_scales;            // FP8 cache with a scale per (block, KV head, part) instead: value = code value * kv_scales[block][head][part]
+    float* kv_scales;
     bool kv_fp8() const { return kv_elem == 1; }
 };
 
@@ -41,6 +43,16 @@ hipError_t launch_kv_write(const void* k_new, const void* v_new, const int64_t* 
 hipError_t launch_fp8_blocks_to_bf16(const void* cache_fp8, const int32_t* block_table, int max_blocks,
                                      const int32_t* seq_lens, int num_seqs, int nb, int hkv_l, void* scratch_bf16,
                                      int32_t* table_out, hipStream_t st);
+
+// scaled_cache.hip : the append of an FP8 cache with block scales (any dtype / head_dim)
+hipError_t launch_kv_write_scaled(const void* k_new, const void* v_new, const int64_t* slots, int n_tokens, void* cache,
+                                  const AttnShape& a, hipStream_t st);
+
+// tables.hip : block tables, slot maps and row offsets from request lengths
+size_t tables_workspace(int num_seqs);
+hipError_t launch_tables_append(const shiftattn_tables& t, const int32_t* new_lens, int num_prefill, int total_prefill_q, int rows, int32_t* cu,
+                                int64_t* slots, int32_t* taken, void* workspace, hipStream_t st);
+hipError_t launch_tables_truncate(const shiftattn_tables& t, const int32_t* keep_lens, void* workspace, hipStream_t st);
 
 // attn_generic.hip : any dtype / head_dim / head ratio, one wavefront per (token, head) row
 hipError_t launch_attn_generic(const void* q, const void* cache, const int32_t* block_table,

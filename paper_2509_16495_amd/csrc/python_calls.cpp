@@ -21,6 +21,9 @@ namespace {
     F(mixed, mixed) F(kv_write, kv_write) F(qkv, qkv_proj_pack_ws) F(o_proj, unpack_o_proj_ws) F(qkv_plain, qkv_proj_pack)   \
     F(o_proj_plain, unpack_o_proj) F(qkv_fp8, qkv_proj_pack_fp8_ws) F(o_proj_fp8, unpack_o_proj_fp8_ws)                      \
     F(quantize_rows, quantize_rows_fp8) F(quantize_recv, quantize_recv_fp8)                                                 \
+    F(prefill_scaled, prefill_scaled) F(decode_scaled, decode_scaled) F(mixed_scaled, mixed_scaled)                         \
+    F(kv_write_scaled, kv_write_scaled) F(tables_append, tables_append) F(tables_truncate, tables_truncate)                 \
+    F(tables_bytes, tables_workspace_bytes)                                                                                 \
     F(prefill_bytes, prefill_workspace_bytes) F(decode_bytes, decode_workspace_bytes) F(mixed_bytes, mixed_workspace_bytes)
 struct Library {
 #define SHIFTATTN_POINTER(member, name) decltype(&shiftattn_##name) member;
@@ -98,8 +101,17 @@ int64_t local_kv_heads(int64_t P, int64_t h_kv) { return h_kv == 0 ? 0 : h_kv >=
 
 constexpr int64_t kBlock = 16;
 
+// whether the cache has a scale for each block and head, which then fit it
+bool scales_of(const at::Tensor* s, const at::Tensor& cache) {
+    if (!s) return false;
+    need(cache.scalar_type() == at::kByte && s->scalar_type() == at::kFloat && s->dim() == 3 && s->size(0) == cache.size(0) && s->size(1) == cache.size(1) &&
+             s->size(2) == 2 && s->is_contiguous(),
+         "kv_scales: contiguous float32 [num_blocks, hkv_l, 2] beside a uint8 kv_cache");
+    return true;
+}
+
 shiftattn_attn describe(const at::Tensor& q, const at::Tensor& cache, const at::Tensor& table, PyObject* scale, const at::Tensor* k_new,
-                        const at::Tensor* out, PyObject* k_scale, PyObject* v_scale) {
+                        const at::Tensor* out, PyObject* k_scale, PyObject* v_scale, const at::Tensor* kv_scales) {
     dims(q, 3, "q");
     dims(cache, 4, "kv_cache");
     const bool fp8 = cache.scalar_type() == at::kByte;
@@ -111,7 +123,7 @@ shiftattn_attn describe(const at::Tensor& q, const at::Tensor& cache, const at::
     a.block_size = kBlock, a.num_blocks = cut(cache.size(0)), a.max_blocks_per_seq = cut(table.size(1));
     a.softmax_scale = real(scale);
     a.q_stride = row_stride(q), a.kv_stride = k_new ? row_stride(*k_new) : 0, a.out_stride = out ? row_stride(*out) : 0;
-    a.kv_format = fp8 ? SHIFTATTN_KV_FP8_E4M3 : SHIFTATTN_KV_SAME;
+    a.kv_format = scales_of(kv_scales, cache) ? SHIFTATTN_KV_FP8_E4M3_BLOCKS : fp8 ? SHIFTATTN_KV_FP8_E4M3 : SHIFTATTN_KV_SAME;
     a.k_scale = real(k_scale), a.v_scale = real(v_scale);
     return a;
 }
@@ -231,48 +243,54 @@ SHIFTATTN_CALL(unpack_head2seq) {
 }
 
 // q, kv_cache, block_table, cu_seqlens_q, seq_lens, max_q_len, max_seq_len, out, softmax_scale, k_new, v_new, slot_mapping, workspace,
-// k_scale, v_scale
+// k_scale, v_scale, kv_scales
 SHIFTATTN_CALL(prefill) {
     Owned own;
-    return run(n, 15, [&] {
+    return run(n, 16, [&] {
         const at::Tensor &q = tensor(a[0]), &cache = tensor(a[1]), &table = tensor(a[2]), &cu = tensor(a[3]), &lens = tensor(a[4]), &out = tensor(a[7]);
         const at::Tensor *k = tensor_or_none(a[9]), *v = tensor_or_none(a[10]), *slots = tensor_or_none(a[11]);
         const int64_t seqs = lens.size(0);
         need(cu.scalar_type() == at::kInt && lens.scalar_type() == at::kInt && cu.size(0) == seqs + 1 && cu.is_contiguous() && lens.is_contiguous(),
              "cu_seqlens_q, seq_lens: contiguous int32 [num_seqs + 1], [num_seqs]");
         need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out: shape and type of q");
-        const shiftattn_attn d = describe(q, cache, table, a[8], k, &out, a[13], a[14]);
+        const at::Tensor* scales = tensor_or_none(a[15]);
+        const shiftattn_attn d = describe(q, cache, table, a[8], k, &out, a[13], a[14], scales);
         need(table.size(0) >= seqs, "block_table: a row per sequence");
         rows_of(q, out, k, v, slots, cache);
         const int32_t mq = whole(a[5]), ms = whole(a[6]);
         const at::Tensor* ws = workspace(a[12], a[0], own, [&] { return lib.prefill_bytes(cut(seqs), cut(q.size(0)), mq, ms, &d); });
         return [d, pq = ptr(q), pk = ptr(k), pv = ptr(v), ps = ptr(slots), pc = ptr(cache), pt = ptr(table), pu = ptr(cu), pl = ptr(lens), seqs = cut(seqs),
-                rows = cut(q.size(0)), mq, ms, po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream()] {
+                rows = cut(q.size(0)), mq, ms, po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream(), pb = static_cast<float*>(ptr(scales))] {
+            if (d.kv_format == SHIFTATTN_KV_FP8_E4M3_BLOCKS)
+                return lib.prefill_scaled(pq, pk, pv, static_cast<int64_t*>(ps), pc, pb, static_cast<int32_t*>(pt), static_cast<int32_t*>(pu),
+                                          static_cast<int32_t*>(pl), seqs, rows, mq, ms, po, pw, nw, &d, st);
             return lib.prefill(pq, pk, pv, static_cast<int64_t*>(ps), pc, static_cast<int32_t*>(pt), static_cast<int32_t*>(pu), static_cast<int32_t*>(pl),
                                seqs, rows, mq, ms, po, pw, nw, &d, st);
         };
     });
 }
 
-// q, kv_cache, block_table, seq_lens, max_seq_len, out, softmax_scale, k_new, v_new, slot_mapping, workspace, k_scale, v_scale; owned: the
-// library's scratch memory instead of a workspace
+// q, kv_cache, block_table, seq_lens, max_seq_len, out, softmax_scale, k_new, v_new, slot_mapping, workspace, k_scale, v_scale, kv_scales;
+// owned: the library's scratch memory instead of a workspace
 PyObject* decode_call(PyObject* const* a, Py_ssize_t n, bool owned) {
     Owned own;
-    return run(n, 13, [&] {
+    return run(n, 14, [&] {
         const at::Tensor &q = tensor(a[0]), &cache = tensor(a[1]), &table = tensor(a[2]), &lens = tensor(a[3]), &out = tensor(a[5]);
         const at::Tensor *k = tensor_or_none(a[7]), *v = tensor_or_none(a[8]), *slots = tensor_or_none(a[9]);
         dims(q, 3, "q");
         need(lens.scalar_type() == at::kInt && lens.size(0) == q.size(0) && lens.is_contiguous(), "seq_lens: contiguous int32 [num_seqs]");
         need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out: shape and type of q");
-        const shiftattn_attn d = describe(q, cache, table, a[6], k, &out, a[11], a[12]);
+        const at::Tensor* scales = tensor_or_none(a[13]);
+        const shiftattn_attn d = describe(q, cache, table, a[6], k, &out, a[11], a[12], scales);
         need(table.size(0) >= q.size(0), "block_table: a row per sequence");
         rows_of(q, out, k, v, slots, cache);
         const int32_t ms = whole(a[4]);
         const at::Tensor* ws = owned ? nullptr : workspace(a[10], a[0], own, [&] { return lib.decode_bytes(cut(q.size(0)), ms, &d); });
         return [d, pq = ptr(q), pk = ptr(k), pv = ptr(v), ps = ptr(slots), pc = ptr(cache), pt = ptr(table), pl = ptr(lens), seqs = cut(q.size(0)), ms,
-                po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream(), owned] {
+                po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream(), owned, pb = static_cast<float*>(ptr(scales))] {
             const auto* slot = static_cast<int64_t*>(ps);
             const auto *blocks = static_cast<int32_t*>(pt), *len = static_cast<int32_t*>(pl);
+            if (d.kv_format == SHIFTATTN_KV_FP8_E4M3_BLOCKS && !owned) return lib.decode_scaled(pq, pk, pv, slot, pc, pb, blocks, len, seqs, ms, po, pw, nw, &d, st);
             return owned ? lib.decode_static(pq, pk, pv, slot, pc, blocks, len, seqs, ms, po, &d, st)
                          : lib.decode(pq, pk, pv, slot, pc, blocks, len, seqs, ms, po, pw, nw, &d, st);
         };
@@ -282,10 +300,10 @@ SHIFTATTN_CALL(decode) { return decode_call(a, n, false); }
 SHIFTATTN_CALL(decode_static) { return decode_call(a, n, true); }
 
 // q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_prefill_seqs, max_q_len, max_prefill_seq_len, max_decode_seq_len, out, softmax_scale,
-// k_new, v_new, slot_mapping, workspace, k_scale, v_scale
+// k_new, v_new, slot_mapping, workspace, k_scale, v_scale, kv_scales
 SHIFTATTN_CALL(mixed) {
     Owned own;
-    return run(n, 17, [&] {
+    return run(n, 18, [&] {
         const at::Tensor &q = tensor(a[0]), &cache = tensor(a[1]), &table = tensor(a[2]), &cu = tensor(a[3]), &lens = tensor(a[4]), &out = tensor(a[9]);
         const at::Tensor *k = tensor_or_none(a[11]), *v = tensor_or_none(a[12]), *slots = tensor_or_none(a[13]);
         dims(q, 3, "q");
@@ -293,23 +311,29 @@ SHIFTATTN_CALL(mixed) {
         need(rows >= 0 && chunk_rows >= 0 && cu.size(0) == chunks + 1, "cu_seqlens_q: [num_prefill_seqs + 1], one row of q per other sequence");
         need(cu.scalar_type() == at::kInt && lens.scalar_type() == at::kInt && cu.is_contiguous() && lens.is_contiguous(), "cu_seqlens_q, seq_lens: contiguous int32");
         need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type() && table.size(0) == lens.size(0), "out: shape and type of q; block_table: a row per sequence");
-        const shiftattn_attn d = describe(q, cache, table, a[10], k, &out, a[15], a[16]);
+        const at::Tensor* scales = tensor_or_none(a[17]);
+        const shiftattn_attn d = describe(q, cache, table, a[10], k, &out, a[15], a[16], scales);
         rows_of(q, out, k, v, slots, cache);
         const int32_t mq = whole(a[6]), mp = whole(a[7]), md = whole(a[8]);
         const at::Tensor* ws = workspace(a[14], a[0], own, [&] { return lib.mixed_bytes(cut(chunks), cut(chunk_rows), mq, mp, cut(rows), md, &d); });
         return [d, pq = ptr(q), pk = ptr(k), pv = ptr(v), ps = ptr(slots), pc = ptr(cache), pt = ptr(table), pu = ptr(cu), pl = ptr(lens),
-                chunks = cut(chunks), chunk_rows = cut(chunk_rows), mq, mp, rows = cut(rows), md, po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream()] {
+                chunks = cut(chunks), chunk_rows = cut(chunk_rows), mq, mp, rows = cut(rows), md, po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream(),
+                pb = static_cast<float*>(ptr(scales))] {
+            if (d.kv_format == SHIFTATTN_KV_FP8_E4M3_BLOCKS)
+                return lib.mixed_scaled(pq, pk, pv, static_cast<int64_t*>(ps), pc, pb, static_cast<int32_t*>(pt), static_cast<int32_t*>(pu),
+                                        static_cast<int32_t*>(pl), chunks, chunk_rows, mq, mp, rows, md, po, pw, nw, &d, st);
             return lib.mixed(pq, pk, pv, static_cast<int64_t*>(ps), pc, static_cast<int32_t*>(pt), static_cast<int32_t*>(pu), static_cast<int32_t*>(pl),
                              chunks, chunk_rows, mq, mp, rows, md, po, pw, nw, &d, st);
         };
     });
 }
 
-// q, kv_cache, block_table, softmax_scale, k_new, out, k_scale, v_scale -> the descriptor's bytes
+// q, kv_cache, block_table, softmax_scale, k_new, out, k_scale, v_scale, kv_scales -> the descriptor's bytes
 SHIFTATTN_CALL(attn_desc) {
     PyObject* bytes = nullptr;
-    PyObject* done = run(n, 8, [&] {
-        const shiftattn_attn d = describe(tensor(a[0]), tensor(a[1]), tensor(a[2]), a[3], tensor_or_none(a[4]), tensor_or_none(a[5]), a[6], a[7]);
+    PyObject* done = run(n, 9, [&] {
+        const shiftattn_attn d = describe(tensor(a[0]), tensor(a[1]), tensor(a[2]), a[3], tensor_or_none(a[4]), tensor_or_none(a[5]), a[6], a[7],
+                                          tensor_or_none(a[8]));
         bytes = PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&d), sizeof(d));
         if (!bytes) throw PythonError{};
         return [] { return 0; };
@@ -318,9 +342,9 @@ SHIFTATTN_CALL(attn_desc) {
     return bytes;
 }
 
-// k_new, v_new, slot_mapping, kv_cache, k_scale, v_scale
+// k_new, v_new, slot_mapping, kv_cache, k_scale, v_scale, kv_scales
 SHIFTATTN_CALL(kv_write) {
-    return run(n, 6, [&] {
+    return run(n, 7, [&] {
         const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &slots = tensor(a[2]), &cache = tensor(a[3]);
         dims(k, 3, "k_new");
         apart(k);
@@ -334,11 +358,64 @@ SHIFTATTN_CALL(kv_write) {
         shiftattn_attn d{};
         d.num_q_heads = d.num_kv_heads = cut(k.size(1)), d.head_dim = cut(k.size(2)), d.dtype = dtype_code(k), d.block_size = kBlock;
         d.num_blocks = cut(cache.size(0)), d.softmax_scale = 1.0f, d.kv_stride = row_stride(k);
-        d.kv_format = cache.scalar_type() == at::kByte ? SHIFTATTN_KV_FP8_E4M3 : SHIFTATTN_KV_SAME;
+        const at::Tensor* scales = tensor_or_none(a[6]);
+        d.kv_format = scales_of(scales, cache) ? SHIFTATTN_KV_FP8_E4M3_BLOCKS : cache.scalar_type() == at::kByte ? SHIFTATTN_KV_FP8_E4M3 : SHIFTATTN_KV_SAME;
         d.k_scale = real(a[4]), d.v_scale = real(a[5]);
-        return [d, pk = ptr(k), pv = ptr(v), ps = ptr(slots), rows = cut(k.size(0)), pc = ptr(cache), st = stream()] {
+        return [d, pk = ptr(k), pv = ptr(v), ps = ptr(slots), rows = cut(k.size(0)), pc = ptr(cache), st = stream(), pb = static_cast<float*>(ptr(scales))] {
+            if (d.kv_format == SHIFTATTN_KV_FP8_E4M3_BLOCKS) return lib.kv_write_scaled(pk, pv, static_cast<int64_t*>(ps), rows, pc, pb, &d, st);
             return lib.kv_write(pk, pv, static_cast<int64_t*>(ps), rows, pc, &d, st);
         };
+    });
+}
+
+// the engine's tables, as both calls below take them
+shiftattn_tables tables_of(const at::Tensor& lens, const at::Tensor& table, const at::Tensor& free, const at::Tensor& count) {
+    dims(table, 2, "block_table");
+    need(lens.scalar_type() == at::kInt && lens.dim() == 1 && lens.is_contiguous() && table.scalar_type() == at::kInt && table.is_contiguous() &&
+             table.size(0) == lens.size(0),
+         "seq_lens: contiguous int32 [num_seqs], block_table: contiguous int32 [num_seqs, max_blocks]");
+    need(free.scalar_type() == at::kInt && free.dim() == 1 && free.is_contiguous() && count.scalar_type() == at::kInt && count.numel() == 1,
+         "free_blocks: contiguous int32 [num_blocks], free_count: one int32");
+    shiftattn_tables t{};
+    t.num_seqs = cut(lens.size(0)), t.max_blocks_per_seq = cut(table.size(1)), t.num_blocks = cut(free.size(0));
+    t.seq_lens = static_cast<int32_t*>(ptr(lens)), t.block_table = static_cast<int32_t*>(ptr(table));
+    t.free_blocks = static_cast<int32_t*>(ptr(free)), t.free_count = static_cast<int32_t*>(ptr(count));
+    return t;
+}
+
+// new_lens, num_prefill_seqs, total_prefill_q, seq_lens, block_table, free_blocks, free_count, cu_seqlens_q, slot_mapping, taken, workspace
+SHIFTATTN_CALL(tables_append) {
+    Owned own;
+    return run(n, 11, [&] {
+        const at::Tensor &fresh = tensor(a[0]), &lens = tensor(a[3]), &cu = tensor(a[7]), &slots = tensor(a[8]), &taken = tensor(a[9]);
+        const int32_t chunks = whole(a[1]), chunk_rows = whole(a[2]);
+        const at::Tensor &table = tensor(a[4]), &free = tensor(a[5]), &count = tensor(a[6]);
+        need(fresh.scalar_type() == at::kInt && taken.scalar_type() == at::kInt && fresh.sizes() == lens.sizes() && taken.sizes() == lens.sizes() &&
+                 fresh.is_contiguous() && taken.is_contiguous(),
+             "new_lens, taken: contiguous int32 [num_seqs]");
+        need(cu.scalar_type() == at::kInt && cu.dim() == 1 && cu.size(0) == static_cast<int64_t>(chunks) + 1 && cu.is_contiguous(),
+             "cu_seqlens_q: contiguous int32 [num_prefill_seqs + 1]");
+        need(slots.scalar_type() == at::kLong && slots.dim() == 1 && slots.is_contiguous(), "slot_mapping: contiguous int64 [rows]");
+        const shiftattn_tables t = tables_of(lens, table, free, count);
+        const at::Tensor* ws = workspace(a[10], a[3], own, [&] { return lib.tables_bytes(t.num_seqs); });
+        return [t, pn = ptr(fresh), chunks, chunk_rows, rows = cut(slots.size(0)), pu = ptr(cu), ps = ptr(slots), pt = ptr(taken), pw = ptr(ws), nw = bytes(ws),
+                st = stream()] {
+            return lib.tables_append(&t, static_cast<int32_t*>(pn), chunks, chunk_rows, rows, static_cast<int32_t*>(pu), static_cast<int64_t*>(ps),
+                                     static_cast<int32_t*>(pt), pw, nw, st);
+        };
+    });
+}
+
+// keep_lens, seq_lens, block_table, free_blocks, free_count, workspace
+SHIFTATTN_CALL(tables_truncate) {
+    Owned own;
+    return run(n, 6, [&] {
+        const at::Tensor &keep = tensor(a[0]), &lens = tensor(a[1]);
+        const at::Tensor &table = tensor(a[2]), &free = tensor(a[3]), &count = tensor(a[4]);
+        need(keep.scalar_type() == at::kInt && keep.sizes() == lens.sizes() && keep.is_contiguous(), "keep_lens: contiguous int32 [num_seqs]");
+        const shiftattn_tables t = tables_of(lens, table, free, count);
+        const at::Tensor* ws = workspace(a[5], a[1], own, [&] { return lib.tables_bytes(t.num_seqs); });
+        return [t, pk = ptr(keep), pw = ptr(ws), nw = bytes(ws), st = stream()] { return lib.tables_truncate(&t, static_cast<int32_t*>(pk), pw, nw, st); };
     });
 }
 
@@ -463,7 +540,7 @@ PyMethodDef methods[] = {SHIFTATTN_METHOD(bind), SHIFTATTN_METHOD(pack_seq2head)
                          SHIFTATTN_METHOD(decode), SHIFTATTN_METHOD(decode_static), SHIFTATTN_METHOD(mixed), SHIFTATTN_METHOD(kv_write),
                          SHIFTATTN_METHOD(qkv_proj_pack), SHIFTATTN_METHOD(unpack_o_proj), SHIFTATTN_METHOD(quantize_rows_fp8),
                          SHIFTATTN_METHOD(quantize_recv_fp8), SHIFTATTN_METHOD(qkv_proj_pack_fp8), SHIFTATTN_METHOD(unpack_o_proj_fp8),
-                         SHIFTATTN_METHOD(attn_desc),
+                         SHIFTATTN_METHOD(attn_desc), SHIFTATTN_METHOD(tables_append), SHIFTATTN_METHOD(tables_truncate),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
