@@ -19,6 +19,7 @@
  *   shiftattn_qkv_proj_pack[_fp8]   qkv = x * W_qkv^T written straight into the send buffers
  *   shiftattn_unpack_o_proj[_fp8]   embed = unpack(recv) * W_o^T read in place from the receive buffers
  *   shiftattn_quantize_rows_fp8 / shiftattn_quantize_recv_fp8   per-row FP8 quantisation for the above
+ *   shiftattn_..._int8              the same projections and quantisers over 8-bit integers
  *
  * In TP mode (the shift configuration, SP=1) a rank calls only kv_write/prefill/decode on the
  * fused rows its own QKV projection produced; in SP mode it packs, exchanges, attends,
@@ -230,6 +231,33 @@ int shiftattn_qkv_proj_pack_fp8_ws(const void *x_codes, const float *x_scales, c
 int shiftattn_unpack_o_proj_fp8_ws(const void *recv_codes, const float *a_scales, const void *w_codes,
                                    const float *w_scales, void *out, int32_t T, int32_t T_pad, int32_t d_model,
                                    const shiftattn_xchg *xc, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- The same projections with 8-bit integers -----------------------------------------------------------
+ * As the FP8 calls, with int8 codes in the place of FP8 ones: a scale for each token and for each output feature,
+ *   y[t][f] = x_scale[t] * w_scale[f] * sum_k x_code[t][k] * w_code[f][k],
+ * the sum exact in 32-bit integers (k below 131072, else EUNSUPPORTED), rounded to float32, scaled and rounded to bf16.  So results are
+ * the same bits with any workspace and without one.
+ * quantize_{rows,recv}_int8: a = the row's largest finite magnitude, scale = a / 127, code = the integer nearest to the exact product
+ *   x * (127 / a), ties to even, where both quotients are float32; a row whose a is below 2^-100 gets scale 1 and codes of 0.
+ *   Infinities become 127 or -127 (in such a row too), NaN 0.
+ * shiftattn_proj_workspace_bytes_int8: the size for int8 operands. */
+int shiftattn_quantize_rows_int8(const void *x, void *codes, float *scales, int32_t rows, int32_t cols,
+                                 void *stream);
+int shiftattn_quantize_recv_int8(const void *recv, void *codes, float *scales, int32_t T, int32_t T_pad,
+                                 const shiftattn_xchg *xc, void *stream);
+int shiftattn_qkv_proj_pack_int8(const void *x_codes, const float *x_scales, const void *w_codes,
+                                 const float *w_scales, void *send, int32_t T, int32_t T_pad, int32_t d_model,
+                                 const shiftattn_xchg *xc, void *stream);
+int shiftattn_unpack_o_proj_int8(const void *recv_codes, const float *a_scales, const void *w_codes,
+                                 const float *w_scales, void *out, int32_t T, int32_t T_pad, int32_t d_model,
+                                 const shiftattn_xchg *xc, void *stream);
+size_t shiftattn_proj_workspace_bytes_int8(int32_t rows, int32_t n_features, int32_t k);
+int shiftattn_qkv_proj_pack_int8_ws(const void *x_codes, const float *x_scales, const void *w_codes,
+                                    const float *w_scales, void *send, int32_t T, int32_t T_pad, int32_t d_model,
+                                    const shiftattn_xchg *xc, void *workspace, size_t workspace_bytes, void *stream);
+int shiftattn_unpack_o_proj_int8_ws(const void *recv_codes, const float *a_scales, const void *w_codes,
+                                    const float *w_scales, void *out, int32_t T, int32_t T_pad, int32_t d_model,
+                                    const shiftattn_xchg *xc, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- KV-cache append (Sec. 2.2: prefill initialises the cache, decoding appends to it) --------
  * k_new, v_new (device, in): [n_tokens][hkv_l][D] with row stride a->kv_stride.

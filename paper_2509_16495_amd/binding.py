@@ -102,6 +102,14 @@ def lib() -> ctypes.CDLL:
         L.shiftattn_quantize_recv_fp8.argtypes = [vp, vp, vp, i32, i32, xp, vp]
         L.shiftattn_qkv_proj_pack_fp8.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, xp, vp]
         L.shiftattn_unpack_o_proj_fp8.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, xp, vp]
+        L.shiftattn_proj_workspace_bytes_int8.argtypes = [i32, i32, i32]
+        L.shiftattn_proj_workspace_bytes_int8.restype = ctypes.c_size_t
+        L.shiftattn_qkv_proj_pack_int8_ws.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, xp, vp, ctypes.c_size_t, vp]
+        L.shiftattn_unpack_o_proj_int8_ws.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, xp, vp, ctypes.c_size_t, vp]
+        L.shiftattn_quantize_rows_int8.argtypes = [vp, vp, vp, i32, i32, vp]
+        L.shiftattn_quantize_recv_int8.argtypes = [vp, vp, vp, i32, i32, xp, vp]
+        L.shiftattn_qkv_proj_pack_int8.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, xp, vp]
+        L.shiftattn_unpack_o_proj_int8.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, xp, vp]
         L.shiftattn_kv_write.argtypes = [vp, vp, i64p, i32, vp, ap, vp]
         L.shiftattn_prefill.argtypes = [vp, vp, vp, i64p, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, sz, ap, vp]
         L.shiftattn_decode.argtypes = [vp, vp, vp, i64p, vp, vp, vp, i32, i32, vp, vp, sz, ap, vp]
@@ -313,6 +321,33 @@ def unpack_o_proj_fp8(recv_codes: torch.Tensor, a_scales: torch.Tensor, w_codes:
                       out: torch.Tensor, workspace: Optional[torch.Tensor] = None) -> None:
     """FP8 E4M3 codes recv [P, T_pad, hq_l, D] (one scale per token) and w [d_model, h D] (one per feature) -> out [T, d_model] bf16."""
     _check(_native().unpack_o_proj_fp8(recv_codes, a_scales, w_codes, w_scales, out, workspace))
+
+
+def proj_workspace_bytes_int8(rows: int, n_features: int, k: int) -> int:
+    """proj_workspace_bytes() of a product over int8 codes."""
+    return int(lib().shiftattn_proj_workspace_bytes_int8(rows, n_features, k))
+
+
+def quantize_rows_int8(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> None:
+    """x [rows, cols] bf16 -> codes [rows, cols] int8, scales [rows] float32 (largest finite magnitude / 127)."""
+    _check(_native().quantize_rows_int8(x, codes, scales))
+
+
+def quantize_recv_int8(recv: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> None:
+    """recv [P, T_pad, hq_l, D] bf16 -> codes of the same shape (int8), scales [T]: one scale per token over all buffers."""
+    _check(_native().quantize_recv_int8(recv, codes, scales))
+
+
+def qkv_proj_pack_int8(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
+                       send: torch.Tensor, P: int, h: int, h_kv: int, workspace: Optional[torch.Tensor] = None) -> None:
+    """int8 codes x [T, d_model] and w [(h + 2 h_kv) D, d_model] with a scale per token and per feature -> bf16 send buffers."""
+    _check(_native().qkv_proj_pack_int8(x_codes, x_scales, w_codes, w_scales, send, P, h, h_kv, workspace))
+
+
+def unpack_o_proj_int8(recv_codes: torch.Tensor, a_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor,
+                       out: torch.Tensor, workspace: Optional[torch.Tensor] = None) -> None:
+    """int8 codes recv [P, T_pad, hq_l, D] (one scale per token) and w [d_model, h D] (one per feature) -> out [T, d_model] bf16."""
+    _check(_native().unpack_o_proj_int8(recv_codes, a_scales, w_codes, w_scales, out, workspace))
 
 
 def attn_desc(q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Tensor, softmax_scale: float,

@@ -266,6 +266,99 @@ int option_prefill_pairing() { return g_options[SHIFTATTN_OPT_PREFILL_PAIRING].l
 int option_prefill_scaled_q() { return g_options[SHIFTATTN_OPT_PREFILL_SCALED_Q].load(std::memory_order_relaxed); }
 }  // namespace shiftattn
 
+// ---- quantisers and projections over 8-bit codes, FP8 E4M3 or int8 ------------------------------------------------------
+namespace {
+
+// sums of int8 products stay in 32 bits: 128 * 128 * k below 2^31
+int check_int8_k(bool int8, int k) {
+    return int8 && k >= 131072 ? fail(SHIFTATTN_EUNSUPPORTED, "k = %d: int8 products are summed in 32 bits, k must be below 131072", k) : 0;
+}
+
+int quantize_rows(bool int8, const void* x, void* codes, float* scales, int32_t rows, int32_t cols, void* stream) {
+    if (rows < 0 || cols < 1) return fail(SHIFTATTN_EINVAL, "rows = %d, cols = %d", rows, cols);
+    if (cols % 8) return fail(SHIFTATTN_EUNSUPPORTED, "cols = %d is not a multiple of 8", cols);
+    if (rows == 0) return SHIFTATTN_OK;
+    if (!x || !codes || !scales) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (!aligned16(x) || (reinterpret_cast<uintptr_t>(codes) & 7) || (reinterpret_cast<uintptr_t>(scales) & 3))
+        return fail(SHIFTATTN_EINVAL, "x must be 16-byte, codes 8-byte, scales 4-byte aligned");
+    hipError_t e = (int8 ? launch_quantize_rows_int8 : launch_quantize_rows_fp8)(x, codes, scales, rows, cols, cols, 0, cols, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "quantize_rows launch");
+}
+
+int quantize_recv(bool int8, const void* recv, void* codes, float* scales, int32_t T, int32_t T_pad,
+                                const shiftattn_xchg* xc, void* stream) {
+    XchgShape s;
+    if (int rc = check_xchg(xc, T, T_pad, false, &s)) return rc;
+    if (xc->dtype != SHIFTATTN_BF16) return fail(SHIFTATTN_EUNSUPPORTED, "the quantiser reads bf16 rows");
+    if (xc->head_dim % 8) return fail(SHIFTATTN_EUNSUPPORTED, "head_dim = %d is not a multiple of 8", xc->head_dim);
+    if (s.T == 0) return SHIFTATTN_OK;
+    if (!recv || !codes || !scales) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (!aligned16(recv) || (reinterpret_cast<uintptr_t>(codes) & 7) || (reinterpret_cast<uintptr_t>(scales) & 3))
+        return fail(SHIFTATTN_EINVAL, "recv must be 16-byte, codes 8-byte, scales 4-byte aligned");
+    const int seg = s.hq_l * xc->head_dim;
+    hipError_t e = (int8 ? launch_quantize_rows_int8 : launch_quantize_rows_fp8)(recv, codes, scales, s.T, s.P * seg, seg, static_cast<int64_t>(s.T_pad) * seg, seg,
+                                            static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "quantize_recv launch");
+}
+
+int qkv_proj_pack_codes(bool int8, const void* x_codes, const float* x_scales, const void* w_codes, const float* w_scales,
+                                   void* send, int32_t T, int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+    XchgShape s;
+    if (int rc = check_xchg(xc, T, T_pad, true, &s)) return rc;
+    if (d_model < 1) return fail(SHIFTATTN_EINVAL, "d_model = %d", d_model);
+    if (!qkv_proj_pack_supported(s, d_model, elem_size(xc->dtype)))
+        return fail(SHIFTATTN_EUNSUPPORTED, "projection into the send buffers is built for bf16 results, head_dim 128, d_model a "
+                                            "multiple of 64 and an even number of heads per row (got d_model = %d, %d heads)",
+                    d_model, s.h + 2 * s.h_kv);
+    if (int rc = check_int8_k(int8, d_model)) return rc;
+    if (s.T_pad == 0) return SHIFTATTN_OK;
+    if (!send || (s.T > 0 && (!x_codes || !w_codes || !x_scales || !w_scales))) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (!aligned16(x_codes) || !aligned16(w_codes) || !aligned16(send) || !aligned16(w_scales) || (reinterpret_cast<uintptr_t>(x_scales) & 3))
+        return fail(SHIFTATTN_EINVAL, "x_codes / w_codes / w_scales / send must be 16-byte aligned, x_scales 4-byte");
+    if (workspace_bytes > 0 && (!workspace || !aligned16(workspace)))
+        return fail(SHIFTATTN_EINVAL, "workspace is NULL or not 16-byte aligned");
+    if (int rc = ensure_device_ready()) return rc;
+    const int n_feat = (s.h + 2 * s.h_kv) * 128;
+    const int kg = s.T > 0 && !force_generic() ? proj_stream_ranges(s.T_pad, n_feat, d_model, true, workspace_bytes) : 0;
+    hipError_t e;
+    if (kg > 0)
+        e = launch_qkv_proj_stream(x_codes, w_codes, send, d_model, s, x_scales, w_scales, int8, kg, workspace, static_cast<hipStream_t>(stream));
+    else
+        e = launch_qkv_proj_pack(x_codes, w_codes, send, d_model, s, x_scales, w_scales, int8, force_generic() ? nullptr : workspace,
+                                 workspace_bytes, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "qkv_proj_pack launch");
+}
+
+int unpack_o_proj_codes(bool int8, const void* recv_codes, const float* a_scales, const void* w_codes, const float* w_scales,
+                                   void* out, int32_t T, int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+    XchgShape s;
+    if (int rc = check_xchg(xc, T, T_pad, false, &s)) return rc;
+    if (d_model < 1) return fail(SHIFTATTN_EINVAL, "d_model = %d", d_model);
+    if (!unpack_o_proj_supported(s, d_model, elem_size(xc->dtype)))
+        return fail(SHIFTATTN_EUNSUPPORTED, "projection out of the receive buffers is built for bf16 results, head_dim 128 and "
+                                            "d_model a multiple of 256 (got d_model = %d)", d_model);
+    if (int rc = check_int8_k(int8, s.h * 128)) return rc;
+    if (s.T == 0) return SHIFTATTN_OK;
+    if (!recv_codes || !a_scales || !w_codes || !w_scales || !out) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (!aligned16(recv_codes) || !aligned16(w_codes) || !aligned16(out) || !aligned16(w_scales) || (reinterpret_cast<uintptr_t>(a_scales) & 3))
+        return fail(SHIFTATTN_EINVAL, "recv_codes / w_codes / w_scales / out must be 16-byte aligned, a_scales 4-byte");
+    if (workspace_bytes > 0 && (!workspace || !aligned16(workspace)))
+        return fail(SHIFTATTN_EINVAL, "workspace is NULL or not 16-byte aligned");
+    if (int rc = ensure_device_ready()) return rc;
+    const int kg = force_generic() ? 0 : proj_stream_ranges(s.T, d_model, s.h * 128, true, workspace_bytes);
+    hipError_t e;
+    if (kg > 0)
+        e = launch_o_proj_stream(recv_codes, w_codes, out, d_model, s, a_scales, w_scales, int8, kg, workspace, static_cast<hipStream_t>(stream));
+    else
+        e = launch_unpack_o_proj(recv_codes, w_codes, out, d_model, s, a_scales, w_scales, int8, force_generic() ? nullptr : workspace,
+                                 workspace_bytes, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "unpack_o_proj launch");
+}
+
+}  // namespace
+
 // ---- the attention calls; scaled: the cache has a scale for each block, in kv_scales -----------------------------------
 namespace {
 
@@ -548,9 +641,9 @@ int shiftattn_qkv_proj_pack_ws(const void* x, const void* w_qkv, void* send, int
     const int kg = s.T > 0 && !force_generic() ? proj_stream_ranges(s.T_pad, n_feat, d_model, false, workspace_bytes) : 0;
     hipError_t e;
     if (kg > 0)
-        e = launch_qkv_proj_stream(x, w_qkv, send, d_model, s, nullptr, nullptr, kg, workspace, static_cast<hipStream_t>(stream));
+        e = launch_qkv_proj_stream(x, w_qkv, send, d_model, s, nullptr, nullptr, false, kg, workspace, static_cast<hipStream_t>(stream));
     else
-        e = launch_qkv_proj_pack(x, w_qkv, send, d_model, s, nullptr, nullptr, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+        e = launch_qkv_proj_pack(x, w_qkv, send, d_model, s, nullptr, nullptr, false, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "qkv_proj_pack launch");
 }
 
@@ -576,9 +669,9 @@ int shiftattn_unpack_o_proj_ws(const void* recv, const void* w_o, void* out, int
     const int kg = force_generic() ? 0 : proj_stream_ranges(s.T, d_model, s.h * 128, false, workspace_bytes);
     hipError_t e;
     if (kg > 0)
-        e = launch_o_proj_stream(recv, w_o, out, d_model, s, nullptr, nullptr, kg, workspace, static_cast<hipStream_t>(stream));
+        e = launch_o_proj_stream(recv, w_o, out, d_model, s, nullptr, nullptr, false, kg, workspace, static_cast<hipStream_t>(stream));
     else
-        e = launch_unpack_o_proj(recv, w_o, out, d_model, s, nullptr, nullptr, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+        e = launch_unpack_o_proj(recv, w_o, out, d_model, s, nullptr, nullptr, false, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "unpack_o_proj launch");
 }
 
@@ -612,89 +705,58 @@ int shiftattn_proj_plan(int32_t rows, int32_t n_features, int32_t k, int32_t fp8
 }
 
 int shiftattn_quantize_rows_fp8(const void* x, void* codes, float* scales, int32_t rows, int32_t cols, void* stream) {
-    if (rows < 0 || cols < 1) return fail(SHIFTATTN_EINVAL, "rows = %d, cols = %d", rows, cols);
-    if (cols % 8) return fail(SHIFTATTN_EUNSUPPORTED, "cols = %d is not a multiple of 8", cols);
-    if (rows == 0) return SHIFTATTN_OK;
-    if (!x || !codes || !scales) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
-    if (!aligned16(x) || (reinterpret_cast<uintptr_t>(codes) & 7) || (reinterpret_cast<uintptr_t>(scales) & 3))
-        return fail(SHIFTATTN_EINVAL, "x must be 16-byte, codes 8-byte, scales 4-byte aligned");
-    hipError_t e = launch_quantize_rows_fp8(x, codes, scales, rows, cols, cols, 0, cols, static_cast<hipStream_t>(stream));
-    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "quantize_rows_fp8 launch");
+    return quantize_rows(false, x, codes, scales, rows, cols, stream);
 }
 
-int shiftattn_quantize_recv_fp8(const void* recv, void* codes, float* scales, int32_t T, int32_t T_pad,
-                                const shiftattn_xchg* xc, void* stream) {
-    XchgShape s;
-    if (int rc = check_xchg(xc, T, T_pad, false, &s)) return rc;
-    if (xc->dtype != SHIFTATTN_BF16) return fail(SHIFTATTN_EUNSUPPORTED, "the quantiser reads bf16 rows");
-    if (xc->head_dim % 8) return fail(SHIFTATTN_EUNSUPPORTED, "head_dim = %d is not a multiple of 8", xc->head_dim);
-    if (s.T == 0) return SHIFTATTN_OK;
-    if (!recv || !codes || !scales) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
-    if (!aligned16(recv) || (reinterpret_cast<uintptr_t>(codes) & 7) || (reinterpret_cast<uintptr_t>(scales) & 3))
-        return fail(SHIFTATTN_EINVAL, "recv must be 16-byte, codes 8-byte, scales 4-byte aligned");
-    const int seg = s.hq_l * xc->head_dim;
-    hipError_t e = launch_quantize_rows_fp8(recv, codes, scales, s.T, s.P * seg, seg, static_cast<int64_t>(s.T_pad) * seg, seg,
-                                            static_cast<hipStream_t>(stream));
-    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "quantize_recv_fp8 launch");
+int shiftattn_quantize_recv_fp8(const void* recv, void* codes, float* scales, int32_t T, int32_t T_pad, const shiftattn_xchg* xc, void* stream) {
+    return quantize_recv(false, recv, codes, scales, T, T_pad, xc, stream);
 }
 
-int shiftattn_qkv_proj_pack_fp8_ws(const void* x_codes, const float* x_scales, const void* w_codes, const float* w_scales,
-                                   void* send, int32_t T, int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc,
-                                   void* workspace, size_t workspace_bytes, void* stream) {
-    XchgShape s;
-    if (int rc = check_xchg(xc, T, T_pad, true, &s)) return rc;
-    if (d_model < 1) return fail(SHIFTATTN_EINVAL, "d_model = %d", d_model);
-    if (!qkv_proj_pack_supported(s, d_model, elem_size(xc->dtype)))
-        return fail(SHIFTATTN_EUNSUPPORTED, "projection into the send buffers is built for bf16 results, head_dim 128, d_model a "
-                                            "multiple of 64 and an even number of heads per row (got d_model = %d, %d heads)",
-                    d_model, s.h + 2 * s.h_kv);
-    if (s.T_pad == 0) return SHIFTATTN_OK;
-    if (!send || (s.T > 0 && (!x_codes || !w_codes || !x_scales || !w_scales))) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
-    if (!aligned16(x_codes) || !aligned16(w_codes) || !aligned16(send) || !aligned16(w_scales) || (reinterpret_cast<uintptr_t>(x_scales) & 3))
-        return fail(SHIFTATTN_EINVAL, "x_codes / w_codes / w_scales / send must be 16-byte aligned, x_scales 4-byte");
-    if (workspace_bytes > 0 && (!workspace || !aligned16(workspace)))
-        return fail(SHIFTATTN_EINVAL, "workspace is NULL or not 16-byte aligned");
-    if (int rc = ensure_device_ready()) return rc;
-    const int n_feat = (s.h + 2 * s.h_kv) * 128;
-    const int kg = s.T > 0 && !force_generic() ? proj_stream_ranges(s.T_pad, n_feat, d_model, true, workspace_bytes) : 0;
-    hipError_t e;
-    if (kg > 0)
-        e = launch_qkv_proj_stream(x_codes, w_codes, send, d_model, s, x_scales, w_scales, kg, workspace, static_cast<hipStream_t>(stream));
-    else
-        e = launch_qkv_proj_pack(x_codes, w_codes, send, d_model, s, x_scales, w_scales, force_generic() ? nullptr : workspace,
-                                 workspace_bytes, static_cast<hipStream_t>(stream));
-    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "qkv_proj_pack_fp8 launch");
+int shiftattn_qkv_proj_pack_fp8_ws(const void* x_codes, const float* x_scales, const void* w_codes, const float* w_scales, void* send, int32_t T,
+                                   int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc, void* workspace, size_t workspace_bytes, void* stream) {
+    return qkv_proj_pack_codes(false, x_codes, x_scales, w_codes, w_scales, send, T, T_pad, d_model, xc, workspace, workspace_bytes, stream);
+}
+
+int shiftattn_unpack_o_proj_fp8_ws(const void* recv_codes, const float* a_scales, const void* w_codes, const float* w_scales, void* out, int32_t T,
+                                   int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc, void* workspace, size_t workspace_bytes, void* stream) {
+    return unpack_o_proj_codes(false, recv_codes, a_scales, w_codes, w_scales, out, T, T_pad, d_model, xc, workspace, workspace_bytes, stream);
+}
+
+int shiftattn_quantize_rows_int8(const void* x, void* codes, float* scales, int32_t rows, int32_t cols, void* stream) {
+    return quantize_rows(true, x, codes, scales, rows, cols, stream);
+}
+
+int shiftattn_quantize_recv_int8(const void* recv, void* codes, float* scales, int32_t T, int32_t T_pad, const shiftattn_xchg* xc, void* stream) {
+    return quantize_recv(true, recv, codes, scales, T, T_pad, xc, stream);
+}
+
+int shiftattn_qkv_proj_pack_int8_ws(const void* x_codes, const float* x_scales, const void* w_codes, const float* w_scales, void* send, int32_t T,
+                                   int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc, void* workspace, size_t workspace_bytes, void* stream) {
+    return qkv_proj_pack_codes(true, x_codes, x_scales, w_codes, w_scales, send, T, T_pad, d_model, xc, workspace, workspace_bytes, stream);
+}
+
+int shiftattn_unpack_o_proj_int8_ws(const void* recv_codes, const float* a_scales, const void* w_codes, const float* w_scales, void* out, int32_t T,
+                                   int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc, void* workspace, size_t workspace_bytes, void* stream) {
+    return unpack_o_proj_codes(true, recv_codes, a_scales, w_codes, w_scales, out, T, T_pad, d_model, xc, workspace, workspace_bytes, stream);
+}
+
+int shiftattn_qkv_proj_pack_int8(const void* x_codes, const float* x_scales, const void* w_codes, const float* w_scales, void* send, int32_t T,
+                                 int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc, void* stream) {
+    return shiftattn_qkv_proj_pack_int8_ws(x_codes, x_scales, w_codes, w_scales, send, T, T_pad, d_model, xc, nullptr, 0, stream);
+}
+
+int shiftattn_unpack_o_proj_int8(const void* recv_codes, const float* a_scales, const void* w_codes, const float* w_scales, void* out, int32_t T,
+                                 int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc, void* stream) {
+    return shiftattn_unpack_o_proj_int8_ws(recv_codes, a_scales, w_codes, w_scales, out, T, T_pad, d_model, xc, nullptr, 0, stream);
+}
+
+size_t shiftattn_proj_workspace_bytes_int8(int32_t rows, int32_t n_features, int32_t k) {
+    return shiftattn_proj_workspace_bytes_fp8(rows, n_features, k);   // as many bytes an element, the same plans
 }
 
 int shiftattn_qkv_proj_pack_fp8(const void* x_codes, const float* x_scales, const void* w_codes, const float* w_scales,
                                 void* send, int32_t T, int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc, void* stream) {
     return shiftattn_qkv_proj_pack_fp8_ws(x_codes, x_scales, w_codes, w_scales, send, T, T_pad, d_model, xc, nullptr, 0, stream);
-}
-
-int shiftattn_unpack_o_proj_fp8_ws(const void* recv_codes, const float* a_scales, const void* w_codes, const float* w_scales,
-                                   void* out, int32_t T, int32_t T_pad, int32_t d_model, const shiftattn_xchg* xc,
-                                   void* workspace, size_t workspace_bytes, void* stream) {
-    XchgShape s;
-    if (int rc = check_xchg(xc, T, T_pad, false, &s)) return rc;
-    if (d_model < 1) return fail(SHIFTATTN_EINVAL, "d_model = %d", d_model);
-    if (!unpack_o_proj_supported(s, d_model, elem_size(xc->dtype)))
-        return fail(SHIFTATTN_EUNSUPPORTED, "projection out of the receive buffers is built for bf16 results, head_dim 128 and "
-                                            "d_model a multiple of 256 (got d_model = %d)", d_model);
-    if (s.T == 0) return SHIFTATTN_OK;
-    if (!recv_codes || !a_scales || !w_codes || !w_scales || !out) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
-    if (!aligned16(recv_codes) || !aligned16(w_codes) || !aligned16(out) || !aligned16(w_scales) || (reinterpret_cast<uintptr_t>(a_scales) & 3))
-        return fail(SHIFTATTN_EINVAL, "recv_codes / w_codes / w_scales / out must be 16-byte aligned, a_scales 4-byte");
-    if (workspace_bytes > 0 && (!workspace || !aligned16(workspace)))
-        return fail(SHIFTATTN_EINVAL, "workspace is NULL or not 16-byte aligned");
-    if (int rc = ensure_device_ready()) return rc;
-    const int kg = force_generic() ? 0 : proj_stream_ranges(s.T, d_model, s.h * 128, true, workspace_bytes);
-    hipError_t e;
-    if (kg > 0)
-        e = launch_o_proj_stream(recv_codes, w_codes, out, d_model, s, a_scales, w_scales, kg, workspace, static_cast<hipStream_t>(stream));
-    else
-        e = launch_unpack_o_proj(recv_codes, w_codes, out, d_model, s, a_scales, w_scales, force_generic() ? nullptr : workspace,
-                                 workspace_bytes, static_cast<hipStream_t>(stream));
-    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "unpack_o_proj_fp8 launch");
 }
 
 int shiftattn_unpack_o_proj_fp8(const void* recv_codes, const float* a_scales, const void* w_codes, const float* w_scales,

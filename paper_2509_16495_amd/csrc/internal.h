@@ -206,14 +206,14 @@ int option_prefill_scaled_q();     // 1: the 256-column kernel's first attempt w
 // proj_gemm.hip : the projections in front of the first exchange and behind the second (bf16, head_dim 128)
 bool qkv_proj_pack_supported(const XchgShape& s, int d_model, int elem);
 bool unpack_o_proj_supported(const XchgShape& s, int d_model, int elem);
-// scales non-null: the operands are FP8 E4M3 codes with one scale per token row and one per output feature
+// scales non-null: the operands are FP8 E4M3 codes, or int8 ones (int8), with one scale per token row and one per output feature
 // (the result stays bf16); the XchgShape then describes the bf16 side (send buffers) or, for the receive buffers,
 // their head geometry
 hipError_t launch_qkv_proj_pack(const void* x, const void* w_qkv, void* send, int d_model, const XchgShape& s,
-                                const float* x_scales, const float* w_scales, void* workspace, size_t workspace_bytes,
+                                const float* x_scales, const float* w_scales, bool int8, void* workspace, size_t workspace_bytes,
                                 hipStream_t st);
 hipError_t launch_unpack_o_proj(const void* recv, const void* w_o, void* out, int d_model, const XchgShape& s,
-                                const float* a_scales, const float* w_scales, void* workspace, size_t workspace_bytes,
+                                const float* a_scales, const float* w_scales, bool int8, void* workspace, size_t workspace_bytes,
                                 hipStream_t st);
 // bytes of workspace that let the large-batch kernel split k over workgroups for its last (or only) round of tiles; 0: no split
 size_t proj_gemm_workspace(int M_out, int N, int K, bool fp8);
@@ -229,17 +229,21 @@ void proj_gemm_describe(int M_out, int N, int K, bool fp8, size_t workspace_byte
 // the workspace that the size query names (shiftattn_proj_workspace_bytes)
 size_t proj_workspace(int M_out, int N, int K, bool fp8);
 hipError_t launch_qkv_proj_stream(const void* x, const void* w_qkv, void* send, int d_model, const XchgShape& s,
-                                  const float* x_scales, const float* w_scales, int kg, void* workspace, hipStream_t st);
+                                  const float* x_scales, const float* w_scales, bool int8, int kg, void* workspace, hipStream_t st);
 hipError_t launch_o_proj_stream(const void* recv, const void* w_o, void* out, int d_model, const XchgShape& s,
-                                const float* a_scales, const float* w_scales, int kg, void* workspace, hipStream_t st);
+                                const float* a_scales, const float* w_scales, bool int8, int kg, void* workspace, hipStream_t st);
 // (row_base: the partial results start at this token row of the result; rows below it are not touched)
 hipError_t launch_proj_finish(const float* partial, int kg, int t_rows, void* c, int M, int M_out, int N, int mode,
-                              const XchgShape& s, const float* x_scales, const float* w_scales, hipStream_t st,
+                              const XchgShape& s, const float* x_scales, const float* w_scales, bool int8, hipStream_t st,
                               int row_base = 0);
 // layout_kernels.hip : rows of bf16 values -> FP8 E4M3 codes + one float32 scale per row (amax / 448).  Element k of
 // row t lies at (k / seg_len) * seg_stride + t * row_stride + k % seg_len, in `x` and in `codes` alike.
 hipError_t launch_quantize_rows_fp8(const void* x, void* codes, float* scales, int rows, int cols, int seg_len,
                                     int64_t seg_stride, int64_t row_stride, hipStream_t st);
+
+// the same with int8 codes: scale = amax / 127, code = nearest integer to x * (127 / amax)
+hipError_t launch_quantize_rows_int8(const void* x, void* codes, float* scales, int rows, int cols, int seg_len,
+                                     int64_t seg_stride, int64_t row_stride, hipStream_t st);
 
 // ceilings.hip : attainable-rate probes for benchmark reports
 hipError_t launch_mfma_ceiling(const void* operands, void* sink, int iters, int64_t* flops, hipStream_t st);

@@ -476,6 +476,107 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_fp8_kernel(const uint1
     });
 }
 
+// The same rows as int8 codes: a = largest finite |x| of the row, scale = a / 127, code = the integer nearest to the exact product
+// x * (127 / a), both quotients float32 (a below 2^-100: scale 1 and codes of 0); infinities saturate, NaN gives 0.  One fused multiply-add
+// rounds the exact product to an integer, by adding 1.5 * 2^23, whose last place is 1; the code is its low byte.
+template <int kPieces>
+__global__ __launch_bounds__(kThreads) void quantize_rows_int8_kernel(const uint16_t* __restrict__ x, uint8_t* __restrict__ codes,
+                                                                      float* __restrict__ scales, int cols, int seg_len,
+                                                                      int64_t seg_stride, int64_t row_stride) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    __shared__ uint32_t wave_max[kThreads / 64];
+    const int64_t row = blockIdx.x;
+    const int pieces = cols / 8;
+    auto offset = [&](int piece) -> size_t {
+        const int k = piece * 8, seg = k / seg_len;
+        return static_cast<size_t>(seg) * seg_stride + static_cast<size_t>(row) * row_stride + (k - seg * seg_len);
+    };
+    u16x2 top = {0, 0};
+    auto take_max = [&](u32x4 v) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[j] & 0x7FFF7FFFu));
+    };
+    u32x4 held[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int piece = threadIdx.x + i * kThreads;
+        held[i] = u32x4{0u, 0u, 0u, 0u};
+        if (piece < pieces) held[i] = *reinterpret_cast<const u32x4*>(x + offset(piece));
+    }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) take_max(held[i]);
+    if constexpr (kPieces == kQuantPieces)
+        for (int piece = threadIdx.x + kQuantPieces * kThreads; piece < pieces; piece += kThreads)
+            take_max(*reinterpret_cast<const u32x4*>(x + offset(piece)));
+    auto row_max = [&](uint32_t bits) -> uint32_t {
+#pragma unroll
+        for (int sh = 32; sh > 0; sh >>= 1) bits = max(bits, static_cast<uint32_t>(__shfl_xor(static_cast<int>(bits), sh)));
+        if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = bits;
+        __syncthreads();
+        return max(max(wave_max[0], wave_max[1]), max(wave_max[2], wave_max[3]));
+    };
+    uint32_t bits = row_max(max(top[0], top[1]));
+    const bool finite = bits < 0x7F80u;
+    if (!finite) {   // (uniform, rare) infinities or NaN: the largest of the others
+        uint32_t m = 0;
+        for (int piece = threadIdx.x; piece < pieces; piece += kThreads) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(x + offset(piece));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t b = (v[j >> 1] >> (16 * (j & 1))) & 0x7FFFu;
+                if (b < 0x7F80u) m = max(m, b);
+            }
+        }
+        __syncthreads();
+        bits = row_max(m);
+    }
+    const bool tiny = bits < ((127u - 100u) << 7);   // 2^-100
+    const float amax = __uint_as_float(bits << 16);
+    const float inv = tiny ? 1.f : 127.f / amax;
+    if (threadIdx.x == 0) scales[row] = tiny ? 1.f : amax / 127.f;
+    auto code = [&](float v) -> uint32_t {
+        if (!finite && !(fabsf(v) < INFINITY)) return v != v ? 0u : v > 0.f ? 127u : static_cast<uint32_t>(-127);   // (the first is uniform)
+        return __float_as_uint(fmaf(v, inv, 12582912.f));
+    };
+    auto encode = [&](u32x4 v) -> u32x2 {
+        u32x2 r;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t a = v[2 * h], b = v[2 * h + 1];
+            const uint32_t c0 = code(__uint_as_float(a << 16)), c1 = code(__uint_as_float(a & 0xFFFF0000u));
+            const uint32_t c2 = code(__uint_as_float(b << 16)), c3 = code(__uint_as_float(b & 0xFFFF0000u));
+            r[h] = __builtin_amdgcn_perm(c1, c0, 0x0C0C0400u) | __builtin_amdgcn_perm(c3, c2, 0x04000C0Cu);
+        }
+        return r;
+    };
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+        const int piece = threadIdx.x + i * kThreads;
+        if (piece < pieces) *reinterpret_cast<u32x2*>(codes + offset(piece)) = encode(held[i]);
+    }
+    if constexpr (kPieces == kQuantPieces)
+        for (int piece = threadIdx.x + kQuantPieces * kThreads; piece < pieces; piece += kThreads)
+            *reinterpret_cast<u32x2*>(codes + offset(piece)) = encode(*reinterpret_cast<const u32x4*>(x + offset(piece)));
+}
+
+hipError_t launch_quantize_rows_int8(const void* x, void* codes, float* scales, int rows, int cols, int seg_len,
+                                     int64_t seg_stride, int64_t row_stride, hipStream_t st) {
+    if (rows == 0) return hipSuccess;
+    auto run = [&](auto kernel) {
+        kernel<<<static_cast<unsigned>(rows), kThreads, 0, st>>>(static_cast<const uint16_t*>(x), static_cast<uint8_t*>(codes), scales,
+                                                                 cols, seg_len, seg_stride, row_stride);
+        return hipGetLastError();
+    };
+    switch ((cols / 8 + kThreads - 1) / kThreads) {
+        case 0: case 1: return run(quantize_rows_int8_kernel<1>);
+        case 2: return run(quantize_rows_int8_kernel<2>);
+        case 3: return run(quantize_rows_int8_kernel<3>);
+        case 4: return run(quantize_rows_int8_kernel<4>);
+        case 5: case 6: return run(quantize_rows_int8_kernel<6>);
+        default: return run(quantize_rows_int8_kernel<kQuantPieces>);
+    }
+}
+
 hipError_t launch_quantize_rows_fp8(const void* x, void* codes, float* scales, int rows, int cols, int seg_len,
                                     int64_t seg_stride, int64_t row_stride, hipStream_t st) {
     if (rows == 0) return hipSuccess;

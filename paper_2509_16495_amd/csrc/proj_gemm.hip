@@ -44,6 +44,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 256;                 // features (and for large batches token rows) per workgroup; N is a multiple of it
@@ -85,14 +86,19 @@ __device__ inline bf16x8 frag(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 __device__ inline __attribute__((always_inline)) void mfma_16x16x32(f32x4& d, u32x4 a, u32x4 b) {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(d) : "v"(a), "v"(b));
 }
+// int8: 16 x 16 x 64 in the same registers, clocks and lanes (a lane's 16 bytes are 16 elements of k); sums are 32-bit integers
+__device__ inline __attribute__((always_inline)) void mfma_16x16x64_i8(f32x4& d, u32x4 a, u32x4 b) {
+    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(d) : "v"(a), "v"(b));
+}
 __device__ inline __attribute__((always_inline)) void mfma_settle() { asm volatile("s_nop 7\n\ts_nop 7" ::: "memory"); }
 
 struct GemmParams {
     const unsigned char* __restrict__ w;   // [N][K], bf16 or FP8 E4M3 codes
     const unsigned char* __restrict__ x;   // token rows of the same type; see mode
     uint16_t* __restrict__ c;              // bf16
-    const float* __restrict__ xs;          // FP8: one scale per token row
-    const float* __restrict__ ws;          // FP8: one scale per output feature
+    const float* __restrict__ xs;          // FP8, int8: one scale per token row
+    const float* __restrict__ ws;          // FP8, int8: one scale per output feature
+    bool int8;
     int M, M_out, N, K;               // M token rows exist, rows M..M_out-1 of the result are written as zeros
     // mode 0 (qkv_proj_pack): x dense [M][K]; result columns scattered to send buffers (XchgShape below)
     // mode 1 (unpack_o_proj): x gathered from recv [P][T_pad][hq_l][128] (k = (p hq_l + j) 128 + e); result dense [M][N]
@@ -110,13 +116,16 @@ struct GemmParams {
 // accumulation); the result is multiplied by the token's and the feature's scale before it is rounded to bf16.
 // kSplit: the workgroup covers one of p.k_splits ranges of k and leaves fp32 sums in p.partial (for FP8 operands: before
 // the scales, which the finishing kernel applies).  One call is one output tile (and k range): work item `item` of the launch.
-template <bool kFp8, bool kSplit, int TN, int TM, int ST>
+// kInt8: both operands are int8 codes (two v_mfma_i32_16x16x64_i8 where bf16 has two v_mfma_f32_16x16x32_bf16: the same stages, slices and
+// slots over twice the k); sums are 32-bit integers, rounded to float32 once, in front of the scales.
+template <bool kFp8, bool kSplit, int TN, int TM, int ST, bool kInt8>
 __device__ __attribute__((always_inline)) void proj_gemm_tile(const GemmParams& p, const int item) {
     using S_ = TileShape<TN, TM, ST>;
     constexpr int kAT = S_::kAT, kBT = S_::kBT, kMfmas = S_::kMfmas, kReads = S_::kReads;
     constexpr int kLoadsN = S_::kLoadsN, kLoadsM = S_::kLoadsM, kLoads = S_::kLoads, kStage = S_::kStage, kStages = ST;
     constexpr int kTokenBytes = TN * kRowBytes;   // where a stage's token rows start
-    constexpr int kElem = kFp8 ? 1 : 2;          // bytes per operand element
+    constexpr bool kCodes = kFp8 || kInt8;       // 8-bit operands with scales
+    constexpr int kElem = kCodes ? 1 : 2;        // bytes per operand element
     constexpr int kBK = kRowBytes / kElem;       // k per stage
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     // (an opaque copy of the thread index per work item, and another one for the epilogue below: as invariants of the
@@ -142,11 +151,11 @@ __device__ __attribute__((always_inline)) void proj_gemm_tile(const GemmParams& 
         m_idx = group * p.group_rows + in_group - n_idx * rows;
     }
     const int n0 = n_idx * TN, m0 = p.m_base + m_idx * TM;
-    // this workgroup's k stages: [kt0, kt0 + k_steps) of all; with FP8 operands the very last stage may hold 64 k only
+    // this workgroup's k stages: [kt0, kt0 + k_steps) of all; with 8-bit operands the very last stage may hold 64 k only
     const int kt_all = (p.K + kBK - 1) / kBK;
     const int kt0 = kSplit ? static_cast<int>(static_cast<int64_t>(kt_all) * split / n_splits) : 0;
     const int k_steps = kSplit ? static_cast<int>(static_cast<int64_t>(kt_all) * (split + 1) / n_splits) - kt0 : kt_all;
-    const bool ragged = kFp8 && p.K % kBK != 0 && kt0 + k_steps == kt_all;
+    const bool ragged = kCodes && p.K % kBK != 0 && kt0 + k_steps == kt_all;
 
     // ---- direct-to-LDS loads: this wavefront fills a quarter of the rows of both operand tiles, eight rows of
     // 128 bytes (1 KiB, eight whole cache lines) per instruction; lane -> row 8 j + lane / 8, LDS piece position
@@ -318,7 +327,7 @@ __device__ __attribute__((always_inline)) void proj_gemm_tile(const GemmParams& 
         int st = 0;
         const int n_plain = k_steps - kStages - (ragged ? 1 : 0);
         for (; st < n_plain; ++st) stage.template operator()<1>(st);
-        if constexpr (kFp8) {
+        if constexpr (kCodes) {
             if (ragged && st + kStages < k_steps) {
                 stage.template operator()<2>(st);
                 ++st;
@@ -357,7 +366,8 @@ __device__ __attribute__((always_inline)) void proj_gemm_tile(const GemmParams& 
             [&]<int... I>(std::integer_sequence<int, I...>) {
                 (([&]() {
                      constexpr int i = I / kBT, j = I % kBT;
-                     mfma_16x16x32(acc[i][j], a[S][i], b[S][j]);
+                     if constexpr (kInt8) mfma_16x16x64_i8(acc[i][j], a[S][i], b[S][j]);
+                     else mfma_16x16x32(acc[i][j], a[S][i], b[S][j]);
                      // read r goes behind MFMA r * span / kReads, load l behind l * kMfmas / kLoads + kLoadSkew (M0) and the next
                      constexpr int kSpan = kDense ? 3 * kMfmas / 4 : kMfmas;
                      constexpr int r = (I * kReads + kSpan - 1) / kSpan;
@@ -387,6 +397,13 @@ __device__ __attribute__((always_inline)) void proj_gemm_tile(const GemmParams& 
             asm volatile("s_nop 4" ::: "memory");
             slice.template operator()<0, true, 0>(lds + rd_off, 1);
             meet.template operator()<kLoadMode>(st);
+            if constexpr (kInt8 && kLoadMode == 0) {
+                if (ragged && st == k_steps - 1) {   // a half-filled last stage: its second slice repeats the first one (see the loads)
+#pragma unroll
+                    for (int j = 0; j < kBT; ++j) b[1][j] = u32x4{0u, 0u, 0u, 0u};
+                    asm volatile("s_nop 4" ::: "memory");
+                }
+            }
             // (behind the last stage: stale data, not used)
             slice.template operator()<1, false, kLoadMode>(lds + rd_next, 0);
             next_buffer();
@@ -493,7 +510,10 @@ __device__ __attribute__((always_inline)) void proj_gemm_tile(const GemmParams& 
     constexpr int kQuads = kAT;
     const int tok_lane = lane_e & 15;
     auto quad_feature = [&](int q) { return 16 * q + 4 * (lane_e >> 4); };
-    auto quad_value = [&](int q, int t, int e) -> float { return acc[q][t][e]; };
+    auto quad_value = [&](int q, int t, int e) -> float {
+        if constexpr (kInt8) return static_cast<float>(__float_as_int(acc[q][t][e]));
+        else return acc[q][t][e];
+    };
     const int f_wave = n0 + wn * S_::kWaveN;     // first feature of this wavefront; its features lie in one head
     // The bf16 result goes through LDS (the stage buffers are free by now): a wavefront lays its 128 tokens x 128
     // features down as rows of 256 bytes (pitch 272: the 8-byte writes of 16 token rows then spread over all banks),
@@ -508,17 +528,17 @@ __device__ __attribute__((always_inline)) void proj_gemm_tile(const GemmParams& 
             const int tok = t * kTokStep + tok_lane;
             const int m = m0 + wm * S_::kWaveM + tok;
             float row_scale = 1.f;
-            if constexpr (kFp8) row_scale = m < p.M ? p.xs[m] : 0.f;
+            if constexpr (kCodes) row_scale = m < p.M ? p.xs[m] : 0.f;
 #pragma unroll
             for (int q = 0; q < kQuads; ++q) {
                 const int f = quad_feature(q);
                 f32x4 col_scale = {1.f, 1.f, 1.f, 1.f};
-                if constexpr (kFp8) col_scale = *reinterpret_cast<const f32x4*>(p.ws + f_wave + f);
+                if constexpr (kCodes) col_scale = *reinterpret_cast<const f32x4*>(p.ws + f_wave + f);
                 bf16x4 v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float y = m < p.M ? quad_value(q, t, e) : 0.f;   // rows M .. M_out - 1 of the result are zeros
-                    if constexpr (kFp8) y = y * row_scale * col_scale[e];
+                    if constexpr (kCodes) y = y * row_scale * col_scale[e];
                     v[e] = static_cast<__bf16>(y);
                 }
                 *reinterpret_cast<u32x2*>(stg + tok * S_::kStagingPitch + f * 2) = __builtin_bit_cast(u32x2, v);
@@ -546,7 +566,7 @@ __device__ __attribute__((always_inline)) void proj_gemm_tile(const GemmParams& 
 #pragma unroll
             for (int q = 0; q < kQuads; ++q)
                 *reinterpret_cast<f32x4*>(row + quad_feature(q)) =
-                    f32x4{quad_value(q, t, 0), quad_value(q, t, 1), quad_value(q, t, 2), quad_value(q, t, 3)};
+                    f32x4{acc[q][t][0], acc[q][t][1], acc[q][t][2], acc[q][t][3]};
         }
         return;
     }
@@ -582,13 +602,13 @@ __device__ __attribute__((always_inline)) void proj_gemm_tile(const GemmParams& 
 // The grid is persistent: as many workgroups as the chip holds walk the launch's work items (output tile, k range) in
 // rounds, so a compute unit goes from one tile to the next without waiting to be scheduled (ten rounds of tiles at the
 // 70B shape).  Workgroup b runs on XCD b % 8, see item_order() for which item of a round it takes.
-template <bool kFp8, bool kSplit, int TN, int TM, int ST>
+template <bool kFp8, bool kSplit, int TN, int TM, int ST, bool kInt8 = false>
 __global__ __launch_bounds__(kGemmThreads, (TileShape<TN, TM, ST>::kPerCu)) void proj_gemm_kernel(GemmParams p) {
     const int xcd = blockIdx.x % 8, in_xcd = blockIdx.x / 8;
     for (int base = 0; base + static_cast<int>(blockIdx.x) < p.items; base += gridDim.x) {
         const int count = min(static_cast<int>(gridDim.x), p.items - base);   // items of this round
         const int item = !kSplit && p.group_rows == 0 ? static_cast<int>(blockIdx.x) : xcd * (count / 8) + min(xcd, count % 8) + in_xcd;
-        proj_gemm_tile<kFp8, kSplit, TN, TM, ST>(p, base + item);
+        proj_gemm_tile<kFp8, kSplit, TN, TM, ST, kInt8>(p, base + item);
         // the next item's loads go where other wavefronts may still be reading their staged result rows
         __builtin_amdgcn_s_waitcnt(wait_imm(kNoVm, 0));
         asm volatile("s_barrier" ::: "memory");
@@ -610,7 +630,7 @@ inline int item_order(int n_tiles, int m_tiles, int k_splits, int most) {
     return (m_tiles + groups - 1) / groups;
 }
 
-template <bool kFp8, int TN, int TM, int ST>
+template <bool kFp8, int TN, int TM, int ST, bool kInt8>
 hipError_t launch(const GemmParams& p, hipStream_t st) {
     using S = TileShape<TN, TM, ST>;
     const int64_t items = static_cast<int64_t>(p.N / TN) * p.m_tiles * p.k_splits;
@@ -625,8 +645,8 @@ hipError_t launch(const GemmParams& p, hipStream_t st) {
     if (e != hipSuccess) return e;
     const int slots = cus * S::kPerCu;
     const unsigned grid = static_cast<unsigned>(items < slots ? items : slots);
-    if (p.k_splits > 1) proj_gemm_kernel<kFp8, true, TN, TM, ST><<<grid, kGemmThreads, S::kLds, st>>>(q);
-    else proj_gemm_kernel<kFp8, false, TN, TM, ST><<<grid, kGemmThreads, S::kLds, st>>>(q);
+    if (p.k_splits > 1) proj_gemm_kernel<kFp8, true, TN, TM, ST, kInt8><<<grid, kGemmThreads, S::kLds, st>>>(q);
+    else proj_gemm_kernel<kFp8, false, TN, TM, ST, kInt8><<<grid, kGemmThreads, S::kLds, st>>>(q);
     return hipGetLastError();
 }
 
@@ -701,21 +721,24 @@ GemmPlan plan_gemm(int M_out, int N, int K, bool fp8, size_t workspace_bytes) {
     return best;
 }
 
-template <bool kFp8>
-hipError_t launch_kind(TileKind kind, const GemmParams& p, hipStream_t st) {
+template <bool kFp8, bool kInt8>
+hipError_t launch_tile(TileKind kind, const GemmParams& p, hipStream_t st) {
     switch (kind) {
-        case kTile256x256: return launch<kFp8, 256, 256, 2>(p, st);
-        case kTile256x128: return launch<kFp8, 256, 128, 3>(p, st);
-        default: return launch<kFp8, 128, 128, 4>(p, st);
+        case kTile256x256: return launch<kFp8, 256, 256, 2, kInt8>(p, st);
+        case kTile256x128: return launch<kFp8, 256, 128, 3, kInt8>(p, st);
+        default: return launch<kFp8, 128, 128, 4, kInt8>(p, st);
     }
 }
+hipError_t launch_kind(TileKind kind, const GemmParams& p, hipStream_t st) {
+    return p.int8 ? launch_tile<false, true>(kind, p, st) : p.xs ? launch_tile<true, false>(kind, p, st) : launch_tile<false, false>(kind, p, st);
+}
 
-template <bool kFp8, int TN, int TM, int ST>
+template <bool kFp8, int TN, int TM, int ST, bool kInt8 = false>
 hipError_t init_tile() {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&proj_gemm_kernel<kFp8, false, TN, TM, ST>),
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&proj_gemm_kernel<kFp8, false, TN, TM, ST, kInt8>),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, TileShape<TN, TM, ST>::kLds);
     if (e != hipSuccess) return e;
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&proj_gemm_kernel<kFp8, true, TN, TM, ST>),
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&proj_gemm_kernel<kFp8, true, TN, TM, ST, kInt8>),
                                hipFuncAttributeMaxDynamicSharedMemorySize, TileShape<TN, TM, ST>::kLds);
 }
 
@@ -724,8 +747,9 @@ hipError_t init_tile() {
 // bf16, head_dim 128; the feature dimension of either product must be a multiple of the 256-wide tile
 template <int TN, int TM, int ST>
 hipError_t init_shape() {
-    const hipError_t e = init_tile<false, TN, TM, ST>();
-    return e == hipSuccess ? init_tile<true, TN, TM, ST>() : e;
+    hipError_t e = init_tile<false, TN, TM, ST>();
+    if (e == hipSuccess) e = init_tile<true, TN, TM, ST>();
+    return e == hipSuccess ? init_tile<false, TN, TM, ST, true>() : e;
 }
 
 hipError_t proj_gemm_init() {
@@ -782,30 +806,31 @@ double proj_gemm_us(int M_out, int N, int K, bool fp8, size_t workspace_bytes) {
 
 // runs the product in the best way for which the workspace has room
 static hipError_t run_gemm(GemmParams& p, void* workspace, size_t workspace_bytes, hipStream_t st) {
-    const bool fp8 = p.xs != nullptr;
+    const bool fp8 = p.xs != nullptr;   // (or int8: as many bytes, the same matrix rate)
     const GemmPlan pl = plan_gemm(p.M_out, p.N, p.K, fp8, workspace ? workspace_bytes : 0);
     p.partial = nullptr;
     p.k_splits = 1;
     if (pl.lead_tiles > 0) {
         p.m_base = 0;
         p.m_tiles = pl.lead_tiles;
-        const hipError_t e = fp8 ? launch_kind<true>(pl.lead, p, st) : launch_kind<false>(pl.lead, p, st);
+        const hipError_t e = launch_kind(pl.lead, p, st);
         if (e != hipSuccess) return e;
     }
     p.m_base = pl.lead_tiles * kTileTokens[pl.lead];
     p.m_tiles = (p.M_out - p.m_base + kTileTokens[pl.tail] - 1) / kTileTokens[pl.tail];
     p.k_splits = pl.splits;
     if (pl.splits > 1) p.partial = static_cast<float*>(workspace);
-    const hipError_t e = fp8 ? launch_kind<true>(pl.tail, p, st) : launch_kind<false>(pl.tail, p, st);
+    const hipError_t e = launch_kind(pl.tail, p, st);
     if (e != hipSuccess || pl.splits == 1) return e;
-    return launch_proj_finish(p.partial, p.k_splits, p.M_out - p.m_base, p.c, p.M, p.M_out, p.N, p.mode, p.s, p.xs, p.ws, st,
+    return launch_proj_finish(p.partial, p.k_splits, p.M_out - p.m_base, p.c, p.M, p.M_out, p.N, p.mode, p.s, p.xs, p.ws, p.int8, st,
                               p.m_base);
 }
 
 hipError_t launch_qkv_proj_pack(const void* x, const void* w_qkv, void* send, int d_model, const XchgShape& s,
-                                const float* x_scales, const float* w_scales, void* workspace, size_t workspace_bytes,
+                                const float* x_scales, const float* w_scales, bool int8, void* workspace, size_t workspace_bytes,
                                 hipStream_t st) {
     GemmParams p;
+    p.int8 = int8;
     p.w = static_cast<const unsigned char*>(w_qkv);
     p.x = static_cast<const unsigned char*>(x);
     p.c = static_cast<uint16_t*>(send);
@@ -822,9 +847,10 @@ hipError_t launch_qkv_proj_pack(const void* x, const void* w_qkv, void* send, in
 }
 
 hipError_t launch_unpack_o_proj(const void* recv, const void* w_o, void* out, int d_model, const XchgShape& s,
-                                const float* a_scales, const float* w_scales, void* workspace, size_t workspace_bytes,
+                                const float* a_scales, const float* w_scales, bool int8, void* workspace, size_t workspace_bytes,
                                 hipStream_t st) {
     GemmParams p;
+    p.int8 = int8;
     p.w = static_cast<const unsigned char*>(w_o);
     p.x = static_cast<const unsigned char*>(recv);
     p.c = static_cast<uint16_t*>(out);

@@ -45,6 +45,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSWaves = 8;                         // wavefronts that the size query counts with
@@ -60,8 +61,9 @@ struct StreamParams {
     const unsigned char* __restrict__ x;   // token rows, see mode
     uint16_t* __restrict__ c;              // bf16 result
     float* __restrict__ partial;           // kg > 1: [kg][rows][N] fp32
-    const float* __restrict__ xs;          // FP8 products: one scale per token row ...
+    const float* __restrict__ xs;          // products of 8-bit codes: one scale per token row ...
     const float* __restrict__ ws;          // ... and one per output feature (nullptr: none)
+    bool int8;                             // the codes are int8: sums are 32-bit integers (in `partial` too)
     int M, M_out, N, K;                    // M token rows exist, rows M .. M_out - 1 of the result are zeros
     int mode;                              // 0: x dense [M][K], result into the send buffers; 1: x gathered from the
                                            // receive buffers (k = (p hq_l + j) 128 + e), result dense [M][N]
@@ -103,6 +105,15 @@ __device__ inline void store4(const StreamParams& p, int t, int f, u32x2 v) {
     }
 }
 
+// sums of int8 products, kept in float registers as the bits of integers: their sum, and their value
+__device__ inline f32x4 add_int(f32x4 a, f32x4 b) {
+    return __builtin_bit_cast(f32x4, __builtin_bit_cast(i32x4, a) + __builtin_bit_cast(i32x4, b));
+}
+__device__ inline f32x4 from_int(f32x4 v) {
+    const i32x4 i = __builtin_bit_cast(i32x4, v);
+    return f32x4{static_cast<float>(i[0]), static_cast<float>(i[1]), static_cast<float>(i[2]), static_cast<float>(i[3])};
+}
+
 __device__ inline u32x2 round4(f32x4 v) {
     bf16x4 r;
 #pragma unroll
@@ -117,10 +128,12 @@ constexpr int stream_waves() { return UX + UW <= 10 ? 8 : 4; }
 template <int UX, int UW>
 constexpr int stream_steps() { return 160 / stream_waves<UX, UW>() / (UX + UW); }
 
-// UX: pieces of eight token rows, UW: pieces of eight weight rows per step; kFp8: both operands are FP8 E4M3 codes
-template <int UX, int UW, bool kFp8>
+// UX: pieces of eight token rows, UW: pieces of eight weight rows per step; kFp8: both operands are FP8 E4M3 codes; kInt8: int8 codes, two
+// v_mfma_i32_16x16x64_i8 per step and pair of tiles (a lane's 16 bytes of k are those of the bf16 form).  Integer sums are exact, so
+// the result does not depend on how k is split; they are rounded to float32 once, in front of the scales.
+template <int UX, int UW, bool kFp8, bool kInt8 = false>
 __global__ __launch_bounds__((64 * stream_waves<UX, UW>())) void proj_stream_kernel(StreamParams p) {
-    constexpr int kElem = kFp8 ? 1 : 2;
+    constexpr int kElem = kFp8 || kInt8 ? 1 : 2;
     constexpr int kStepK = kStepRowBytes / kElem;
     constexpr int kWaves = stream_waves<UX, UW>(), kUnits = UX + UW, kRing = stream_steps<UX, UW>(), kSlot = kUnits * 1024;
     constexpr int TB = (UX + 1) / 2, TW = (UW + 1) / 2;
@@ -249,6 +262,15 @@ __global__ __launch_bounds__((64 * stream_waves<UX, UW>())) void proj_stream_ker
 #pragma unroll
                 for (int tb = 0; tb < TB; ++tb)
                     acc[tw][tb] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(both(a[tw]), both(b[tb]), acc[tw][tb], 0, 0, 0, 127, 0, 127);
+        } else if constexpr (kInt8) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int tw = 0; tw < TW; ++tw)
+#pragma unroll
+                    for (int tb = 0; tb < TB; ++tb)
+                        acc[tw][tb] = __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                            __builtin_bit_cast(i32x4, a[tw][kb]), __builtin_bit_cast(i32x4, b[tb][kb]), __builtin_bit_cast(i32x4, acc[tw][tb]), 0, 0, 0));
         } else {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
@@ -274,14 +296,19 @@ __global__ __launch_bounds__((64 * stream_waves<UX, UW>())) void proj_stream_ker
 #pragma unroll
         for (int w2 = 1; w2 < kWaves; ++w2) {
             const f32x4 v = reinterpret_cast<const f32x4*>(lds + w2 * (kRing * kSlot))[i];
+            if constexpr (kInt8) {
+                sum = add_int(sum, v);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += v[e];
+                for (int e = 0; e < 4; ++e) sum[e] += v[e];
+            }
         }
         if (p.kg > 1) {   // rows past the last token are not read
             if (t < p.M) *reinterpret_cast<f32x4*>(p.partial + (static_cast<size_t>(kr) * p.M_out + t) * p.N + f) = sum;
             continue;
         }
-        if constexpr (kFp8) {
+        if constexpr (kInt8) sum = from_int(sum);
+        if constexpr (kFp8 || kInt8) {
             if (t < p.M) {
                 const float row_scale = p.xs[t];
                 const f32x4 col_scale = *reinterpret_cast<const f32x4*>(p.ws + f);
@@ -329,7 +356,8 @@ hipError_t launch_stream(const StreamParams& p, hipStream_t st) {
     const unsigned grid = (p.N + p.rows_per_block - 1) / p.rows_per_block * p.kg;
 #define SHIFTATTN_STREAM_LAUNCH(ux_, uw_)                                                                   \
     if (ux == ux_ && uw == uw_) {                                                                         \
-        if (p.xs) proj_stream_kernel<ux_, uw_, true><<<grid, 64 * stream_waves<ux_, uw_>(), stream_lds<ux_, uw_>(), st>>>(p);     \
+        if (p.int8) proj_stream_kernel<ux_, uw_, false, true><<<grid, 64 * stream_waves<ux_, uw_>(), stream_lds<ux_, uw_>(), st>>>(p); \
+        else if (p.xs) proj_stream_kernel<ux_, uw_, true><<<grid, 64 * stream_waves<ux_, uw_>(), stream_lds<ux_, uw_>(), st>>>(p);     \
         else proj_stream_kernel<ux_, uw_, false><<<grid, 64 * stream_waves<ux_, uw_>(), stream_lds<ux_, uw_>(), st>>>(p);         \
         return hipGetLastError();                                                                         \
     }
@@ -361,12 +389,17 @@ __global__ __launch_bounds__(256) void proj_stream_finish_kernel(StreamParams p,
 #pragma unroll
             for (int x = 0; x < kFinishAhead; ++x) {
                 if (c + x < p.kg) {
+                    if (p.int8) {   // uniform
+                        sum = add_int(sum, v[x]);
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[e] += v[x][e];
+                        for (int e = 0; e < 4; ++e) sum[e] += v[x][e];
+                    }
                 }
             }
         }
-        if (p.xs) {   // the scales of FP8 operands, applied as the unsplit kernel applies them
+        if (p.int8) sum = from_int(sum);
+        if (p.xs) {   // the scales of 8-bit operands, applied as the unsplit kernel applies them
             const float row_scale = p.xs[t];
             const f32x4 col_scale = *reinterpret_cast<const f32x4*>(p.ws + f);
 #pragma unroll
@@ -380,8 +413,9 @@ __global__ __launch_bounds__(256) void proj_stream_finish_kernel(StreamParams p,
 
 // result = sum over kg partial results [kg][t_rows][N] (fp32) in group order, rounded once, stored with the layout of `mode`
 hipError_t launch_proj_finish(const float* partial, int kg, int t_rows, void* c, int M, int M_out, int N, int mode,
-                              const XchgShape& s, const float* x_scales, const float* w_scales, hipStream_t st, int row_base) {
+                              const XchgShape& s, const float* x_scales, const float* w_scales, bool int8, hipStream_t st, int row_base) {
     StreamParams p = {};
+    p.int8 = int8;
     p.xs = x_scales;
     p.ws = w_scales;
     p.partial = const_cast<float*>(partial);
@@ -404,6 +438,8 @@ hipError_t proj_stream_init() {
     if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&proj_stream_kernel<ux_, uw_, false>),  \
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, stream_lds<ux_, uw_>());  \
     if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&proj_stream_kernel<ux_, uw_, true>),   \
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, stream_lds<ux_, uw_>());  \
+    if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&proj_stream_kernel<ux_, uw_, false, true>), \
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, stream_lds<ux_, uw_>());
     SHIFTATTN_STREAM_SHAPES(SHIFTATTN_STREAM_INIT)
 #undef SHIFTATTN_STREAM_INIT
@@ -515,13 +551,14 @@ static hipError_t run_stream(StreamParams& p, int kg, void* workspace, hipStream
     p.rows_per_block = stream_rows(p.N, kg);
     const hipError_t e = launch_stream(p, st);
     if (e != hipSuccess || kg == 1) return e;
-    return launch_proj_finish(p.partial, kg, p.M_out, p.c, p.M, p.M_out, p.N, p.mode, p.s, p.xs, p.ws, st, 0);
+    return launch_proj_finish(p.partial, kg, p.M_out, p.c, p.M, p.M_out, p.N, p.mode, p.s, p.xs, p.ws, p.int8, st, 0);
 }
 
-// kg: k ranges, see proj_stream_ranges(); x_scales / w_scales: nullptr for bf16 operands, the row scales of FP8 E4M3 codes otherwise
+// kg: k ranges, see proj_stream_ranges(); x_scales / w_scales: nullptr for bf16 operands, the row scales of FP8 E4M3 or int8 codes otherwise
 hipError_t launch_qkv_proj_stream(const void* x, const void* w_qkv, void* send, int d_model, const XchgShape& s,
-                                  const float* x_scales, const float* w_scales, int kg, void* workspace, hipStream_t st) {
+                                  const float* x_scales, const float* w_scales, bool int8, int kg, void* workspace, hipStream_t st) {
     StreamParams p = {};
+    p.int8 = int8;
     p.w = static_cast<const unsigned char*>(w_qkv);
     p.x = static_cast<const unsigned char*>(x);
     p.c = static_cast<uint16_t*>(send);
@@ -537,8 +574,9 @@ hipError_t launch_qkv_proj_stream(const void* x, const void* w_qkv, void* send, 
 }
 
 hipError_t launch_o_proj_stream(const void* recv, const void* w_o, void* out, int d_model, const XchgShape& s,
-                                const float* a_scales, const float* w_scales, int kg, void* workspace, hipStream_t st) {
+                                const float* a_scales, const float* w_scales, bool int8, int kg, void* workspace, hipStream_t st) {
     StreamParams p = {};
+    p.int8 = int8;
     p.w = static_cast<const unsigned char*>(w_o);
     p.x = static_cast<const unsigned char*>(recv);
     p.c = static_cast<uint16_t*>(out);

@@ -23,7 +23,8 @@ namespace {
     F(quantize_rows, quantize_rows_fp8) F(quantize_recv, quantize_recv_fp8)                                                 \
     F(prefill_scaled, prefill_scaled) F(decode_scaled, decode_scaled) F(mixed_scaled, mixed_scaled)                         \
     F(kv_write_scaled, kv_write_scaled) F(tables_append, tables_append) F(tables_truncate, tables_truncate)                 \
-    F(tables_bytes, tables_workspace_bytes)                                                                                 \
+    F(qkv_int8, qkv_proj_pack_int8_ws) F(o_proj_int8, unpack_o_proj_int8_ws) F(quantize_rows_int8, quantize_rows_int8)       \
+    F(quantize_recv_int8, quantize_recv_int8) F(tables_bytes, tables_workspace_bytes)                                                                                 \
     F(prefill_bytes, prefill_workspace_bytes) F(decode_bytes, decode_workspace_bytes) F(mixed_bytes, mixed_workspace_bytes)
 struct Library {
 #define SHIFTATTN_POINTER(member, name) decltype(&shiftattn_##name) member;
@@ -461,36 +462,43 @@ SHIFTATTN_CALL(unpack_o_proj) {
 }
 
 // x, codes, scales
-SHIFTATTN_CALL(quantize_rows_fp8) {
+PyObject* quantize_rows_call(PyObject* const* a, Py_ssize_t n, bool int8) {
+    const at::ScalarType kCode = int8 ? at::kChar : at::kByte;
     return run(n, 3, [&] {
         const at::Tensor &x = tensor(a[0]), &codes = tensor(a[1]), &scales = tensor(a[2]);
         dims(x, 2, "x");
-        need(x.scalar_type() == at::kBFloat16 && codes.scalar_type() == at::kByte && scales.scalar_type() == at::kFloat, "x bfloat16, codes uint8, scales float32");
+        need(x.scalar_type() == at::kBFloat16 && codes.scalar_type() == kCode && scales.scalar_type() == at::kFloat, "x bfloat16, codes uint8 (FP8) or int8, scales float32");
         need(codes.sizes() == x.sizes() && scales.dim() == 1 && scales.size(0) == x.size(0) && x.is_contiguous() && codes.is_contiguous() && scales.is_contiguous(),
              "codes: shape of x, scales: [rows], contiguous");
-        return [px = ptr(x), pc = ptr(codes), ps = ptr(scales), rows = cut(x.size(0)), cols = cut(x.size(1)), st = stream()] {
-            return lib.quantize_rows(px, pc, static_cast<float*>(ps), rows, cols, st);
+        return [px = ptr(x), pc = ptr(codes), ps = ptr(scales), rows = cut(x.size(0)), cols = cut(x.size(1)), st = stream(), int8] {
+            return (int8 ? lib.quantize_rows_int8 : lib.quantize_rows)(px, pc, static_cast<float*>(ps), rows, cols, st);
         };
     });
 }
+SHIFTATTN_CALL(quantize_rows_fp8) { return quantize_rows_call(a, n, false); }
+SHIFTATTN_CALL(quantize_rows_int8) { return quantize_rows_call(a, n, true); }
 
 // recv, codes, scales
-SHIFTATTN_CALL(quantize_recv_fp8) {
+PyObject* quantize_recv_call(PyObject* const* a, Py_ssize_t n, bool int8) {
+    const at::ScalarType kCode = int8 ? at::kChar : at::kByte;
     return run(n, 3, [&] {
         const at::Tensor &recv = tensor(a[0]), &codes = tensor(a[1]), &scales = tensor(a[2]);
         dims(recv, 4, "recv");
-        need(recv.scalar_type() == at::kBFloat16 && codes.scalar_type() == at::kByte && scales.scalar_type() == at::kFloat && codes.sizes() == recv.sizes(),
-             "recv bfloat16, codes uint8 of its shape, scales float32");
+        need(recv.scalar_type() == at::kBFloat16 && codes.scalar_type() == kCode && scales.scalar_type() == at::kFloat && codes.sizes() == recv.sizes(),
+             "recv bfloat16, codes uint8 (FP8) or int8 of its shape, scales float32");
         need(recv.is_contiguous() && codes.is_contiguous() && scales.is_contiguous(), "recv, codes, scales: contiguous");
         return [x = exchange(recv.size(0), recv.size(0) * recv.size(2), 0, recv.size(3), SHIFTATTN_BF16), pr = ptr(recv), pc = ptr(codes), ps = ptr(scales),
-                T = cut(scales.size(0)), T_pad = cut(recv.size(1)), st = stream()] {
-            return lib.quantize_recv(pr, pc, static_cast<float*>(ps), T, T_pad, &x, st);
+                T = cut(scales.size(0)), T_pad = cut(recv.size(1)), st = stream(), int8] {
+            return (int8 ? lib.quantize_recv_int8 : lib.quantize_recv)(pr, pc, static_cast<float*>(ps), T, T_pad, &x, st);
         };
     });
 }
+SHIFTATTN_CALL(quantize_recv_fp8) { return quantize_recv_call(a, n, false); }
+SHIFTATTN_CALL(quantize_recv_int8) { return quantize_recv_call(a, n, true); }
 
 // x_codes, x_scales, w_codes, w_scales, send, P, h, h_kv, workspace
-SHIFTATTN_CALL(qkv_proj_pack_fp8) {
+PyObject* qkv_codes_call(PyObject* const* a, Py_ssize_t n, bool int8) {
+    const at::ScalarType kCode = int8 ? at::kChar : at::kByte;
     return run(n, 9, [&] {
         const at::Tensor &x = tensor(a[0]), &xs = tensor(a[1]), &w = tensor(a[2]), &ws = tensor(a[3]), &send = tensor(a[4]);
         const at::Tensor* work = dense_or_none(a[8]);
@@ -499,22 +507,25 @@ SHIFTATTN_CALL(qkv_proj_pack_fp8) {
         dims(w, 2, "w_codes");
         dims(send, 4, "send");
         const int64_t D = send.size(3);
-        need(x.scalar_type() == at::kByte && w.scalar_type() == at::kByte && xs.scalar_type() == at::kFloat && ws.scalar_type() == at::kFloat &&
+        need(x.scalar_type() == kCode && w.scalar_type() == kCode && xs.scalar_type() == at::kFloat && ws.scalar_type() == at::kFloat &&
                  send.scalar_type() == at::kBFloat16,
-             "codes uint8, scales float32, send bfloat16");
+             "codes uint8 (FP8) or int8, scales float32, send bfloat16");
         need(w.size(0) == (h + 2 * h_kv) * D && w.size(1) == x.size(1) && xs.dim() == 1 && xs.size(0) == x.size(0) && ws.dim() == 1 && ws.size(0) == w.size(0) &&
                  P > 0 && send.size(0) == P && send.size(2) == h / P + 2 * local_kv_heads(P, h_kv),
              "x [T, d_model], w [(h + 2 h_kv) D, d_model], a scale per row, send [P, T_pad, hq_l + 2 hkv_l, D]");
         need(x.is_contiguous() && xs.is_contiguous() && w.is_contiguous() && ws.is_contiguous() && send.is_contiguous(), "contiguous");
         return [xc = exchange(P, h, h_kv, D, SHIFTATTN_BF16), px = ptr(x), pxs = ptr(xs), pw = ptr(w), pws = ptr(ws), po = ptr(send), T = cut(x.size(0)),
-                T_pad = cut(send.size(1)), d = cut(x.size(1)), pk = ptr(work), nk = bytes(work), st = stream()] {
-            return lib.qkv_fp8(px, static_cast<float*>(pxs), pw, static_cast<float*>(pws), po, T, T_pad, d, &xc, pk, nk, st);
+                T_pad = cut(send.size(1)), d = cut(x.size(1)), pk = ptr(work), nk = bytes(work), st = stream(), int8] {
+            return (int8 ? lib.qkv_int8 : lib.qkv_fp8)(px, static_cast<float*>(pxs), pw, static_cast<float*>(pws), po, T, T_pad, d, &xc, pk, nk, st);
         };
     });
 }
+SHIFTATTN_CALL(qkv_proj_pack_fp8) { return qkv_codes_call(a, n, false); }
+SHIFTATTN_CALL(qkv_proj_pack_int8) { return qkv_codes_call(a, n, true); }
 
 // recv_codes, a_scales, w_codes, w_scales, out, workspace
-SHIFTATTN_CALL(unpack_o_proj_fp8) {
+PyObject* o_codes_call(PyObject* const* a, Py_ssize_t n, bool int8) {
+    const at::ScalarType kCode = int8 ? at::kChar : at::kByte;
     return run(n, 6, [&] {
         const at::Tensor &recv = tensor(a[0]), &as = tensor(a[1]), &w = tensor(a[2]), &ws = tensor(a[3]), &out = tensor(a[4]);
         const at::Tensor* work = dense_or_none(a[5]);
@@ -522,18 +533,20 @@ SHIFTATTN_CALL(unpack_o_proj_fp8) {
         dims(w, 2, "w_codes");
         dims(out, 2, "out");
         const int64_t P = recv.size(0), h = P * recv.size(2), D = recv.size(3);
-        need(recv.scalar_type() == at::kByte && w.scalar_type() == at::kByte && as.scalar_type() == at::kFloat && ws.scalar_type() == at::kFloat &&
+        need(recv.scalar_type() == kCode && w.scalar_type() == kCode && as.scalar_type() == at::kFloat && ws.scalar_type() == at::kFloat &&
                  out.scalar_type() == at::kBFloat16,
-             "codes uint8, scales float32, out bfloat16");
+             "codes uint8 (FP8) or int8, scales float32, out bfloat16");
         need(w.size(0) == out.size(1) && w.size(1) == h * D && as.size(0) >= out.size(0) && ws.dim() == 1 && ws.size(0) == out.size(1),
              "recv [P, T_pad, hq_l, D], w [d_model, h D], a scale per token and per feature, out [T, d_model]");
         need(recv.is_contiguous() && as.is_contiguous() && w.is_contiguous() && ws.is_contiguous() && out.is_contiguous(), "contiguous");
         return [xc = exchange(P, h, 0, D, SHIFTATTN_BF16), pr = ptr(recv), pas = ptr(as), pw = ptr(w), pws = ptr(ws), po = ptr(out), T = cut(out.size(0)),
-                T_pad = cut(recv.size(1)), d = cut(out.size(1)), pk = ptr(work), nk = bytes(work), st = stream()] {
-            return lib.o_proj_fp8(pr, static_cast<float*>(pas), pw, static_cast<float*>(pws), po, T, T_pad, d, &xc, pk, nk, st);
+                T_pad = cut(recv.size(1)), d = cut(out.size(1)), pk = ptr(work), nk = bytes(work), st = stream(), int8] {
+            return (int8 ? lib.o_proj_int8 : lib.o_proj_fp8)(pr, static_cast<float*>(pas), pw, static_cast<float*>(pws), po, T, T_pad, d, &xc, pk, nk, st);
         };
     });
 }
+SHIFTATTN_CALL(unpack_o_proj_fp8) { return o_codes_call(a, n, false); }
+SHIFTATTN_CALL(unpack_o_proj_int8) { return o_codes_call(a, n, true); }
 
 #define SHIFTATTN_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SHIFTATTN_METHOD(bind), SHIFTATTN_METHOD(pack_seq2head), SHIFTATTN_METHOD(unpack_head2seq), SHIFTATTN_METHOD(prefill),
@@ -541,6 +554,8 @@ PyMethodDef methods[] = {SHIFTATTN_METHOD(bind), SHIFTATTN_METHOD(pack_seq2head)
                          SHIFTATTN_METHOD(qkv_proj_pack), SHIFTATTN_METHOD(unpack_o_proj), SHIFTATTN_METHOD(quantize_rows_fp8),
                          SHIFTATTN_METHOD(quantize_recv_fp8), SHIFTATTN_METHOD(qkv_proj_pack_fp8), SHIFTATTN_METHOD(unpack_o_proj_fp8),
                          SHIFTATTN_METHOD(attn_desc), SHIFTATTN_METHOD(tables_append), SHIFTATTN_METHOD(tables_truncate),
+                         SHIFTATTN_METHOD(quantize_rows_int8), SHIFTATTN_METHOD(quantize_recv_int8), SHIFTATTN_METHOD(qkv_proj_pack_int8),
+                         SHIFTATTN_METHOD(unpack_o_proj_int8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -3,7 +3,6 @@ import numpy as np
 import pytest
 
 import plain_8bit as P
-from paper_2509_16495_amd import workloads as W
 
 pytestmark = pytest.mark.gpu
 
