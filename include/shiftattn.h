@@ -237,8 +237,8 @@ int shiftattn_unpack_o_proj_fp8_ws(const void *recv_codes, const float *a_scales
  *   y[t][f] = x_scale[t] * w_scale[f] * sum_k x_code[t][k] * w_code[f][k],
  * the sum exact in 32-bit integers (k below 131072, else EUNSUPPORTED), rounded to float32, scaled and rounded to bf16.  So results are
  * the same bits with any workspace and without one.
- * quantize_{rows,recv}_int8: a = the row's largest finite magnitude, scale = a / 127, code = the integer nearest to the exact product
- *   x * (127 / a), ties to even, where both quotients are float32; a row whose a is below 2^-100 gets scale 1 and codes of 0.
+ * quantize_{rows,recv}_int8: a = the row's largest finite magnitude, scale = a * (1 / 127), inv = 127 * (1 / a), each operation rounded
+ *   to float32; code = the integer nearest to the exact product x * inv, ties to even; a row whose a is below 2^-100 gets scale 1 and codes of 0.
  *   Infinities become 127 or -127 (in such a row too), NaN 0.
  * shiftattn_proj_workspace_bytes_int8: the size for int8 operands. */
 int shiftattn_quantize_rows_int8(const void *x, void *codes, float *scales, int32_t rows, int32_t cols,

@@ -241,7 +241,7 @@ hipError_t launch_proj_finish(const float* partial, int kg, int t_rows, void* c,
 hipError_t launch_quantize_rows_fp8(const void* x, void* codes, float* scales, int rows, int cols, int seg_len,
                                     int64_t seg_stride, int64_t row_stride, hipStream_t st);
 
-// the same with int8 codes: scale = amax / 127, code = nearest integer to x * (127 / amax)
+// the same with int8 codes: scale = amax * (1 / 127), code = nearest integer to x * (127 * (1 / amax))
 hipError_t launch_quantize_rows_int8(const void* x, void* codes, float* scales, int rows, int cols, int seg_len,
                                      int64_t seg_stride, int64_t row_stride, hipStream_t st);
 

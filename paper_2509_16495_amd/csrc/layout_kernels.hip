@@ -476,8 +476,8 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_fp8_kernel(const uint1
     });
 }
 
-// The same rows as int8 codes: a = largest finite |x| of the row, scale = a / 127, code = the integer nearest to the exact product
-// x * (127 / a), both quotients float32 (a below 2^-100: scale 1 and codes of 0); infinities saturate, NaN gives 0.  One fused multiply-add
+// The same rows as int8 codes: a = largest finite |x| of the row, scale = a * (1 / 127), inv = 127 * (1 / a), each operation rounded to
+// float32, code = the integer nearest to the exact product x * inv (a below 2^-100: scale 1 and codes of 0); infinities saturate, NaN gives 0.  One fused multiply-add
 // rounds the exact product to an integer, by adding 1.5 * 2^23, whose last place is 1; the code is its low byte.
 template <int kPieces>
 __global__ __launch_bounds__(kThreads) void quantize_rows_int8_kernel(const uint16_t* __restrict__ x, uint8_t* __restrict__ codes,
@@ -532,8 +532,8 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_int8_kernel(const uint
     }
     const bool tiny = bits < ((127u - 100u) << 7);   // 2^-100
     const float amax = __uint_as_float(bits << 16);
-    const float inv = tiny ? 1.f : 127.f / amax;
-    if (threadIdx.x == 0) scales[row] = tiny ? 1.f : amax / 127.f;
+    const float inv = tiny ? 1.f : 127.f * (1.f / amax);
+    if (threadIdx.x == 0) scales[row] = tiny ? 1.f : amax * (1.f / 127.f);
     auto code = [&](float v) -> uint32_t {
         if (!finite && !(fabsf(v) < INFINITY)) return v != v ? 0u : v > 0.f ? 127u : static_cast<uint32_t>(-127);   // (the first is uniform)
         return __float_as_uint(fmaf(v, inv, 12582912.f));

@@ -180,7 +180,7 @@ def quantise_int8(x):
     top = np.where(np.isfinite(x), np.abs(x), 0).max(-1, keepdims=True).astype(np.float32)
     tiny = top < np.float32(2.0 ** -100)
     safe = np.where(tiny, np.float32(1), top)
-    inv, scale = np.where(tiny, np.float32(1), np.float32(127) / safe), np.where(tiny, np.float32(1), safe / np.float32(127))
+    inv, scale = np.where(tiny, np.float32(1), np.float32(127) * (np.float32(1) / safe)), np.where(tiny, np.float32(1), safe * (np.float32(1) / np.float32(127)))
     with np.errstate(invalid="ignore", over="ignore"):
         y = np.clip(np.round(x.astype(np.float64) * inv), -127, 127)
     return np.where(np.isnan(y), 0, y).astype(np.int8), scale[..., 0]
