@@ -175,10 +175,10 @@ int check_new_kv(const void* k_new, const void* v_new, const int64_t* slots, boo
 }
 
 bool use_prefill_mfma(const AttnShape& s, int num_seqs, int max_seq_len) {
-    return !force_generic() && !s.block_scales && prefill_mfma_supported(s, num_seqs, max_seq_len);
+    return !force_generic() && prefill_mfma_supported(s, num_seqs, max_seq_len);
 }
 bool use_decode_mfma(const AttnShape& s, int num_seqs, int max_seq_len) {
-    return !force_generic() && !s.block_scales && decode_mfma_supported(s, num_seqs, max_seq_len);
+    return !force_generic() && decode_mfma_supported(s, num_seqs, max_seq_len);
 }
 
 // Argument checks of a prefill / decode call that need no launch (shared with the mixed entry point, which must

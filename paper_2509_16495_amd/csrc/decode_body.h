@@ -34,7 +34,13 @@
 // registers to the two bf16 pieces it stands for (exact: every E4M3 value is a bf16 value) and parked
 // where the bf16 path would have put them, so the LDS layout, the operand reads and all arithmetic are
 // shared.  k_scale rides in the logit scale, v_scale in the merge.
+//
+// With block scales (kBlockScales) the scales of the group's two blocks come with their codes, 8 bytes a block, and are applied by the
+// widening instruction, so that everything behind it is as for the other caches.  The wavefront that holds a pair's last group
+// owns that block: it finds the scale that the new token wants, and where it is larger than the block's, moves the codes it has just
+// loaded to the new scale in registers and writes them back (block_scale.h).
 #pragma once
+#include "block_scale.h"
 #include "internal.h"
 
 namespace shiftattn {
@@ -56,6 +62,7 @@ namespace decode_flat {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kD = 128;
 constexpr int kGroup = 32;         // tokens per wavefront step
@@ -81,14 +88,14 @@ constexpr int kIndexInts = kFlatMaxPairs + 1 + 16;        // LDS ints behind the
 // The flat kernel: see the file header.  cum[i + 1] holds the padded token count of pairs 0..i in
 // its upper bits and (padded - real) length of pair i in its low five bits.
 // the two bf16 pieces (8 elements each) of one 16-byte piece of E4M3 codes
-__device__ inline void widen_fp8(u32x4 codes, u32x4& lo, u32x4& hi) {
+__device__ inline void widen_fp8(u32x4 codes, u32x4& lo, u32x4& hi, float scale = 1.0f) {
     typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-        lo[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[w]), 1.0f, false));
-        lo[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[w]), 1.0f, true));
-        hi[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[2 + w]), 1.0f, false));
-        hi[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[2 + w]), 1.0f, true));
+        lo[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[w]), scale, false));
+        lo[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[w]), scale, true));
+        hi[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[2 + w]), scale, false));
+        hi[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[2 + w]), scale, true));
     }
 }
 
@@ -98,6 +105,7 @@ struct AppendArgs {
     const int64_t* slots;    // [num_seqs]; negative: nothing to append for that sequence
     int64_t kv_stride;
     float k_scale, v_scale;  // FP8 cache only
+    float* scales_out;       // block scales: where the append leaves them
 };
 
 // One workgroup of kWaves wavefronts, number wg of n_wg.  smem: kWaves x kStageBytes, 16-byte aligned; index: kIndexInts ints.
@@ -106,12 +114,13 @@ struct AppendArgs {
 // P = 1, exact in bf16, and the heaviest keys carry most of the rounding error: the fewer and longer ranges that decode rows get
 // beside chunks would else make them 1.5 % less exact than in a launch of their own (20 unified batches, two seeds each, relative
 // 2-norm against float64: 2.12e-3 against 2.09e-3; with it 2.03e-3), at the same speed.
-template <bool kFp8, bool kAppend, int kWaves, bool kGroupRef>
+template <bool kFp8, bool kAppend, int kWaves, bool kGroupRef, bool kBlockScales = false>
 __device__ __attribute__((always_inline)) inline void decode_flat_body(
     const uint16_t* __restrict__ q, int64_t q_stride, uint16_t* __restrict__ cache,
     const int32_t* __restrict__ block_table, int max_blocks, const int32_t* __restrict__ seq_lens,
     float* __restrict__ o_part, float* __restrict__ ml_part, int2* __restrict__ plan, int num_seqs, int hq_l, int hkv_l,
-    float c, int r_min, const AppendArgs& ap, unsigned char* smem, int* index, int wg, int n_wg) {
+    float c, int r_min, const AppendArgs& ap, unsigned char* smem, int* index, int wg, int n_wg, const float* __restrict__ scales = nullptr) {
+    static_assert(!kBlockScales || kFp8, "block scales belong to FP8 codes");
     int* cum = index;                             // [kFlatMaxPairs + 1]
     int* wave_sum = index + kFlatMaxPairs + 1;    // [kWaves]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -259,6 +268,7 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
         blk1 = table[min(b0 + 1, last_block)];
     };
     GroupFrags f;
+    f32x2 sc[2] = {{1.f, 1.f}, {1.f, 1.f}};   // block scales of the group's two blocks: K, V
     auto load_group = [&](int pr, int blk0, int blk1) {
         const int g = pr % hkv_l;
         if constexpr (kFp8) {  // one byte per element: K 2 KiB then V^T 2 KiB per (block, head)
@@ -271,6 +281,10 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
                 f.k[2 + j] = __builtin_nontemporal_load(k1 + 64 * j);
                 f.v[j] = __builtin_nontemporal_load(k0 + 128 + 64 * j);
                 f.v[2 + j] = __builtin_nontemporal_load(k1 + 128 + 64 * j);
+            }
+            if constexpr (kBlockScales) {
+                sc[0] = *reinterpret_cast<const f32x2*>(scales + (static_cast<size_t>(blk0) * hkv_l + g) * 2);
+                sc[1] = *reinterpret_cast<const f32x2*>(scales + (static_cast<size_t>(blk1) * hkv_l + g) * 2);
             }
         } else {
             const u32x4* k0 = reinterpret_cast<const u32x4*>(cache + cache_part_offset(blk0, g, 0, hkv_l, kD)) + lane;
@@ -338,6 +352,80 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
         fetch_ids(n_pair, n_pos, n_begin, n_ctx, blk0, blk1);
     }
     while (true) {
+        int patch_at = -1;   // block scales: where a new K row goes in the parked group, and its values (lanes 0 .. 15)
+        u32x4 patch;
+        if constexpr (kAppend && kBlockScales) {
+            const int off_g = pos - seg_begin;
+            if (off_g + kGroup >= ctx) {  // uniform: this group holds the pair's last token, position ctx - 1
+                const int s_a = pair / hkv_l, g_a = pair % hkv_l;
+                const int64_t slot = ap.slots[s_a];
+                if (slot >= 0) {
+                    const int tl = ctx - 1 - off_g, b = tl >> 4, t = tl & 15;  // block of the group, offset in it
+                    const int64_t blk_a = slot / kBlockSize;
+                    const size_t row = static_cast<size_t>(s_a) * ap.kv_stride + static_cast<size_t>(g_a) * kD;
+                    unsigned char* k_at = reinterpret_cast<unsigned char*>(cache) + cache_part_offset(blk_a, g_a, 0, hkv_l, kD);
+                    unsigned char* v_at = reinterpret_cast<unsigned char*>(cache) + cache_part_offset(blk_a, g_a, 1, hkv_l, kD);
+                    const u32x4 kx = *reinterpret_cast<const u32x4*>(ap.k_new + row + 8 * col);
+                    const float vx[2] = {__uint_as_float(static_cast<uint32_t>(ap.v_new[row + lane]) << 16),
+                                         __uint_as_float(static_cast<uint32_t>(ap.v_new[row + 64 + lane]) << 16)};
+                    float kf[8];
+                    uint32_t top_k = 0, top_v = max(finite_magnitude(vx[0]), finite_magnitude(vx[1]));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        kf[e] = __uint_as_float(e % 2 ? kx[e / 2] & 0xFFFF0000u : kx[e / 2] << 16);
+                        top_k = max(top_k, finite_magnitude(kf[e]));
+                    }
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) top_k = max(top_k, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top_k), o)));
+#pragma unroll
+                    for (int o = 32; o > 0; o >>= 1) top_v = max(top_v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top_v), o)));
+                    const f32x2 had = b ? sc[1] : sc[0];
+                    f32x2 now = {block_scale(top_k), block_scale(top_v)};
+                    if (t > 0) now[0] = fmaxf(now[0], had[0]), now[1] = fmaxf(now[1], had[1]);
+                    const bool grown = t > 0 && __builtin_amdgcn_readfirstlane(now[0] > had[0] || now[1] > had[1]);
+#pragma unroll
+                    for (int bb = 0; bb < 2; ++bb) {
+                        if (bb != b) continue;
+                        if (grown) {   // codes of the tokens in front of t move to the new scales (a ratio of 1 leaves them as they are)
+                            const float rk = had[0] / now[0], rv = had[1] / now[1];
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                if (8 * j + (lane >> 3) < t) {   // K: this piece lies in one token's row
+#pragma unroll
+                                    for (int w = 0; w < 4; ++w) f.k[2 * bb + j][w] = rescale_codes(f.k[2 * bb + j][w], rk);
+                                    *reinterpret_cast<u32x4*>(k_at + 1024 * j + 16 * lane) = f.k[2 * bb + j];
+                                }
+#pragma unroll
+                                for (int w = 0; w < 4; ++w) {    // V: tokens 4 w .. 4 w + 3 of one head-dim row
+                                    const uint32_t mask = t >= 4 * w + 4 ? 0xFFFFFFFFu : t <= 4 * w ? 0u : (1u << (8 * (t - 4 * w))) - 1u;
+                                    const uint32_t old = f.v[2 * bb + j][w];
+                                    f.v[2 * bb + j][w] = (rescale_codes(old, rv) & mask) | (old & ~mask);
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t code = e4m3_pair(vx[j], 0.f, now[1]) & 0xFFu;
+#pragma unroll
+                            for (int w = 0; w < 4; ++w)
+                                if (w == t >> 2) f.v[2 * bb + j][w] = (f.v[2 * bb + j][w] & ~(0xFFu << (8 * (t & 3)))) | (code << (8 * (t & 3)));
+                            if (grown) *reinterpret_cast<u32x4*>(v_at + 1024 * j + 16 * lane) = f.v[2 * bb + j];
+                            else v_at[1024 * j + 16 * lane + t] = static_cast<unsigned char>(code);
+                        }
+                        sc[bb] = now;
+                    }
+                    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+                    u32x2_t codes;
+                    codes[0] = e4m3_pair(kf[0], kf[1], now[0]) | (e4m3_pair(kf[2], kf[3], now[0]) << 16);
+                    codes[1] = e4m3_pair(kf[4], kf[5], now[0]) | (e4m3_pair(kf[6], kf[7], now[0]) << 16);
+                    u32x4 hi;
+                    widen_fp8(u32x4{codes[0], codes[1], 0u, 0u}, patch, hi, now[0]);
+                    patch_at = b * 4096 + t * 256 + ((lane ^ (t & 3) ^ (4 * ((t >> 2) ^ b))) << 4);
+                    if (lane < 16) *reinterpret_cast<u32x2_t*>(k_at + t * kD + 8 * lane) = codes;
+                    if (lane == 0) *reinterpret_cast<f32x2*>(ap.scales_out + (static_cast<size_t>(blk_a) * hkv_l + g_a) * 2) = now;
+                }
+            }
+        }
         // group (pair, pos) has arrived in f: park it in LDS, then reuse f for the next group
         if constexpr (kFp8) {
 #pragma unroll
@@ -345,11 +433,11 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     u32x4 lo, hi;
-                    widen_fp8(f.k[2 * b + j], lo, hi);
+                    widen_fp8(f.k[2 * b + j], lo, hi, sc[b][0]);
                     const int ka = (kw8 ^ (64 * ((2 * j) ^ b))) + 4096 * b + 2048 * j;
                     *reinterpret_cast<u32x4*>(my + ka) = lo;
                     *reinterpret_cast<u32x4*>(my + (ka ^ 16)) = hi;
-                    widen_fp8(f.v[2 * b + j], lo, hi);
+                    widen_fp8(f.v[2 * b + j], lo, hi, sc[b][1]);
                     const int va = vw8 + 4096 * b + 2048 * j;
                     *reinterpret_cast<u32x4*>(my + va) = lo;
                     *reinterpret_cast<u32x4*>(my + (va ^ 16)) = hi;
@@ -363,7 +451,10 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
                 *reinterpret_cast<u32x4*>(my + vw + 4096 + 1024 * j) = f.v[4 + j];
             }
         }
-        if constexpr (kAppend) {
+        if constexpr (kAppend && kBlockScales) {
+            if (patch_at >= 0 && lane < 16) *reinterpret_cast<u32x4*>(my + patch_at) = patch;
+        }
+        if constexpr (kAppend && !kBlockScales) {
             const int off_g = pos - seg_begin;
             if (off_g + kGroup >= ctx) {  // uniform: this group holds the pair's last token, position ctx - 1
                 const int s_a = pair / hkv_l, g_a = pair % hkv_l;

@@ -13,16 +13,16 @@ constexpr int kWaves = 4;
 constexpr int kFlatWorkgroups = 512;                      // two resident per compute unit
 constexpr int kFlatWorkers = kFlatWorkgroups * kWaves;    // wavefronts, each with its own token range
 
-template <bool kFp8, bool kAppend>
+template <bool kFp8, bool kAppend, bool kBlockScales = false>
 __global__ __launch_bounds__(kWaves * 64, 2) void decode_flat_kernel(
     const uint16_t* __restrict__ q, int64_t q_stride, uint16_t* __restrict__ cache,
     const int32_t* __restrict__ block_table, int max_blocks, const int32_t* __restrict__ seq_lens,
     float* __restrict__ o_part, float* __restrict__ ml_part, int2* __restrict__ plan, int num_seqs, int hq_l, int hkv_l,
-    float c, int r_min, AppendArgs ap) {
+    float c, int r_min, AppendArgs ap, const float* __restrict__ scales) {
     __shared__ __attribute__((aligned(16))) unsigned char smem[kWaves * kStageBytes];
     __shared__ int index[kIndexInts];
-    decode_flat_body<kFp8, kAppend, kWaves, false>(q, q_stride, cache, block_table, max_blocks, seq_lens, o_part, ml_part, plan, num_seqs, hq_l,
-                                            hkv_l, c, r_min, ap, smem, index, blockIdx.x, kFlatWorkgroups);
+    decode_flat_body<kFp8, kAppend, kWaves, false, kBlockScales>(q, q_stride, cache, block_table, max_blocks, seq_lens, o_part, ml_part, plan, num_seqs, hq_l,
+                                            hkv_l, c, r_min, ap, smem, index, blockIdx.x, kFlatWorkgroups, scales);
 }
 
 }  // namespace
@@ -92,13 +92,16 @@ hipError_t launch_decode_mfma(const void* q, const void* k_new, const void* v_ne
         uint16_t* out_run = static_cast<uint16_t*>(out) + static_cast<size_t>(s0) * a.out_stride;
         const AppendArgs ap = {append ? static_cast<const uint16_t*>(k_new) + static_cast<size_t>(s0) * a.kv_stride : nullptr,
                                append ? static_cast<const uint16_t*>(v_new) + static_cast<size_t>(s0) * a.kv_stride : nullptr,
-                               append ? slots + s0 : nullptr, a.kv_stride, a.k_scale, a.v_scale};
+                               append ? slots + s0 : nullptr, a.kv_stride, a.k_scale, a.v_scale, a.kv_scales};
         auto launch = [&](auto kernel) {
             kernel<<<kFlatWorkgroups, kWaves * 64, 0, st>>>(q_run, a.q_stride, static_cast<uint16_t*>(cache),
                                                             block_table + static_cast<size_t>(s0) * a.max_blocks, a.max_blocks,
-                                                            seq_lens + s0, o_part, ml_part, plan, n, a.hq_l, a.hkv_l, c, r_min, ap);
+                                                            seq_lens + s0, o_part, ml_part, plan, n, a.hq_l, a.hkv_l, c, r_min, ap, a.kv_scales);
         };
-        if (a.kv_fp8()) {
+        if (a.block_scales) {
+            if (append) launch(decode_flat_kernel<true, true, true>);
+            else launch(decode_flat_kernel<true, false, true>);
+        } else if (a.kv_fp8()) {
             if (append) launch(decode_flat_kernel<true, true>);
             else launch(decode_flat_kernel<true, false>);
         } else {

@@ -40,7 +40,8 @@ hipError_t launch_kv_write(const void* k_new, const void* v_new, const int64_t* 
                            void* cache, const AttnShape& a, hipStream_t st);
 // D = 128: the FP8 E4M3 cache blocks block_table[s][i], i < ceil(seq_lens[s] / 16), widened to bf16 at
 // scratch block s * nb + i (same K | V^T arrangement); table_out[s][i] = s * nb + i for all i < nb.
-hipError_t launch_fp8_blocks_to_bf16(const void* cache_fp8, const int32_t* block_table, int max_blocks,
+// scales: of a cache with block scales, which are applied (exact too); else nullptr, and the values are those of the codes
+hipError_t launch_fp8_blocks_to_bf16(const void* cache_fp8, const float* scales, const int32_t* block_table, int max_blocks,
                                      const int32_t* seq_lens, int num_seqs, int nb, int hkv_l, void* scratch_bf16,
                                      int32_t* table_out, hipStream_t st);
 

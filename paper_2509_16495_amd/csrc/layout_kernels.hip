@@ -301,7 +301,9 @@ __global__ __launch_bounds__(kThreads) void kv_write_fp8_kernel(const Elem* __re
 // FP8 E4M3 cache blocks of the contexts of a batch, widened to bf16 (D = 128): one workgroup per
 // (sequence, block index, KV head), one 16-byte piece of codes per thread.  K and V^T keep their
 // arrangement, so element e of the 4 KiB of codes becomes element e of the 8 KiB of bf16.
-__global__ __launch_bounds__(kThreads) void fp8_blocks_to_bf16_kernel(const uint8_t* __restrict__ cache,
+// kBlockScales: times the scale of the block, head and part, a power of two that the widening instruction applies.
+template <bool kBlockScales>
+__global__ __launch_bounds__(kThreads) void fp8_blocks_to_bf16_kernel(const uint8_t* __restrict__ cache, const float* __restrict__ scales,
                                                                       const int32_t* __restrict__ block_table,
                                                                       int max_blocks, const int32_t* __restrict__ seq_lens,
                                                                       int nb, int hkv_l, uint16_t* __restrict__ scratch,
@@ -314,13 +316,15 @@ __global__ __launch_bounds__(kThreads) void fp8_blocks_to_bf16_kernel(const uint
     const int64_t src_blk = block_table[static_cast<size_t>(s) * max_blocks + i];
     constexpr int D = 128, kCodes = 2 * kBlockSize * D;  // codes (and bf16 elements) per (block, head)
     const u32x4 codes = *(reinterpret_cast<const u32x4*>(cache + (static_cast<size_t>(src_blk) * hkv_l + g) * kCodes) + threadIdx.x);
+    float scale = 1.0f;   // K: the first half of the workgroup
+    if constexpr (kBlockScales) scale = scales[(static_cast<size_t>(src_blk) * hkv_l + g) * 2 + threadIdx.x / (kThreads / 2)];
     u32x4 lo, hi;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-        lo[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[w]), 1.0f, false));
-        lo[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[w]), 1.0f, true));
-        hi[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[2 + w]), 1.0f, false));
-        hi[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[2 + w]), 1.0f, true));
+        lo[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[w]), scale, false));
+        lo[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[w]), scale, true));
+        hi[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[2 + w]), scale, false));
+        hi[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(codes[2 + w]), scale, true));
     }
     u32x4* dst = reinterpret_cast<u32x4*>(scratch + (static_cast<size_t>(dst_blk) * hkv_l + g) * kCodes) + 2 * threadIdx.x;
     dst[0] = lo;
@@ -329,16 +333,19 @@ __global__ __launch_bounds__(kThreads) void fp8_blocks_to_bf16_kernel(const uint
 
 }  // namespace
 
-hipError_t launch_fp8_blocks_to_bf16(const void* cache_fp8, const int32_t* block_table, int max_blocks,
+hipError_t launch_fp8_blocks_to_bf16(const void* cache_fp8, const float* scales, const int32_t* block_table, int max_blocks,
                                      const int32_t* seq_lens, int num_seqs, int nb, int hkv_l, void* scratch_bf16,
                                      int32_t* table_out, hipStream_t st) {
     const int64_t wgs = static_cast<int64_t>(num_seqs) * nb;
     if (wgs == 0) return hipSuccess;
     if (wgs > 0x7FFFFFFF || hkv_l > 65535) return hipErrorInvalidValue;
     dim3 grid(static_cast<unsigned>(wgs), static_cast<unsigned>(hkv_l));
-    fp8_blocks_to_bf16_kernel<<<grid, kThreads, 0, st>>>(static_cast<const uint8_t*>(cache_fp8), block_table, max_blocks,
-                                                         seq_lens, nb, hkv_l, static_cast<uint16_t*>(scratch_bf16), table_out);
-    return hipGetLastError();
+    auto run = [&](auto kernel) {
+        kernel<<<grid, kThreads, 0, st>>>(static_cast<const uint8_t*>(cache_fp8), scales, block_table, max_blocks, seq_lens, nb, hkv_l,
+                                          static_cast<uint16_t*>(scratch_bf16), table_out);
+        return hipGetLastError();
+    };
+    return scales ? run(fp8_blocks_to_bf16_kernel<true>) : run(fp8_blocks_to_bf16_kernel<false>);
 }
 
 hipError_t launch_pack(const void* qkv, void* send, const XchgShape& s, hipStream_t st) {

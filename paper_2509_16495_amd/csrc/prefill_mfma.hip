@@ -730,7 +730,7 @@ Plan make_plan(int num_seqs, int total_q, int max_q_len, int max_seq_len, const 
     return pl;
 }
 
-// FP8 E4M3 cache: the blocks the batch reads are first widened to bf16 (exact) into a scratch cache in
+// FP8 E4M3 cache (with block scales: times these, exact too): the blocks the batch reads are first widened to bf16 (exact) into a scratch cache in
 // the workspace, block i of sequence s at scratch block s * nb + i with nb = blocks of the longest
 // context, together with the block table that says so; the kernel then runs on the scratch cache with
 // k_scale in its logit scale and v_scale on its output.  The pass moves 1.5 bytes per cached element
@@ -995,7 +995,7 @@ hipError_t bf16_view(const void* cache, const int32_t* block_table, const int32_
     unsigned char* scratch = static_cast<unsigned char*>(workspace) + (partial_bytes + 255) / 256 * 256;
     int32_t* table2 = reinterpret_cast<int32_t*>(scratch + f.cache_bytes);
     *v = {scratch, table2, f.nb};
-    return launch_fp8_blocks_to_bf16(cache, block_table, a.max_blocks, seq_lens, num_seqs, f.nb, a.hkv_l, scratch, table2, st);
+    return launch_fp8_blocks_to_bf16(cache, a.kv_scales, block_table, a.max_blocks, seq_lens, num_seqs, f.nb, a.hkv_l, scratch, table2, st);
 }
 
 PrefillParams narrow_params(const void* q, const CacheView& v, const int32_t* cu_seqlens_q, const int32_t* seq_lens, int num_seqs,
@@ -1118,7 +1118,7 @@ constexpr double kBothLimit = 0.88;
 
 BothPlan plan_both(int num_seqs, int total_q, int max_q_len, int max_seq_len, int num_dec, int max_dec_len, const AttnShape& a) {
     BothPlan best{};
-    if (option_prefill_splits() != 0 || option_prefill_pairing() == 1) return best;
+    if (option_prefill_splits() != 0 || option_prefill_pairing() == 1 || a.block_scales) return best;
     if (num_seqs < 1 || total_q < 1 || max_q_len < 1 || num_dec < 1 || max_dec_len < 1 || !decode_mfma_one_launch(num_dec, max_dec_len, a))
         return best;
     const double bytes = decode_bytes(num_dec, max_dec_len, a);
