@@ -483,8 +483,9 @@ int mixed(bool scaled, float* kv_scales, const void* q, const void* k_new, const
         return rc;
     if (new_kv) {
         if (!aligned16(kv_cache)) return fail(SHIFTATTN_EINVAL, "kv_cache must be 16-byte aligned");
-        hipError_t e = launch_kv_write(k_new, v_new, slot_mapping, static_cast<int>(rows), kv_cache, s,
-                                       static_cast<hipStream_t>(stream));
+        hipError_t e = scaled ? launch_kv_write_scaled(k_new, v_new, slot_mapping, static_cast<int>(rows), total_prefill_q, kv_cache, s,
+                                                       static_cast<hipStream_t>(stream))
+                              : launch_kv_write(k_new, v_new, slot_mapping, static_cast<int>(rows), kv_cache, s, static_cast<hipStream_t>(stream));
         if (e != hipSuccess) return hip_fail(e, "kv_write launch");
     }
     if (workspace && aligned16(workspace) && use_prefill_mfma(s, num_prefill_seqs, max_prefill_seq_len) &&

@@ -45,8 +45,9 @@ hipError_t launch_fp8_blocks_to_bf16(const void* cache_fp8, const float* scales,
                                      const int32_t* seq_lens, int num_seqs, int nb, int hkv_l, void* scratch_bf16,
                                      int32_t* table_out, hipStream_t st);
 
-// scaled_cache.hip : the append of an FP8 cache with block scales (any dtype / head_dim)
-hipError_t launch_kv_write_scaled(const void* k_new, const void* v_new, const int64_t* slots, int n_tokens, void* cache,
+// scaled_cache.hip : the append of an FP8 cache with block scales (any dtype / head_dim); the rows from chunk_rows on are expected to
+// be of one token a sequence (which only decides how they are shared out)
+hipError_t launch_kv_write_scaled(const void* k_new, const void* v_new, const int64_t* slots, int n_tokens, int chunk_rows, void* cache,
                                   const AttnShape& a, hipStream_t st);
 
 // tables.hip : block tables, slot maps and row offsets from request lengths

@@ -604,7 +604,7 @@ hipError_t launch_quantize_rows_fp8(const void* x, void* codes, float* scales, i
 
 hipError_t launch_kv_write(const void* k_new, const void* v_new, const int64_t* slots, int n_tokens, void* cache,
                            const AttnShape& a, hipStream_t st) {
-    if (a.block_scales) return launch_kv_write_scaled(k_new, v_new, slots, n_tokens, cache, a, st);
+    if (a.block_scales) return launch_kv_write_scaled(k_new, v_new, slots, n_tokens, n_tokens, cache, a, st);
     if (a.kv_fp8()) {
         const int64_t items = static_cast<int64_t>(n_tokens) * a.hkv_l * (a.D / 8);
         if (items == 0) return hipSuccess;
