@@ -52,6 +52,7 @@ struct DecodeRole {
     uint16_t* cache;
     const int32_t* block_table;
     const int32_t* seq_lens;
+    const float* scales;  // block scales of an FP8 cache that has them, else nullptr
     float* o_part;
     float* ml_part;
     int2* plan;
@@ -114,12 +115,14 @@ struct AppendArgs {
 // P = 1, exact in bf16, and the heaviest keys carry most of the rounding error: the fewer and longer ranges that decode rows get
 // beside chunks would else make them 1.5 % less exact than in a launch of their own (20 unified batches, two seeds each, relative
 // 2-norm against float64: 2.12e-3 against 2.09e-3; with it 2.03e-3), at the same speed.
-template <bool kFp8, bool kAppend, int kWaves, bool kGroupRef, bool kBlockScales = false>
+// kScales: block scales of an FP8 cache: 0 none, 1 there are some, 2 there are if `scales` is set.
+template <bool kFp8, bool kAppend, int kWaves, bool kGroupRef, int kScales = 0>
 __device__ __attribute__((always_inline)) inline void decode_flat_body(
     const uint16_t* __restrict__ q, int64_t q_stride, uint16_t* __restrict__ cache,
     const int32_t* __restrict__ block_table, int max_blocks, const int32_t* __restrict__ seq_lens,
     float* __restrict__ o_part, float* __restrict__ ml_part, int2* __restrict__ plan, int num_seqs, int hq_l, int hkv_l,
     float c, int r_min, const AppendArgs& ap, unsigned char* smem, int* index, int wg, int n_wg, const float* __restrict__ scales = nullptr) {
+    constexpr bool kBlockScales = kScales != 0;
     static_assert(!kBlockScales || kFp8, "block scales belong to FP8 codes");
     int* cum = index;                             // [kFlatMaxPairs + 1]
     int* wave_sum = index + kFlatMaxPairs + 1;    // [kWaves]
@@ -282,7 +285,7 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
                 f.v[j] = __builtin_nontemporal_load(k0 + 128 + 64 * j);
                 f.v[2 + j] = __builtin_nontemporal_load(k1 + 128 + 64 * j);
             }
-            if constexpr (kBlockScales) {
+            if (kScales == 1 || (kScales == 2 && scales)) {
                 sc[0] = *reinterpret_cast<const f32x2*>(scales + (static_cast<size_t>(blk0) * hkv_l + g) * 2);
                 sc[1] = *reinterpret_cast<const f32x2*>(scales + (static_cast<size_t>(blk1) * hkv_l + g) * 2);
             }
@@ -592,8 +595,8 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
 // the role's body in a kernel with LDS of its own layout: lds holds kWaves x kStageBytes and then kIndexInts ints
 template <bool kFp8, int kWaves>
 __device__ __attribute__((always_inline)) inline void decode_role(const DecodeRole& d, int64_t q_stride, int hq_l, int hkv_l, unsigned char* lds, int wg) {
-    decode_flat_body<kFp8, false, kWaves, true>(d.q, q_stride, d.cache, d.block_table, d.max_blocks, d.seq_lens, d.o_part, d.ml_part, d.plan, d.num_seqs,
-                                          hq_l, hkv_l, d.c, d.r_min, AppendArgs{}, lds, reinterpret_cast<int*>(lds + kWaves * kStageBytes), wg, d.n_wg);
+    decode_flat_body<kFp8, false, kWaves, true, kFp8 ? 2 : 0>(d.q, q_stride, d.cache, d.block_table, d.max_blocks, d.seq_lens, d.o_part, d.ml_part, d.plan, d.num_seqs,
+                                          hq_l, hkv_l, d.c, d.r_min, AppendArgs{}, lds, reinterpret_cast<int*>(lds + kWaves * kStageBytes), wg, d.n_wg, d.scales);
 }
 template <int kWaves>
 constexpr int kRoleLdsBytes = kWaves * kStageBytes + kIndexInts * 4;

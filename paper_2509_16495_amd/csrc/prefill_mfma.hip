@@ -1118,7 +1118,7 @@ constexpr double kBothLimit = 0.88;
 
 BothPlan plan_both(int num_seqs, int total_q, int max_q_len, int max_seq_len, int num_dec, int max_dec_len, const AttnShape& a) {
     BothPlan best{};
-    if (option_prefill_splits() != 0 || option_prefill_pairing() == 1 || a.block_scales) return best;
+    if (option_prefill_splits() != 0 || option_prefill_pairing() == 1) return best;
     if (num_seqs < 1 || total_q < 1 || max_q_len < 1 || num_dec < 1 || max_dec_len < 1 || !decode_mfma_one_launch(num_dec, max_dec_len, a))
         return best;
     const double bytes = decode_bytes(num_dec, max_dec_len, a);
@@ -1225,6 +1225,7 @@ bool launch_prefill_and_decode(const void* q, void* cache, const int32_t* block_
     d.cache = static_cast<uint16_t*>(cache);
     d.block_table = block_table + static_cast<size_t>(num_seqs) * a.max_blocks;
     d.seq_lens = seq_lens + num_seqs;
+    d.scales = a.kv_scales;
     d.o_part = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + dec_at);
     d.ml_part = d.o_part + rows * kD;
     d.plan = reinterpret_cast<int2*>(d.ml_part + rows * 2);
