@@ -405,6 +405,8 @@ int prefill(bool scaled, float* kv_scales, const void* q, const void* k_new, con
     if (mfma)
         e = launch_prefill_mfma(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, max_q_len,
                                 max_seq_len, out, workspace, workspace && aligned16(workspace) ? workspace_bytes : 0, s, st);
+    else if (scaled)
+        e = launch_attn_scaled(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, max_seq_len, out, s, st);
     else if (!force_generic() && prefill_f32_supported(s))
         e = launch_prefill_f32(q, kv_cache, block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, out, s, st);
     else
@@ -439,6 +441,8 @@ int decode(bool scaled, float* kv_scales, const void* q, const void* k_new, cons
         e = launch_decode_mfma(q, fused_append ? k_new : nullptr, fused_append ? v_new : nullptr,
                                fused_append ? slot_mapping : nullptr, kv_cache, block_table, seq_lens, num_seqs, max_seq_len,
                                out, workspace, s, st);
+    else if (scaled)
+        e = launch_attn_scaled(q, kv_cache, block_table, nullptr, seq_lens, num_seqs, num_seqs, max_seq_len, out, s, st);
     else
         e = launch_attn_generic(q, kv_cache, block_table, nullptr, seq_lens, num_seqs, num_seqs, out, s, st);
     return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "decode launch");

@@ -43,8 +43,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 constexpr int kWaves = 4;
 constexpr int kMaxD = 256;
 
-// kBlockScales: FP8 cache with a scale per (block, head, part); K's multiplies the logit, V's the element
-template <typename Elem, typename KvElem, bool kBlockScales = false>
+template <typename Elem, typename KvElem>
 __global__ __launch_bounds__(kWaves * 64) void attn_rows_kernel(
     const Elem* __restrict__ q, const KvElem* __restrict__ cache, const int32_t* __restrict__ block_table,
     const int32_t* __restrict__ cu_seqlens_q, const int32_t* __restrict__ seq_lens, int num_seqs, int total_q,
@@ -96,7 +95,6 @@ __global__ __launch_bounds__(kWaves * 64) void attn_rows_kernel(
 #pragma unroll
                 for (int x = 0; x < kPer; ++x) dot = fmaf(q_s[wave][dv * kPer + x], to_float(u.e[x]), dot);
             }
-            if constexpr (kBlockScales) dot *= a.kv_scales[(static_cast<size_t>(blk) * a.hkv_l + g) * 2];
             logit = dot * (a.scale * a.k_scale);
         }
         const float m_new = fmaxf(m_run, wave_max(logit));  // finite: key t0 is always visible
@@ -111,8 +109,6 @@ __global__ __launch_bounds__(kWaves * 64) void attn_rows_kernel(
         for (int b = 0; b < 4 && t0 + b * kBlockSize <= pos; ++b) {
             const int64_t blk = table[(t0 + b * kBlockSize) / kBlockSize];
             const KvElem* v_part = cache + cache_part_offset(blk, g, 1, a.hkv_l, D);
-            float v_scale = 1.f;
-            if constexpr (kBlockScales) v_scale = a.kv_scales[(static_cast<size_t>(blk) * a.hkv_l + g) * 2 + 1];
 #pragma unroll
             for (int x = 0; x < kMaxD / 64; ++x) {
                 const int d = lane + 64 * x;
@@ -126,8 +122,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_rows_kernel(
                         for (int y = 0; y < kPer; ++y) {
                             const int off = vv * kPer + y;
                             // slots past the context may hold anything (also NaN): select, do not multiply
-                            float val = (t0 + b * kBlockSize + off <= pos) ? to_float(u.e[y]) : 0.f;
-                            if constexpr (kBlockScales) val *= v_scale;
+                            const float val = (t0 + b * kBlockSize + off <= pos) ? to_float(u.e[y]) : 0.f;
                             o[x] = fmaf(p_s[wave][b * kBlockSize + off], val, o[x]);
                         }
                     }
@@ -441,16 +436,7 @@ hipError_t launch_attn_generic(const void* q, const void* cache, const int32_t* 
     const int64_t rows = static_cast<int64_t>(total_q) * a.hq_l;
     if (rows == 0) return hipSuccess;
     const unsigned grid = static_cast<unsigned>((rows + kWaves - 1) / kWaves);
-    if (a.block_scales) {
-        if (a.elem == 2)
-            attn_rows_kernel<uint16_t, uint8_t, true><<<grid, kWaves * 64, 0, st>>>(
-                static_cast<const uint16_t*>(q), static_cast<const uint8_t*>(cache), block_table, cu_seqlens_q, seq_lens,
-                num_seqs, total_q, static_cast<uint16_t*>(out), a);
-        else
-            attn_rows_kernel<float, uint8_t, true><<<grid, kWaves * 64, 0, st>>>(
-                static_cast<const float*>(q), static_cast<const uint8_t*>(cache), block_table, cu_seqlens_q, seq_lens,
-                num_seqs, total_q, static_cast<float*>(out), a);
-    } else if (a.kv_fp8()) {
+    if (a.kv_fp8()) {
         if (a.elem == 2)
             attn_rows_kernel<uint16_t, uint8_t><<<grid, kWaves * 64, 0, st>>>(
                 static_cast<const uint16_t*>(q), static_cast<const uint8_t*>(cache), block_table, cu_seqlens_q, seq_lens,

@@ -50,6 +50,10 @@ hipError_t launch_fp8_blocks_to_bf16(const void* cache_fp8, const float* scales,
 hipError_t launch_kv_write_scaled(const void* k_new, const void* v_new, const int64_t* slots, int n_tokens, int chunk_rows, void* cache,
                                   const AttnShape& a, hipStream_t st);
 
+// attn_scaled.hip : the same cache, any dtype / head_dim, prefill chunks and (cu_seqlens_q null) decode rows
+hipError_t launch_attn_scaled(const void* q, const void* cache, const int32_t* block_table, const int32_t* cu_seqlens_q, const int32_t* seq_lens,
+                              int num_seqs, int rows, int max_seq_len, void* out, const AttnShape& a, hipStream_t st);
+
 // tables.hip : block tables, slot maps and row offsets from request lengths
 size_t tables_workspace(int num_seqs);
 hipError_t launch_tables_append(const shiftattn_tables& t, const int32_t* new_lens, int num_prefill, int total_prefill_q, int rows, int32_t* cu,
