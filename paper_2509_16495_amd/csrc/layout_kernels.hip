@@ -541,29 +541,30 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_int8_kernel(const uint
     const float amax = __uint_as_float(bits << 16);
     const float inv = tiny ? 1.f : 127.f * (1.f / amax);
     if (threadIdx.x == 0) scales[row] = tiny ? 1.f : amax * (1.f / 127.f);
-    auto code = [&](float v) -> uint32_t {
-        if (!finite && !(fabsf(v) < INFINITY)) return v != v ? 0u : v > 0.f ? 127u : static_cast<uint32_t>(-127);   // (the first is uniform)
-        return __float_as_uint(fmaf(v, inv, 12582912.f));
-    };
-    auto encode = [&](u32x4 v) -> u32x2 {
-        u32x2 r;
+    auto store_all = [&](auto&& code) {
+        auto encode = [&](u32x4 v) -> u32x2 {
+            u32x2 r;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t a = v[2 * h], b = v[2 * h + 1];
-            const uint32_t c0 = code(__uint_as_float(a << 16)), c1 = code(__uint_as_float(a & 0xFFFF0000u));
-            const uint32_t c2 = code(__uint_as_float(b << 16)), c3 = code(__uint_as_float(b & 0xFFFF0000u));
-            r[h] = __builtin_amdgcn_perm(c1, c0, 0x0C0C0400u) | __builtin_amdgcn_perm(c3, c2, 0x04000C0Cu);
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t a = v[2 * h], b = v[2 * h + 1];
+                const uint32_t c0 = code(__uint_as_float(a << 16)), c1 = code(__uint_as_float(a & 0xFFFF0000u));
+                const uint32_t c2 = code(__uint_as_float(b << 16)), c3 = code(__uint_as_float(b & 0xFFFF0000u));
+                r[h] = __builtin_amdgcn_perm(c1, c0, 0x0C0C0400u) | __builtin_amdgcn_perm(c3, c2, 0x04000C0Cu);
+            }
+            return r;
+        };
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int piece = threadIdx.x + i * kThreads;
+            if (piece < pieces) *reinterpret_cast<u32x2*>(codes + offset(piece)) = encode(held[i]);
         }
-        return r;
+        if constexpr (kPieces == kQuantPieces)
+            for (int piece = threadIdx.x + kQuantPieces * kThreads; piece < pieces; piece += kThreads)
+                *reinterpret_cast<u32x2*>(codes + offset(piece)) = encode(*reinterpret_cast<const u32x4*>(x + offset(piece)));
     };
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-        const int piece = threadIdx.x + i * kThreads;
-        if (piece < pieces) *reinterpret_cast<u32x2*>(codes + offset(piece)) = encode(held[i]);
-    }
-    if constexpr (kPieces == kQuantPieces)
-        for (int piece = threadIdx.x + kQuantPieces * kThreads; piece < pieces; piece += kThreads)
-            *reinterpret_cast<u32x2*>(codes + offset(piece)) = encode(*reinterpret_cast<const u32x4*>(x + offset(piece)));
+    auto nearest = [&](float v) -> uint32_t { return __float_as_uint(fmaf(v, inv, 12582912.f)); };
+    if (finite) store_all(nearest);   // uniform
+    else store_all([&](float v) -> uint32_t { return fabsf(v) < INFINITY ? nearest(v) : v != v ? 0u : v > 0.f ? 127u : static_cast<uint32_t>(-127); });
 }
 
 hipError_t launch_quantize_rows_int8(const void* x, void* codes, float* scales, int rows, int cols, int seg_len,

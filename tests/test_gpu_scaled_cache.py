@@ -169,6 +169,12 @@ def _check(got, want, dtype, D, keys):
     assert np.all(np.isfinite(got)) and off.max() <= 1.0, (off.max(), np.unravel_index(off.argmax(), off.shape))
 
 
+@pytest.mark.parametrize("dtype,D,hq,hkv", [("f32", 64, 9, 1), ("bf16", 48, 10, 2)])
+def test_prefill_of_many_rows(B, dtype, D, hq, hkv):
+    """Rows times heads beyond the line from which a workgroup takes several heads of a group (the last one fewer)."""
+    _prefill(B, dtype, D, hq, hkv, [(900, 930), (61, 61)])
+
+
 HEADS = [("bf16", 128, 8, 1), ("bf16", 128, 5, 1), ("bf16", 128, 10, 2), ("bf16", 128, 16, 1), ("bf16", 128, 40, 2), ("bf16", 64, 4, 1), ("f32", 64, 4, 2),
          ("f32", 128, 2, 1), ("bf16", 256, 2, 1)]
 
@@ -204,6 +210,10 @@ def test_decode(B, dtype, D, hq, hkv, lens, append):
 @pytest.mark.parametrize("dtype,D,hq,hkv", HEADS)
 @pytest.mark.parametrize("lens", [[(1, 1)], [(70, 70), (33, 200), (0, 5), (1, 1), (128, 300), (17, 40)], [(300, 311)]])
 def test_prefill(B, dtype, D, hq, hkv, lens):
+    _prefill(B, dtype, D, hq, hkv, lens)
+
+
+def _prefill(B, dtype, D, hq, hkv, lens):
     import torch
     rng = np.random.Generator(np.random.PCG64(len(lens) * 31 + D + hq))
     cache, table, slots, k, v = _batch(rng, lens, hkv, D, dtype)
