@@ -769,6 +769,14 @@ struct Choice {
     Prefill64Plan w;
 };
 
+// A cache with block scales is for keys whose magnitudes differ from block to block, and there the 64-column wavefronts can fail at
+// their first attempt, which keeps the reference that a column's first tiles left: up to three walks over the keys.  The 128-column kernel here follows the
+// maximum from tile to tile.  us with the append, tokens of magnitudes exp(N(0, 0.7)) / all alike, 64-column wavefronts -> this kernel:
+// 2 x 1000 tokens on 16000, 8 heads 335 -> 165 / 132 -> 162; 1000 on 20000 213 -> 112 / 94 -> 109; 4 x 4000, 4 heads 188 -> 87 / 80 -> 83; 9000,
+// 8 heads 358 -> 185 / 164 -> 177; 3 x 450 on 4000, 16 heads 174 -> 87 / 73 -> 86.  Twice the time where it goes wrong against a quarter where
+// it does not, and the host does not know which: such caches stay here (unless the tile is set by option).
+bool follows_maximum(const AttnShape& a) { return a.block_scales && option_prefill_tile() == 0; }
+
 Choice choose(int num_seqs, int total_q, int max_q_len, int max_seq_len, const AttnShape& a) {
     Choice c;
     c.narrow = make_plan(num_seqs, total_q, max_q_len, max_seq_len, a);
@@ -776,7 +784,7 @@ Choice choose(int num_seqs, int total_q, int max_q_len, int max_seq_len, const A
     // (a cache widened from FP8 is bf16 by the time a kernel runs, so only the other conditions matter)
     AttnShape b = a;
     b.kv_elem = b.elem;
-    if (!prefill_mfma64_supported(b)) return c;
+    if (!prefill_mfma64_supported(b) || follows_maximum(a)) return c;
     c.w = prefill_mfma64_plan(num_seqs, total_q, max_q_len, max_seq_len, a, option_prefill_splits());
     const int forced = option_prefill_tile();
     if (forced == 128) return c;
@@ -824,6 +832,7 @@ enum Kind { kNarrow, kWide, kHalf, kKinds };
 const TileKernel& cost_of(Kind k) { return k == kNarrow ? kNarrowCost : k == kWide ? kWideCost : kHalfCost; }
 bool kind_allowed(Kind k, const AttnShape& bf16) {
     const int forced = option_prefill_tile();
+    if (k != kNarrow && follows_maximum(bf16)) return false;
     if (k == kNarrow) return forced != 256 || !prefill_mfma64_supported(bf16);
     if (!prefill_mfma64_supported(bf16)) return false;
     return k == kWide ? forced != 128 : forced != 256 && bf16.hq_l / bf16.hkv_l <= 128;
