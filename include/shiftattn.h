@@ -68,7 +68,8 @@
  *          offset o are multiplied by old / new and rounded again (exact but for those that become subnormal), in slots behind
  *          the appended tokens the codes stay.
  * A code is the nearest one to x / scale as above; infinities saturate.  What one call appends to a block must stand next to each
- * other in the call's rows, in slot order: one stretch of rows for each block (as the rows of a chunk are), each slot once.
+ * other in the call's rows, in slot order: one stretch of rows for each block (as the rows of a chunk are), each slot once; rows of
+ * a decode call, or the decode rows of a unified batch, each append to a block of their own.
  */
 #ifndef SHIFTATTN_H
 #define SHIFTATTN_H
@@ -354,8 +355,8 @@ int shiftattn_mixed(const void *q, const void *k_new, const void *v_new, const i
 
 /* ---- The same over a cache with block scales (a->kv_format = SHIFTATTN_KV_FP8_E4M3_BLOCKS; see the top of this file) ----
  * kv_scales (device, in/out): float32 [num_blocks][num_kv_heads][2], written by the append, read by attention.
- * All else as in the calls above, whose workspace queries serve these too (through a->kv_format).  The calls above refuse such a
- * descriptor, and these any other. */
+ * All else as in the calls above, whose workspace queries serve these too (through a->kv_format).  The calls above (and
+ * shiftattn_decode_static, which has no such form) refuse such a descriptor, and these any other. */
 int shiftattn_kv_write_scaled(const void *k_new, const void *v_new, const int64_t *slot_mapping, int32_t n_tokens,
                               void *kv_cache, float *kv_scales, const shiftattn_attn *a, void *stream);
 int shiftattn_prefill_scaled(const void *q, const void *k_new, const void *v_new, const int64_t *slot_mapping,

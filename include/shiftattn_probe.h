@@ -29,7 +29,7 @@
  *   Arguments as for shiftattn_mixed_workspace_bytes.
  * proj_plan: host only, nothing is enqueued.  What a projection of `rows` (>= 1; T_pad for qkv_proj_pack, T for
  *   unpack_o_proj) token rows with an [n_features][k] weight matrix launches when it is given a workspace of
- *   workspace_bytes, under the options as they are set.  fp8: the operands are FP8 codes.
+ *   workspace_bytes, under the options as they are set.  fp8: the operands are 8-bit codes (FP8, or int8, whose plans are the same).
  */
 #ifndef SHIFTATTN_PROBE_H
 #define SHIFTATTN_PROBE_H

@@ -788,7 +788,7 @@ int shiftattn_decode_static(const void* q, const void* k_new, const void* v_new,
                             const int32_t* block_table, const int32_t* seq_lens, int32_t num_seqs, int32_t max_seq_len,
                             void* out, const shiftattn_attn* a, void* stream) {
     const size_t need = shiftattn_decode_workspace_bytes(num_seqs, max_seq_len, a);
-    if (need == SIZE_MAX) {  // let the ordinary entry point name the bad argument (it needs no workspace to do so)
+    if (need == SIZE_MAX || a->kv_format == SHIFTATTN_KV_FP8_E4M3_BLOCKS) {  // (the latter has no such form) let the ordinary entry point name the bad argument (it needs no workspace to do so)
         return shiftattn_decode(q, k_new, v_new, slot_mapping, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, out,
                                 nullptr, 0, a, stream);
     }

@@ -6,9 +6,11 @@
 // The functions take what binding.py's take, positionally and complete, and return the library's status; what is refused is
 // refused with the same exceptions.  They hold no state but the library's addresses and the allocator (bind()).
 #include <Python.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <string>
 
 #include "shiftattn.h"
@@ -84,6 +86,12 @@ int32_t dtype_code(const at::Tensor& t) {
     throw Refused{PyExc_TypeError, std::string("unsupported tensor dtype ") + c10::toString(t.scalar_type())};
 }
 int32_t cut(int64_t v) { return static_cast<int32_t>(v); }
+// a launch goes to the current device: tensors of another one are refused (asked for by the calls over 8-bit codes with scales and the tables)
+void here(std::initializer_list<const at::Tensor*> tensors) {
+    for (const at::Tensor* t : tensors)
+        if (t && t->is_cuda() && t->get_device() != c10::hip::current_device())
+            throw Refused{PyExc_RuntimeError, "a tensor on the current device is wanted, not on " + t->device().str()};
+}
 void* stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
 // elements between consecutive tokens of a [tokens, heads, D] view whose inner two dims are dense
@@ -119,6 +127,7 @@ shiftattn_attn describe(const at::Tensor& q, const at::Tensor& cache, const at::
     need(cache.size(2) == 2 && cache.size(3) == kBlock * q.size(2) && cache.is_contiguous() && (fp8 || cache.scalar_type() == q.scalar_type()),
          "kv_cache: contiguous [num_blocks, hkv_l, 2, 16 * D] of q's type or uint8");
     need(table.scalar_type() == at::kInt && table.dim() == 2 && table.is_contiguous(), "block_table: contiguous int32 [num_seqs, max_blocks]");
+    if (kv_scales) here({&q, &cache, &table, k_new, out, kv_scales});
     shiftattn_attn a{};
     a.num_q_heads = cut(q.size(1)), a.num_kv_heads = cut(cache.size(1)), a.head_dim = cut(q.size(2)), a.dtype = dtype_code(q);
     a.block_size = kBlock, a.num_blocks = cut(cache.size(0)), a.max_blocks_per_seq = cut(table.size(1));
@@ -361,6 +370,7 @@ SHIFTATTN_CALL(kv_write) {
         d.num_blocks = cut(cache.size(0)), d.softmax_scale = 1.0f, d.kv_stride = row_stride(k);
         const at::Tensor* scales = tensor_or_none(a[6]);
         d.kv_format = scales_of(scales, cache) ? SHIFTATTN_KV_FP8_E4M3_BLOCKS : cache.scalar_type() == at::kByte ? SHIFTATTN_KV_FP8_E4M3 : SHIFTATTN_KV_SAME;
+        if (scales) here({&k, &v, &slots, &cache, scales});
         d.k_scale = real(a[4]), d.v_scale = real(a[5]);
         return [d, pk = ptr(k), pv = ptr(v), ps = ptr(slots), rows = cut(k.size(0)), pc = ptr(cache), st = stream(), pb = static_cast<float*>(ptr(scales))] {
             if (d.kv_format == SHIFTATTN_KV_FP8_E4M3_BLOCKS) return lib.kv_write_scaled(pk, pv, static_cast<int64_t*>(ps), rows, pc, pb, &d, st);
@@ -377,8 +387,13 @@ shiftattn_tables tables_of(const at::Tensor& lens, const at::Tensor& table, cons
          "seq_lens: contiguous int32 [num_seqs], block_table: contiguous int32 [num_seqs, max_blocks]");
     need(free.scalar_type() == at::kInt && free.dim() == 1 && free.is_contiguous() && count.scalar_type() == at::kInt && count.numel() == 1,
          "free_blocks: contiguous int32 [num_blocks], free_count: one int32");
+    here({&lens, &table, &free, &count});
     shiftattn_tables t{};
     t.num_seqs = cut(lens.size(0)), t.max_blocks_per_seq = cut(table.size(1)), t.num_blocks = cut(free.size(0));
+    return t;
+}
+// (their places are asked about last)
+shiftattn_tables placed(shiftattn_tables t, const at::Tensor& lens, const at::Tensor& table, const at::Tensor& free, const at::Tensor& count) {
     t.seq_lens = static_cast<int32_t*>(ptr(lens)), t.block_table = static_cast<int32_t*>(ptr(table));
     t.free_blocks = static_cast<int32_t*>(ptr(free)), t.free_count = static_cast<int32_t*>(ptr(count));
     return t;
@@ -397,9 +412,10 @@ SHIFTATTN_CALL(tables_append) {
         need(cu.scalar_type() == at::kInt && cu.dim() == 1 && cu.size(0) == static_cast<int64_t>(chunks) + 1 && cu.is_contiguous(),
              "cu_seqlens_q: contiguous int32 [num_prefill_seqs + 1]");
         need(slots.scalar_type() == at::kLong && slots.dim() == 1 && slots.is_contiguous(), "slot_mapping: contiguous int64 [rows]");
+        here({&fresh, &cu, &slots, &taken});
         const shiftattn_tables t = tables_of(lens, table, free, count);
         const at::Tensor* ws = workspace(a[10], a[3], own, [&] { return lib.tables_bytes(t.num_seqs); });
-        return [t, pn = ptr(fresh), chunks, chunk_rows, rows = cut(slots.size(0)), pu = ptr(cu), ps = ptr(slots), pt = ptr(taken), pw = ptr(ws), nw = bytes(ws),
+        return [t = placed(t, lens, table, free, count), pn = ptr(fresh), chunks, chunk_rows, rows = cut(slots.size(0)), pu = ptr(cu), ps = ptr(slots), pt = ptr(taken), pw = ptr(ws), nw = bytes(ws),
                 st = stream()] {
             return lib.tables_append(&t, static_cast<int32_t*>(pn), chunks, chunk_rows, rows, static_cast<int32_t*>(pu), static_cast<int64_t*>(ps),
                                      static_cast<int32_t*>(pt), pw, nw, st);
@@ -414,9 +430,10 @@ SHIFTATTN_CALL(tables_truncate) {
         const at::Tensor &keep = tensor(a[0]), &lens = tensor(a[1]);
         const at::Tensor &table = tensor(a[2]), &free = tensor(a[3]), &count = tensor(a[4]);
         need(keep.scalar_type() == at::kInt && keep.sizes() == lens.sizes() && keep.is_contiguous(), "keep_lens: contiguous int32 [num_seqs]");
+        here({&keep});
         const shiftattn_tables t = tables_of(lens, table, free, count);
         const at::Tensor* ws = workspace(a[5], a[1], own, [&] { return lib.tables_bytes(t.num_seqs); });
-        return [t, pk = ptr(keep), pw = ptr(ws), nw = bytes(ws), st = stream()] { return lib.tables_truncate(&t, static_cast<int32_t*>(pk), pw, nw, st); };
+        return [t = placed(t, lens, table, free, count), pk = ptr(keep), pw = ptr(ws), nw = bytes(ws), st = stream()] { return lib.tables_truncate(&t, static_cast<int32_t*>(pk), pw, nw, st); };
     });
 }
 
@@ -470,6 +487,7 @@ PyObject* quantize_rows_call(PyObject* const* a, Py_ssize_t n, bool int8) {
         need(x.scalar_type() == at::kBFloat16 && codes.scalar_type() == kCode && scales.scalar_type() == at::kFloat, "x bfloat16, codes uint8 (FP8) or int8, scales float32");
         need(codes.sizes() == x.sizes() && scales.dim() == 1 && scales.size(0) == x.size(0) && x.is_contiguous() && codes.is_contiguous() && scales.is_contiguous(),
              "codes: shape of x, scales: [rows], contiguous");
+        if (int8) here({&x, &codes, &scales});
         return [px = ptr(x), pc = ptr(codes), ps = ptr(scales), rows = cut(x.size(0)), cols = cut(x.size(1)), st = stream(), int8] {
             return (int8 ? lib.quantize_rows_int8 : lib.quantize_rows)(px, pc, static_cast<float*>(ps), rows, cols, st);
         };
@@ -487,6 +505,7 @@ PyObject* quantize_recv_call(PyObject* const* a, Py_ssize_t n, bool int8) {
         need(recv.scalar_type() == at::kBFloat16 && codes.scalar_type() == kCode && scales.scalar_type() == at::kFloat && codes.sizes() == recv.sizes(),
              "recv bfloat16, codes uint8 (FP8) or int8 of its shape, scales float32");
         need(recv.is_contiguous() && codes.is_contiguous() && scales.is_contiguous(), "recv, codes, scales: contiguous");
+        if (int8) here({&recv, &codes, &scales});
         return [x = exchange(recv.size(0), recv.size(0) * recv.size(2), 0, recv.size(3), SHIFTATTN_BF16), pr = ptr(recv), pc = ptr(codes), ps = ptr(scales),
                 T = cut(scales.size(0)), T_pad = cut(recv.size(1)), st = stream(), int8] {
             return (int8 ? lib.quantize_recv_int8 : lib.quantize_recv)(pr, pc, static_cast<float*>(ps), T, T_pad, &x, st);
@@ -514,6 +533,7 @@ PyObject* qkv_codes_call(PyObject* const* a, Py_ssize_t n, bool int8) {
                  P > 0 && send.size(0) == P && send.size(2) == h / P + 2 * local_kv_heads(P, h_kv),
              "x [T, d_model], w [(h + 2 h_kv) D, d_model], a scale per row, send [P, T_pad, hq_l + 2 hkv_l, D]");
         need(x.is_contiguous() && xs.is_contiguous() && w.is_contiguous() && ws.is_contiguous() && send.is_contiguous(), "contiguous");
+        if (int8) here({&x, &xs, &w, &ws, &send, work});
         return [xc = exchange(P, h, h_kv, D, SHIFTATTN_BF16), px = ptr(x), pxs = ptr(xs), pw = ptr(w), pws = ptr(ws), po = ptr(send), T = cut(x.size(0)),
                 T_pad = cut(send.size(1)), d = cut(x.size(1)), pk = ptr(work), nk = bytes(work), st = stream(), int8] {
             return (int8 ? lib.qkv_int8 : lib.qkv_fp8)(px, static_cast<float*>(pxs), pw, static_cast<float*>(pws), po, T, T_pad, d, &xc, pk, nk, st);
@@ -539,6 +559,7 @@ PyObject* o_codes_call(PyObject* const* a, Py_ssize_t n, bool int8) {
         need(w.size(0) == out.size(1) && w.size(1) == h * D && as.size(0) >= out.size(0) && ws.dim() == 1 && ws.size(0) == out.size(1),
              "recv [P, T_pad, hq_l, D], w [d_model, h D], a scale per token and per feature, out [T, d_model]");
         need(recv.is_contiguous() && as.is_contiguous() && w.is_contiguous() && ws.is_contiguous() && out.is_contiguous(), "contiguous");
+        if (int8) here({&recv, &as, &w, &ws, &out, work});
         return [xc = exchange(P, h, 0, D, SHIFTATTN_BF16), pr = ptr(recv), pas = ptr(as), pw = ptr(w), pws = ptr(ws), po = ptr(out), T = cut(out.size(0)),
                 T_pad = cut(recv.size(1)), d = cut(out.size(1)), pk = ptr(work), nk = bytes(work), st = stream(), int8] {
             return (int8 ? lib.o_proj_int8 : lib.o_proj_fp8)(pr, static_cast<float*>(pas), pw, static_cast<float*>(pws), po, T, T_pad, d, &xc, pk, nk, st);

@@ -330,3 +330,70 @@ def test_blocks_whose_offsets_pass_32_bits(B):
     _check(out, want, "bf16", D, 45)
     B.decode(_dev(q[-1:], "bf16"), codes, t, l, 45, out[:1], D ** -0.5, kv_scales=scales)
     _check(out[:1], [w[-1:] for w in want], "bf16", D, 45)
+
+
+@pytest.mark.parametrize("option,value", [("OPT_GENERIC_ONLY", 1), ("OPT_PREFILL_TILE", 128), ("OPT_PREFILL_TILE", 256), ("OPT_PREFILL_SPLITS", 3)])
+def test_kernels_chosen_by_option(B, option, value):
+    """The general kernel on the shapes of the tuned ones, the wide prefill kernels, more key ranges."""
+    import torch
+    B.set_option(getattr(B, option), value)
+    try:
+        _prefill(B, "bf16", 128, 8, 1, [(70, 70), (133, 900), (1, 40)])
+        if option == "OPT_GENERIC_ONLY":
+            test_decode(B, "bf16", 128, 10, 2, [700, 0, 2, 31, 0, 95], True)
+            test_mixed(B, "bf16", 128, 8, 1, [(70, 70), (33, 200)], [1, 17, 250, 64, 0])
+    finally:
+        B.set_option(getattr(B, option), 0)
+
+
+def test_chunks_and_rows_in_one_launch(B):
+    """A unified batch for which the plan puts the decode rows into the prefill kernel's launch, and the same batch with a workspace that
+    only holds the two launches."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(15))
+    D, hq, hkv = 128, 8, 1
+    chunks, rows = [(300, 2300)], [int(c) for c in rng.integers(1, 2200, 60)]
+    lens = chunks + [(1, c) for c in rows]
+    cache, table, slots, k, v = _batch(rng, lens, hkv, D, "bf16")
+    gpu = OnGpu(cache)
+    cache.append(k, v, slots)
+    q = _rows(rng, len(slots), hq, D, "bf16")
+    want = _want(cache, table, lens, q)
+    out = torch.empty((len(slots), hq, D), dtype=torch.bfloat16, device="cuda")
+    dev = dict(q=_dev(q, "bf16"), t=_dev(table), cu=_dev(np.array([0, 300], np.int32)), l=_dev(np.array([c for _, c in lens], np.int32)))
+    a = B.attn_desc(dev["q"], gpu.codes, dev["t"], D ** -0.5, None, out, kv_scales=gpu.scales)
+    assert B.prefill_plan(1, 300, 300, 2300, a, 60, max(rows)).decode_wgs > 0
+    both = B.mixed_workspace_bytes(1, 300, 300, 2300, 60, max(rows), a)
+    least = max(B.prefill_workspace_bytes(1, 300, 300, 2300, a), B.decode_workspace_bytes(60, max(rows), a))
+    new = dict(k_new=_dev(k, "bf16"), v_new=_dev(v, "bf16"), slot_mapping=_dev(slots))
+    for i, size in enumerate((both, least)):
+        ws = torch.full((size,), 0xA5, dtype=torch.uint8, device="cuda")
+        B.mixed(dev["q"], gpu.codes, dev["t"], dev["cu"], dev["l"], 1, 300, 2300, max(rows), out, D ** -0.5, workspace=ws, kv_scales=gpu.scales,
+                **(new if i == 0 else {}))
+        gpu.same(cache)
+        _check(out, want, "bf16", D, 2300)
+
+
+def test_two_streams_at_once(B):
+    """Batches of their own caches and workspaces on two streams, in flight together."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(16))
+    lens, work = [(1, 60 + 31 * i) for i in range(50)], []
+    for _ in range(2):
+        cache, table, slots, k, v = _batch(rng, lens, 1, 128, "bf16")
+        gpu = OnGpu(cache)
+        cache.append(k, v, slots)
+        q = _rows(rng, 50, 8, 128, "bf16")
+        out = torch.empty((50, 8, 128), dtype=torch.bfloat16, device="cuda")
+        args = (_dev(q, "bf16"), gpu.codes, _dev(table), _dev(np.array([c for _, c in lens], np.int32)), lens[-1][1], out, 128 ** -0.5)
+        work.append((cache, gpu, args, dict(k_new=_dev(k, "bf16"), v_new=_dev(v, "bf16"), slot_mapping=_dev(slots), kv_scales=gpu.scales), _want(cache, table, lens, q)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    for _ in range(20):
+        for st, (_, _, args, new, _) in zip(streams, work):
+            with torch.cuda.stream(st):
+                B.decode(*args, **new)
+    torch.cuda.synchronize()
+    for cache, gpu, args, _, want in work:
+        gpu.same(cache)
+        _check(args[5], want, "bf16", 128, lens[-1][1])
