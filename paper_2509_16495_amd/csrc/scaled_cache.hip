@@ -65,8 +65,8 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void kv_write_scaled_kernel(const
     }
 }
 
-// bf16, D = 128: a wavefront takes the runs that start in its window of tokens.  Lane (q, dv) = (lane / 16, lane % 16) holds elements 8 dv ..
-// 8 dv + 7 of the tokens at block offsets 4 q .. 4 q + 3, so that the four codes of a head-dim row that lie next to each other in V's
+// bf16, D = 128 or 64: a wavefront takes the runs that start in its window of tokens.  Lane (q, dv) = (lane / 16, lane % 16) holds elements 8 dv ..
+// 8 dv + 7 (where D has them) of the tokens at block offsets 4 q .. 4 q + 3, so that the four codes of a head-dim row that lie next to each other in V's
 // block come from one lane: a 4 x 4 byte transposition in registers, a word per head-dim row through LDS, and V goes out as whole rows of
 // 16 codes.  Where the run does not fill the block those rows are read first and merged.
 // Bound: bytes for large launches, for small ones the chain of round trips slot - rows - stores.  Windows: of one token up to 4096 (token,
@@ -77,10 +77,10 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 constexpr int kTileBytes = 128 * 16 + 16 * 16;   // per wavefront: 128 rows of 16 codes, 16 bytes more behind every eight (banks)
 
+template <int D>
 __global__ __launch_bounds__(64 * kWavesPerWg) void kv_write_scaled_rows_kernel(const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new,
                                                                                 const int64_t* __restrict__ slots, int n_tokens, int window_of_chunks,
                                                                                 int chunk_rows, uint8_t* cache, float* scales, int hkv_l, int64_t kv_stride) {
-    constexpr int D = 128;
     __shared__ __attribute__((aligned(16))) unsigned char tile_all[kWavesPerWg * kTileBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     unsigned char* tile = tile_all + wave * kTileBytes;
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void kv_write_scaled_rows_kernel(
         for (int i = 0; i < 4; ++i) {
             const int t = 4 * q + i - off;
             kx[i] = vx[i] = u32x4{0u, 0u, 0u, 0u};
-            if (t >= 0 && t < len) {
+            if (t >= 0 && t < len && 8 * dv < D) {
                 const size_t at = src + static_cast<size_t>(t) * kv_stride;
                 kx[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k_new + at));
                 vx[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v_new + at));
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void kv_write_scaled_rows_kernel(
         }
         if (!whole) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) v_old[j] = *reinterpret_cast<const u32x4*>(v_at + 1024 * j + 16 * lane);
+            for (int j = 0; j < D / 64; ++j) v_old[j] = *reinterpret_cast<const u32x4*>(v_at + 1024 * j + 16 * lane);
         }
         if (off > 0) had_k = s_blk[0], had_v = s_blk[1];
         // largest magnitudes as bits, K's in the upper half of a word, V's in the lower
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void kv_write_scaled_rows_kernel(
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 4 * q + i - off;
-            if (t >= 0 && t < len)
+            if (t >= 0 && t < len && 8 * dv < D)
                 __builtin_nontemporal_store(encode(kx[i], now_k), reinterpret_cast<u32x2*>(k_at + (4 * q + i) * D + dv * 8));
             vc[i] = encode(vx[i], now_v);
         }
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void kv_write_scaled_rows_kernel(
         __builtin_amdgcn_wave_barrier();
         const bool grown_k = off > 0 && now_k > had_k, grown_v = off > 0 && now_v > had_v;   // uniform
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < D / 64; ++j) {
             const int d = lane + 64 * j;
             u32x4 row = *reinterpret_cast<const u32x4*>(tile + d * 16 + (d >> 3) * 16);
             if (!whole) {
@@ -222,10 +222,10 @@ __global__ __launch_bounds__(64 * kWavesPerWg) void kv_write_scaled_rows_kernel(
             }
             __builtin_nontemporal_store(row, reinterpret_cast<u32x4*>(v_at + 1024 * j + 16 * lane));
         }
-        if (grown_k) {   // K rows in front of the run: eight rows a load
+        if (grown_k) {   // K rows in front of the run: 1 KiB of rows a load
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (8 * j + (lane >> 3) < off) {
+            for (int j = 0; j < D / 64; ++j) {
+                if ((1024 * j + 16 * lane) / D < off) {
                     u32x4* at = reinterpret_cast<u32x4*>(k_at + 1024 * j + 16 * lane);
                     u32x4 x = *at;
 #pragma unroll
@@ -245,13 +245,16 @@ hipError_t launch_kv_write_scaled(const void* k_new, const void* v_new, const in
                                   const AttnShape& a, hipStream_t st) {
     const int64_t waves = static_cast<int64_t>(n_tokens) * a.hkv_l;
     if (waves == 0) return hipSuccess;
-    if (a.elem == 2 && a.D == 128 && a.hkv_l <= 65535) {
+    if (a.elem == 2 && (a.D == 128 || a.D == 64) && a.hkv_l <= 65535) {
         const int window = static_cast<int64_t>(chunk_rows) * a.hkv_l <= 4096 ? 1 : 8;
         const int64_t windows = (static_cast<int64_t>(chunk_rows) + window - 1) / window + n_tokens - chunk_rows;
         const dim3 grid(static_cast<unsigned>((windows + kWavesPerWg - 1) / kWavesPerWg), static_cast<unsigned>(a.hkv_l));
-        kv_write_scaled_rows_kernel<<<grid, 64 * kWavesPerWg, 0, st>>>(static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), slots,
-                                                                       n_tokens, window, chunk_rows, static_cast<uint8_t*>(cache), a.kv_scales, a.hkv_l, a.kv_stride);
-        return hipGetLastError();
+        auto rows = [&](auto kernel) {
+            kernel<<<grid, 64 * kWavesPerWg, 0, st>>>(static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), slots, n_tokens, window,
+                                                      chunk_rows, static_cast<uint8_t*>(cache), a.kv_scales, a.hkv_l, a.kv_stride);
+            return hipGetLastError();
+        };
+        return a.D == 128 ? rows(kv_write_scaled_rows_kernel<128>) : rows(kv_write_scaled_rows_kernel<64>);
     }
     const int64_t wgs = (waves + kWavesPerWg - 1) / kWavesPerWg;
     if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;

@@ -261,7 +261,8 @@ size_t tables_workspace(int num_seqs) { return (static_cast<size_t>(num_seqs) + 
 // One launch of one workgroup, or a scan and a launch that fills.  Append and truncate of a step, us in a replayed graph, one / two launches
 // for the append: 61 decode rows 5.2 / 7.0, 1000 9.5 / 12.2, 2120 rows 10.1 / 11.2, 2456 10.7 / 10.8, 11520 18.7 / 16.1, 136456 112 / 17.6 (the
 // last two before both were made faster; now 12.6 and 13.1 in two).  How many blocks a truncate gives back is known on the GPU only, so its line lies
-// where the most that it can be costs a workgroup some 80 us: of few blocks one launch saves 1.6 us, of 8500 two save 11.
+// where the most that it can be costs a workgroup some 80 us: of few blocks one launch saves 1.6 us, of 8500 two save 11.  Threads of that one workgroup,
+// 256 / 512 / 1024: append and truncate of 61 decode rows 5.2 / 5.3 / 5.7 us, of 25 prompts (5400 blocks back) 21 / 16.2 / 12.8.
 constexpr int kOneLaunchRows = 2560, kOneLaunchBlocks = 65536;
 
 // threads of the workgroup that scans: as few wavefronts as hold the sequences
@@ -293,7 +294,7 @@ hipError_t launch_tables_truncate(const shiftattn_tables& t, const int32_t* keep
     int32_t* ws = static_cast<int32_t*>(workspace);
     const int64_t entries = static_cast<int64_t>(t.num_seqs) * t.max_blocks_per_seq, most = entries < t.num_blocks ? entries : t.num_blocks;
     if (t.num_seqs <= kOnePass && most <= kOneLaunchBlocks)
-        return by_threads(most > 1024 && t.num_seqs < 256 ? 256 : t.num_seqs, [&](auto threads) {
+        return by_threads(most > 4096 && t.num_seqs < 512 ? 512 : most > 1024 && t.num_seqs < 256 ? 256 : t.num_seqs, [&](auto threads) {
             tables_truncate_kernel<true, decltype(threads)::value><<<1, decltype(threads)::value, 0, st>>>(t, keep_lens, ws);
         });
     hipError_t e = by_threads(t.num_seqs, [&](auto threads) {

@@ -76,11 +76,12 @@ def test_append_is_bit_exact(B, dtype, D, heads, lens):
     gpu.same(cache)
 
 
+@pytest.mark.parametrize("D", [128, 64])
 @pytest.mark.parametrize("heads,lens", [(1, [(4200, 4205), (1, 1), (1, 90), (3, 3), (1, 17), (1, 18), (777, 800), (2, 33)]), (3, [(1500, 1500), (60, 71)] + [(1, 7 * i) for i in range(1, 40)])])
-def test_append_of_many_tokens(B, heads, lens):
+def test_append_of_many_tokens(B, heads, lens, D):
     """Batches in which a wavefront looks after several tokens: runs that cross its window, several of them in one, rows without a slot."""
     rng = np.random.Generator(np.random.PCG64(heads))
-    cache, table, slots, k, v = _batch(rng, lens, heads, 128, "bf16")
+    cache, table, slots, k, v = _batch(rng, lens, heads, D, "bf16")
     pad = np.sort(rng.integers(0, len(lens), 3))            # in front of some sequences, so that the windows shift
     at = np.cumsum([0] + [n for n, _ in lens])[pad]
     slots, k, v = (np.insert(x, at, fill, 0) for x, fill in ((slots, -1), (k, 9.0), (v, 9.0)))
