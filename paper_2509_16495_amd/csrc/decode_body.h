@@ -271,10 +271,13 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
         blk1 = table[min(b0 + 1, last_block)];
     };
     GroupFrags f;
-    f32x2 sc[2] = {{1.f, 1.f}, {1.f, 1.f}};   // block scales of the group's two blocks: K, V
+    f32x2 sc_raw = {1.f, 1.f};   // block scales of the group's two blocks, K and V: the first block's in lanes 0 .. 31
     auto load_group = [&](int pr, int blk0, int blk1) {
         const int g = pr % hkv_l;
         if constexpr (kFp8) {  // one byte per element: K 2 KiB then V^T 2 KiB per (block, head)
+            if (kScales == 1 || (kScales == 2 && scales)) {   // in front of the codes: the first codes to arrive can then be widened
+                sc_raw = *reinterpret_cast<const f32x2*>(scales + (static_cast<size_t>(lane < 32 ? blk0 : blk1) * hkv_l + g) * 2);
+            }
             const unsigned char* cb = reinterpret_cast<const unsigned char*>(cache);
             const u32x4* k0 = reinterpret_cast<const u32x4*>(cb + cache_part_offset(blk0, g, 0, hkv_l, kD)) + lane;
             const u32x4* k1 = reinterpret_cast<const u32x4*>(cb + cache_part_offset(blk1, g, 0, hkv_l, kD)) + lane;
@@ -284,10 +287,6 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
                 f.k[2 + j] = __builtin_nontemporal_load(k1 + 64 * j);
                 f.v[j] = __builtin_nontemporal_load(k0 + 128 + 64 * j);
                 f.v[2 + j] = __builtin_nontemporal_load(k1 + 128 + 64 * j);
-            }
-            if (kScales == 1 || (kScales == 2 && scales)) {
-                sc[0] = *reinterpret_cast<const f32x2*>(scales + (static_cast<size_t>(blk0) * hkv_l + g) * 2);
-                sc[1] = *reinterpret_cast<const f32x2*>(scales + (static_cast<size_t>(blk1) * hkv_l + g) * 2);
             }
         } else {
             const u32x4* k0 = reinterpret_cast<const u32x4*>(cache + cache_part_offset(blk0, g, 0, hkv_l, kD)) + lane;
@@ -355,6 +354,14 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
         fetch_ids(n_pair, n_pos, n_begin, n_ctx, blk0, blk1);
     }
     while (true) {
+        f32x2 sc[2] = {{1.f, 1.f}, {1.f, 1.f}};
+        if constexpr (kBlockScales) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                sc[0][x] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc_raw[x]), 0));
+                sc[1][x] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc_raw[x]), 32));
+            }
+        }
         int patch_at = -1;   // block scales: where a new K row goes in the parked group, and its values (lanes 0 .. 15)
         u32x4 patch;
         if constexpr (kAppend && kBlockScales) {
