@@ -377,8 +377,9 @@ int shiftattn_mixed_scaled(const void *q, const void *k_new, const void *v_new, 
 /* ---- Block tables and slot maps on the GPU ---------------------------------------------------------------------------
  * What the calls above take beside their tensors, kept in device memory and brought from one step to the next there: an engine
  * that replays its steps from a graph, or does not want to wait for lengths to reach the host, gives its sequences cache
- * blocks and takes them back with these two calls.  The arrays are the caller's; a zeroed free_count and a free_blocks filled
- * with 0 .. num_blocks - 1 (then free_count = num_blocks) is all the set-up there is. */
+ * blocks and takes them back with these two calls.  The arrays are the caller's; free_blocks = 0 .. num_blocks - 1, free_count =
+ * num_blocks and seq_lens = 0 are all the set-up there is.  A block belongs to one sequence: what sequences share (a common prefix) the
+ * caller keeps out of the lengths that it truncates. */
 typedef struct shiftattn_tables {
     int32_t num_seqs;           /* sequences of the batch, in the order of shiftattn_mixed: chunks, then decode rows          */
     int32_t max_blocks_per_seq; /* row length of block_table                                                                 */
@@ -400,7 +401,7 @@ typedef struct shiftattn_tables {
  *                                 of the j-th decode sequence; -1 in every other row
  *   taken (device, out)         : int32 [num_seqs], the new tokens for which there was room: new_lens[s] or 0
  *   seq_lens grows by taken; the caller's decode sequences without a token keep their length and get slot -1.
- *   A sequence is refused (taken 0, nothing of it changes) if its tokens exceed its row of block_table, a decode sequence that
+ *   A sequence is refused (taken 0, nothing of it changes) if its tokens exceed its row of block_table or 2^31 - 1, a decode sequence that
  *   brings more than one, a chunk if the rows of the chunks up to and with it (those refused for the first reason apart) exceed
  *   total_prefill_q, and any that needs blocks if the blocks needed up to and with it (of those not refused so far) exceed
  *   free_count.  Blocks leave the stack from the top in the order of sequences and tokens.

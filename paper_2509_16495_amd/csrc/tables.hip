@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void tables_append_kernel(shiftattn_table
     __shared__ uint32_t wave_sum[kThreads / 64];
     __shared__ int given_s;
     __shared__ Shared sh;
-    const int64_t room = static_cast<int64_t>(t.max_blocks_per_seq) * kBlockSize;
+    const int64_t room = min(static_cast<int64_t>(t.max_blocks_per_seq) * kBlockSize, static_cast<int64_t>(kMost));   // (lengths are int32)
     const int height = min(max(*t.free_count, 0), t.num_blocks);
     uint32_t asked_c = 0, need_c = 0, rows_c = 0;
     if (threadIdx.x == 0) given_s = 0;

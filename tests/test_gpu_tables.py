@@ -101,6 +101,19 @@ def test_lengths_near_the_end_of_32_bits(B):
     assert result[2].tolist() == [40, 0, 0, 0, 2]
 
 
+def test_lengths_stay_below_2_31(B):
+    """A row of block_table that could hold more tokens than an int32 length can say."""
+    import torch
+    wide = 2 ** 27 + 2
+    table, lens, free = torch.zeros((1, wide), dtype=torch.int32, device="cuda"), _dev([2 ** 31 - 20]), _dev([5, 6, 7])
+    count, cu, slots, taken = _dev([3]), _dev([0, 0]), _dev(np.zeros(40), np.int64), _dev([0])
+    for new, want in ((30, 0), (20, 0), (19, 19)):
+        B.tables_append(_dev([new]), 1, 40, lens, table, free, count, cu, slots, taken)
+        assert taken.tolist() == [want] and cu.tolist() == [0, want] and lens.tolist() == [2 ** 31 - 20 + want] and int((slots >= 0).sum()) == want
+    # offsets 12 .. 15 of the block that was there (0), then those of the block taken
+    assert count.tolist() == [2] and int(table[0, 2 ** 27 - 1]) == 7 and slots[:19].tolist() == [12, 13, 14, 15] + list(range(112, 127))
+
+
 def test_no_sequences_leave_an_empty_map(B):
     import torch
     plain = P.Tables([], 4, np.arange(3), 3)
