@@ -98,7 +98,6 @@ struct GemmParams {
     uint16_t* __restrict__ c;              // bf16
     const float* __restrict__ xs;          // FP8, int8: one scale per token row
     const float* __restrict__ ws;          // FP8, int8: one scale per output feature
-    bool int8;
     int M, M_out, N, K;               // M token rows exist, rows M..M_out-1 of the result are written as zeros
     // mode 0 (qkv_proj_pack): x dense [M][K]; result columns scattered to send buffers (XchgShape below)
     // mode 1 (unpack_o_proj): x gathered from recv [P][T_pad][hq_l][128] (k = (p hq_l + j) 128 + e); result dense [M][N]
@@ -729,8 +728,8 @@ hipError_t launch_tile(TileKind kind, const GemmParams& p, hipStream_t st) {
         default: return launch<kFp8, 128, 128, 4, kInt8>(p, st);
     }
 }
-hipError_t launch_kind(TileKind kind, const GemmParams& p, hipStream_t st) {
-    return p.int8 ? launch_tile<false, true>(kind, p, st) : p.xs ? launch_tile<true, false>(kind, p, st) : launch_tile<false, false>(kind, p, st);
+hipError_t launch_kind(TileKind kind, const GemmParams& p, bool int8, hipStream_t st) {
+    return int8 ? launch_tile<false, true>(kind, p, st) : p.xs ? launch_tile<true, false>(kind, p, st) : launch_tile<false, false>(kind, p, st);
 }
 
 template <bool kFp8, int TN, int TM, int ST, bool kInt8 = false>
@@ -805,7 +804,7 @@ void proj_gemm_describe(int M_out, int N, int K, bool fp8, size_t workspace_byte
 double proj_gemm_us(int M_out, int N, int K, bool fp8, size_t workspace_bytes) { return plan_gemm(M_out, N, K, fp8, workspace_bytes).us; }
 
 // runs the product in the best way for which the workspace has room
-static hipError_t run_gemm(GemmParams& p, void* workspace, size_t workspace_bytes, hipStream_t st) {
+static hipError_t run_gemm(GemmParams& p, bool int8, void* workspace, size_t workspace_bytes, hipStream_t st) {
     // (or int8: as many bytes, the same matrix rate; over 24 products of 160 .. 3500 rows the plans for FP8 codes are at most 7 % behind the
     // best tile and split for int8 ones, 2 % on average)
     const bool fp8 = p.xs != nullptr;
@@ -815,16 +814,16 @@ static hipError_t run_gemm(GemmParams& p, void* workspace, size_t workspace_byte
     if (pl.lead_tiles > 0) {
         p.m_base = 0;
         p.m_tiles = pl.lead_tiles;
-        const hipError_t e = launch_kind(pl.lead, p, st);
+        const hipError_t e = launch_kind(pl.lead, p, int8, st);
         if (e != hipSuccess) return e;
     }
     p.m_base = pl.lead_tiles * kTileTokens[pl.lead];
     p.m_tiles = (p.M_out - p.m_base + kTileTokens[pl.tail] - 1) / kTileTokens[pl.tail];
     p.k_splits = pl.splits;
     if (pl.splits > 1) p.partial = static_cast<float*>(workspace);
-    const hipError_t e = launch_kind(pl.tail, p, st);
+    const hipError_t e = launch_kind(pl.tail, p, int8, st);
     if (e != hipSuccess || pl.splits == 1) return e;
-    return launch_proj_finish(p.partial, p.k_splits, p.M_out - p.m_base, p.c, p.M, p.M_out, p.N, p.mode, p.s, p.xs, p.ws, p.int8, st,
+    return launch_proj_finish(p.partial, p.k_splits, p.M_out - p.m_base, p.c, p.M, p.M_out, p.N, p.mode, p.s, p.xs, p.ws, int8, st,
                               p.m_base);
 }
 
@@ -832,7 +831,6 @@ hipError_t launch_qkv_proj_pack(const void* x, const void* w_qkv, void* send, in
                                 const float* x_scales, const float* w_scales, bool int8, void* workspace, size_t workspace_bytes,
                                 hipStream_t st) {
     GemmParams p;
-    p.int8 = int8;
     p.w = static_cast<const unsigned char*>(w_qkv);
     p.x = static_cast<const unsigned char*>(x);
     p.c = static_cast<uint16_t*>(send);
@@ -845,14 +843,13 @@ hipError_t launch_qkv_proj_pack(const void* x, const void* w_qkv, void* send, in
     p.mode = 0;
     p.s = s;
     if (s.T == 0) return launch_pack(nullptr, send, s, st);  // only padding rows: the pack kernel writes the zeros
-    return run_gemm(p, workspace, workspace_bytes, st);
+    return run_gemm(p, int8, workspace, workspace_bytes, st);
 }
 
 hipError_t launch_unpack_o_proj(const void* recv, const void* w_o, void* out, int d_model, const XchgShape& s,
                                 const float* a_scales, const float* w_scales, bool int8, void* workspace, size_t workspace_bytes,
                                 hipStream_t st) {
     GemmParams p;
-    p.int8 = int8;
     p.w = static_cast<const unsigned char*>(w_o);
     p.x = static_cast<const unsigned char*>(recv);
     p.c = static_cast<uint16_t*>(out);
@@ -865,7 +862,7 @@ hipError_t launch_unpack_o_proj(const void* recv, const void* w_o, void* out, in
     p.mode = 1;
     p.s = s;
     if (s.T == 0) return hipSuccess;
-    return run_gemm(p, workspace, workspace_bytes, st);
+    return run_gemm(p, int8, workspace, workspace_bytes, st);
 }
 
 }  // namespace shiftattn

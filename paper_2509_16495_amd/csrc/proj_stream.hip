@@ -60,10 +60,9 @@ struct StreamParams {
     const unsigned char* __restrict__ w;   // [N][K] bf16 or FP8 E4M3 codes
     const unsigned char* __restrict__ x;   // token rows, see mode
     uint16_t* __restrict__ c;              // bf16 result
-    float* __restrict__ partial;           // kg > 1: [kg][rows][N] fp32
+    float* __restrict__ partial;           // kg > 1: [kg][rows][N] fp32 (of int8 codes: the bits of 32-bit integers)
     const float* __restrict__ xs;          // products of 8-bit codes: one scale per token row ...
     const float* __restrict__ ws;          // ... and one per output feature (nullptr: none)
-    bool int8;                             // the codes are int8: sums are 32-bit integers (in `partial` too)
     int M, M_out, N, K;                    // M token rows exist, rows M .. M_out - 1 of the result are zeros
     int mode;                              // 0: x dense [M][K], result into the send buffers; 1: x gathered from the
                                            // receive buffers (k = (p hq_l + j) 128 + e), result dense [M][N]
@@ -351,12 +350,12 @@ bool stream_built(StreamShape shape) {
     return false;
 }
 
-hipError_t launch_stream(const StreamParams& p, hipStream_t st) {
+hipError_t launch_stream(const StreamParams& p, bool int8, hipStream_t st) {
     const auto [ux, uw] = stream_shape(p.M_out, p.rows_per_block);
     const unsigned grid = (p.N + p.rows_per_block - 1) / p.rows_per_block * p.kg;
 #define SHIFTATTN_STREAM_LAUNCH(ux_, uw_)                                                                   \
     if (ux == ux_ && uw == uw_) {                                                                         \
-        if (p.int8) proj_stream_kernel<ux_, uw_, false, true><<<grid, 64 * stream_waves<ux_, uw_>(), stream_lds<ux_, uw_>(), st>>>(p); \
+        if (int8) proj_stream_kernel<ux_, uw_, false, true><<<grid, 64 * stream_waves<ux_, uw_>(), stream_lds<ux_, uw_>(), st>>>(p); \
         else if (p.xs) proj_stream_kernel<ux_, uw_, true><<<grid, 64 * stream_waves<ux_, uw_>(), stream_lds<ux_, uw_>(), st>>>(p);     \
         else proj_stream_kernel<ux_, uw_, false><<<grid, 64 * stream_waves<ux_, uw_>(), stream_lds<ux_, uw_>(), st>>>(p);         \
         return hipGetLastError();                                                                         \
@@ -369,6 +368,7 @@ hipError_t launch_stream(const StreamParams& p, hipStream_t st) {
 // Behind either kernel with k ranges: result[t][f .. f + 3] = sum over the ranges in their order, rounded once
 // (row_base: partial row r is row row_base + r of the result)
 constexpr int kFinishAhead = 4;
+template <bool kInt8>
 __global__ __launch_bounds__(256) void proj_stream_finish_kernel(StreamParams p, int t_rows, int row_base) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     const int quads = p.N / 4;
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(256) void proj_stream_finish_kernel(StreamParams p,
 #pragma unroll
             for (int x = 0; x < kFinishAhead; ++x) {
                 if (c + x < p.kg) {
-                    if (p.int8) {   // uniform
+                    if constexpr (kInt8) {
                         sum = add_int(sum, v[x]);
                     } else {
 #pragma unroll
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(256) void proj_stream_finish_kernel(StreamParams p,
                 }
             }
         }
-        if (p.int8) sum = from_int(sum);
+        if constexpr (kInt8) sum = from_int(sum);
         if (p.xs) {   // the scales of 8-bit operands, applied as the unsplit kernel applies them
             const float row_scale = p.xs[t];
             const f32x4 col_scale = *reinterpret_cast<const f32x4*>(p.ws + f);
@@ -415,7 +415,6 @@ __global__ __launch_bounds__(256) void proj_stream_finish_kernel(StreamParams p,
 hipError_t launch_proj_finish(const float* partial, int kg, int t_rows, void* c, int M, int M_out, int N, int mode,
                               const XchgShape& s, const float* x_scales, const float* w_scales, bool int8, hipStream_t st, int row_base) {
     StreamParams p = {};
-    p.int8 = int8;
     p.xs = x_scales;
     p.ws = w_scales;
     p.partial = const_cast<float*>(partial);
@@ -428,7 +427,9 @@ hipError_t launch_proj_finish(const float* partial, int kg, int t_rows, void* c,
     p.s = s;
     const int64_t items = static_cast<int64_t>(M_out - row_base) * (N / 4);
     if (items <= 0) return hipSuccess;
-    proj_stream_finish_kernel<<<static_cast<unsigned>((items + 255) / 256), 256, 0, st>>>(p, t_rows, row_base);
+    const unsigned grid = static_cast<unsigned>((items + 255) / 256);
+    if (int8) proj_stream_finish_kernel<true><<<grid, 256, 0, st>>>(p, t_rows, row_base);
+    else proj_stream_finish_kernel<false><<<grid, 256, 0, st>>>(p, t_rows, row_base);
     return hipGetLastError();
 }
 
@@ -544,21 +545,20 @@ size_t proj_workspace(int M_out, int N, int K, bool fp8) {
     return proj_gemm_workspace(M_out, N, K, fp8);
 }
 
-static hipError_t run_stream(StreamParams& p, int kg, void* workspace, hipStream_t st) {
+static hipError_t run_stream(StreamParams& p, bool int8, int kg, void* workspace, hipStream_t st) {
     p.kg = kg;
     p.kg_log2 = __builtin_ctz(kg);
     p.partial = static_cast<float*>(workspace);
     p.rows_per_block = stream_rows(p.N, kg);
-    const hipError_t e = launch_stream(p, st);
+    const hipError_t e = launch_stream(p, int8, st);
     if (e != hipSuccess || kg == 1) return e;
-    return launch_proj_finish(p.partial, kg, p.M_out, p.c, p.M, p.M_out, p.N, p.mode, p.s, p.xs, p.ws, p.int8, st, 0);
+    return launch_proj_finish(p.partial, kg, p.M_out, p.c, p.M, p.M_out, p.N, p.mode, p.s, p.xs, p.ws, int8, st, 0);
 }
 
 // kg: k ranges, see proj_stream_ranges(); x_scales / w_scales: nullptr for bf16 operands, the row scales of FP8 E4M3 or int8 codes otherwise
 hipError_t launch_qkv_proj_stream(const void* x, const void* w_qkv, void* send, int d_model, const XchgShape& s,
                                   const float* x_scales, const float* w_scales, bool int8, int kg, void* workspace, hipStream_t st) {
     StreamParams p = {};
-    p.int8 = int8;
     p.w = static_cast<const unsigned char*>(w_qkv);
     p.x = static_cast<const unsigned char*>(x);
     p.c = static_cast<uint16_t*>(send);
@@ -570,13 +570,12 @@ hipError_t launch_qkv_proj_stream(const void* x, const void* w_qkv, void* send, 
     p.K = d_model;
     p.mode = 0;
     p.s = s;
-    return run_stream(p, kg, workspace, st);
+    return run_stream(p, int8, kg, workspace, st);
 }
 
 hipError_t launch_o_proj_stream(const void* recv, const void* w_o, void* out, int d_model, const XchgShape& s,
                                 const float* a_scales, const float* w_scales, bool int8, int kg, void* workspace, hipStream_t st) {
     StreamParams p = {};
-    p.int8 = int8;
     p.w = static_cast<const unsigned char*>(w_o);
     p.x = static_cast<const unsigned char*>(recv);
     p.c = static_cast<uint16_t*>(out);
@@ -588,7 +587,7 @@ hipError_t launch_o_proj_stream(const void* recv, const void* w_o, void* out, in
     p.K = s.h * kHeadDim;
     p.mode = 1;
     p.s = s;
-    return run_stream(p, kg, workspace, st);
+    return run_stream(p, int8, kg, workspace, st);
 }
 
 }  // namespace shiftattn
