@@ -210,7 +210,7 @@ hipError_t launch_attn_scaled(const void* q, const void* cache, const int32_t* b
         const int groups = (G + HG - 1) / HG;
         const int64_t wgs = static_cast<int64_t>(rows) * a.hkv_l * groups;
         if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;
-        const int chunks = (max_seq_len + kChunk - 1) / kChunk;
+        const int chunks = max_seq_len / kChunk + (max_seq_len % kChunk != 0);
         int waves = wgs <= 256 ? 16 : wgs <= 1024 ? 8 : 4;
         while (waves > 1 && waves >= 2 * chunks) waves /= 2;   // (none without a chunk)
         attn_scaled_rows_kernel<Elem, HG, decltype(dv)::value><<<static_cast<unsigned>(wgs), 64 * waves, 0, st>>>(

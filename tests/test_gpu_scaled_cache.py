@@ -333,6 +333,27 @@ def test_blocks_whose_offsets_pass_32_bits(B):
     _check(out[:1], [w[-1:] for w in want], "bf16", D, 45)
 
 
+@pytest.mark.parametrize("dtype,D,hq,hkv", [("bf16", 128, 8, 1), ("f32", 64, 4, 1)])
+def test_the_longest_max_seq_len(B, dtype, D, hq, hkv):
+    """An upper bound of 2^31 - 1 tokens for contexts that are short."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(17))
+    cache, table, slots, k, v = _batch(rng, [(3, 700)], hkv, D, dtype)
+    gpu = OnGpu(cache)
+    cache.append(k, v, slots)
+    wide = torch.zeros((1, 2 ** 27), dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = _dev(table)
+    q, longest = _rows(rng, 3, hq, D, dtype), 2 ** 31 - 1
+    out, lens = torch.empty((3, hq, D), dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda"), _dev(np.array([700], np.int32))
+    B.prefill(_dev(q, dtype), gpu.codes, wide, _dev(np.array([0, 3], np.int32)), lens, 3, longest, out, D ** -0.5, k_new=_dev(k, dtype), v_new=_dev(v, dtype),
+              slot_mapping=_dev(slots), kv_scales=gpu.scales)
+    gpu.same(cache)
+    want = _want(cache, table, [(3, 700)], q)
+    _check(out, want, dtype, D, 700)
+    B.decode(_dev(q[-1:], dtype), gpu.codes, wide, lens, longest, out[:1], D ** -0.5, kv_scales=gpu.scales)
+    _check(out[:1], [w[-1:] for w in want], dtype, D, 700)
+
+
 @pytest.mark.parametrize("option,value", [("OPT_GENERIC_ONLY", 1), ("OPT_PREFILL_TILE", 128), ("OPT_PREFILL_TILE", 256), ("OPT_PREFILL_SPLITS", 3)])
 def test_kernels_chosen_by_option(B, option, value):
     """The general kernel on the shapes of the tuned ones, the wide prefill kernels, more key ranges."""
