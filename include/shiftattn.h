@@ -281,9 +281,11 @@ int shiftattn_kv_write(const void *k_new, const void *v_new, const int64_t *slot
  * block_table (device, in)  : int32 [num_seqs][max_blocks_per_seq]
  * cu_seqlens_q (device, in) : int32 [num_seqs + 1], cu_seqlens_q[0] = 0, non-decreasing
  * seq_lens (device, in)     : int32 [num_seqs], seq_lens[s] >= q_len_s
- * total_q, max_q_len, max_seq_len (host): total_q = cu_seqlens_q[num_seqs]; upper bounds on
- *                             q_len_s and seq_lens[s] (they size the launch; exceeding them
- *                             silently drops work)
+ * total_q, max_q_len, max_seq_len (host): rows of q and out, at least cu_seqlens_q[num_seqs]; upper bounds
+ *                             on q_len_s and seq_lens[s] (they size the launch; exceeding them
+ *                             silently drops work).  Rows from cu_seqlens_q[num_seqs] on stand for no
+ *                             token (a chunk that shiftattn_tables_append refused): they are not
+ *                             attended, their rows of out stay as they were, and their slots must be negative
  * out (device, out)         : [total_q][hq_l][D], row stride a->out_stride
  * workspace (device)        : shiftattn_prefill_workspace_bytes(...) bytes, 16-byte aligned; may be
  *                             NULL when that is 0.  Contents are scratch.  Less is refused only
@@ -339,7 +341,8 @@ int shiftattn_decode_static(const void *q, const void *k_new, const void *v_new,
  * batch.  Sequences 0 .. num_prefill_seqs-1 carry the chunks (any q_len, described by cu_seqlens_q
  * [num_prefill_seqs + 1]); the num_decode_seqs sequences after them carry one new token each.
  * Row order of q, out, k_new, v_new, slot_mapping: the total_prefill_q rows of the chunks, then one
- * row per decode sequence.  block_table and seq_lens cover all sequences in that order.
+ * row per decode sequence.  block_table and seq_lens cover all sequences in that order.  Rows of the chunks from
+ * cu_seqlens_q[num_prefill_seqs] on stand for no token, as in shiftattn_prefill; the decode rows start at total_prefill_q all the same.
  * The K/V of all rows is written once, then both kinds of rows run in one launch where that is expected to be faster and
  * the workspace holds the partial results of both (the size asked for does), else one after the other; the result is that of shiftattn_prefill on the first
  * part followed by shiftattn_decode on the second, up to the order in which partial sums are added and the references against
@@ -400,7 +403,8 @@ typedef struct shiftattn_tables {
  *   slot_mapping (device, out)  : int64 [rows]; row cu_seqlens_q[s] + i is token i of chunk s, row total_prefill_q + j the token
  *                                 of the j-th decode sequence; -1 in every other row
  *   taken (device, out)         : int32 [num_seqs], the new tokens for which there was room: new_lens[s] or 0
- *   seq_lens grows by taken; the caller's decode sequences without a token keep their length and get slot -1.
+ *   seq_lens grows by taken; the caller's decode sequences without a token keep their length and get slot -1.  The attention calls take
+ *   all of this as it is, with the same total_prefill_q, whatever was refused.
  *   A sequence is refused (taken 0, nothing of it changes) if its tokens exceed its row of block_table or 2^31 - 1, a decode sequence that
  *   brings more than one, a chunk if the rows of the chunks up to and with it (those refused for the first reason apart) exceed
  *   total_prefill_q, and any that needs blocks if the blocks needed up to and with it (of those not refused so far) exceed

@@ -7,6 +7,7 @@
 // the MFMA kernels do not take (fp32 decode rows, fp32 and bf16 at other head_dims, FP8 caches of either) and is not tuned
 // for speed.
 #include "internal.h"
+#include "query_rows.h"
 
 namespace shiftattn {
 
@@ -58,20 +59,8 @@ __global__ __launch_bounds__(kWaves * 64) void attn_rows_kernel(
     const int j = static_cast<int>(row % a.hq_l);
     const int g = j / (a.hq_l / a.hkv_l);
 
-    int s, pos;
-    if (cu_seqlens_q == nullptr) {
-        s = tok;
-        pos = seq_lens[s] - 1;
-    } else {
-        int lo = 0, hi = num_seqs;  // last s with cu[s] <= tok
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (cu_seqlens_q[mid] <= tok) lo = mid; else hi = mid;
-        }
-        s = lo;
-        const int q_len = cu_seqlens_q[s + 1] - cu_seqlens_q[s];
-        pos = seq_lens[s] - q_len + (tok - cu_seqlens_q[s]);
-    }
+    const auto [s, pos] = query_row(cu_seqlens_q, seq_lens, num_seqs, tok);
+    if (s < 0) return;  // uniform over the wavefront
     const int32_t* table = block_table + static_cast<size_t>(s) * a.max_blocks;
     const int D = a.D;
 
@@ -151,6 +140,7 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const float* _
                                                                   const float* __restrict__ ml_part, int n_rows,
                                                                   int hq_l, int D, int n_parts, int mode,
                                                                   const int32_t* __restrict__ seq_lens, int chunk,
+                                                                  const int32_t* __restrict__ tokens,
                                                                   Elem* __restrict__ out, int64_t out_stride,
                                                                   float out_scale) {
     __shared__ float w_s[kCombineMaxParts];
@@ -158,6 +148,7 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const float* _
     __shared__ float red_s[kCombineThreads / 64];
     const int row = blockIdx.x;  // token * hq_l + head
     const int tok = row / hq_l, head = row % hq_l;
+    if (tokens && tok >= *tokens) return;  // uniform: no token, no partials
     int np = n_parts;
     if (mode == 1) np = (seq_lens[tok] + chunk - 1) / chunk;
     // partial row of part c: row0 + c * part_rows
@@ -217,10 +208,13 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const float* _
 // What bounds it is the chain of loads a row waits for, not the bytes: lane c of a row fetches the (max, sum) pair of part
 // c and the weights go round by cross-lane reads, so a row waits for memory once (twice beyond eight parts), where a walk
 // over the pairs waited once per part: 2048 tokens x 8 heads, 4 parts 10.4 -> 9.1 us; 1000 x 8, 8 parts 9.2 -> 8.0.
+// Rows from *tokens on stand for no token and have no partials: nothing is stored for them.
 constexpr int kSplitRowsPerWg = 8;
 __device__ inline void combine_splits_body(const float* __restrict__ o_part, const float* __restrict__ ml_part, int64_t rows, int hq_l,
-                                           int n_parts, uint16_t* __restrict__ out, int64_t out_stride, float out_scale, int wg) {
+                                           int n_parts, const int32_t* __restrict__ tokens, uint16_t* __restrict__ out, int64_t out_stride,
+                                           float out_scale, int wg) {
     constexpr int D = 128;
+    const int64_t there = static_cast<int64_t>(*tokens) * hq_l;
     const int64_t row_raw = static_cast<int64_t>(wg) * kSplitRowsPerWg + (threadIdx.x >> 5);
     const int64_t row = row_raw < rows ? row_raw : rows - 1;  // (every lane stays for the cross-lane reads)
     const int q4 = threadIdx.x & 31;
@@ -268,7 +262,7 @@ __device__ inline void combine_splits_body(const float* __restrict__ o_part, con
                 if (c + x < c_end) add_part(c + x, v[x]);
         }
     }
-    if (row_raw >= rows) return;
+    if (row_raw >= rows || row >= there) return;
     const float inv = l_star > 0.f ? out_scale / l_star : 0.f;
     const int64_t tok = row / hq_l;
     const int head = static_cast<int>(row - tok * hq_l);
@@ -284,9 +278,10 @@ __device__ inline void combine_splits_body(const float* __restrict__ o_part, con
 __global__ __launch_bounds__(32 * kSplitRowsPerWg) void combine_splits_kernel(const float* __restrict__ o_part,
                                                                               const float* __restrict__ ml_part,
                                                                               int64_t rows, int hq_l, int n_parts,
+                                                                              const int32_t* __restrict__ tokens,
                                                                               uint16_t* __restrict__ out, int64_t out_stride,
                                                                               float out_scale) {
-    combine_splits_body(o_part, ml_part, rows, hq_l, n_parts, out, out_stride, out_scale, blockIdx.x);
+    combine_splits_body(o_part, ml_part, rows, hq_l, n_parts, tokens, out, out_stride, out_scale, blockIdx.x);
 }
 
 // Merge for the flat decode kernel (bf16 output, D = 128; out_scale = v_scale of an FP8 cache, else 1): one workgroup per
@@ -395,24 +390,24 @@ __global__ __launch_bounds__(32 * kGroups) void combine_flat_kernel(
 
 // The two merges of a launch that carried chunks and decode rows: the first dec_rows workgroups take a decode row each.
 __global__ __launch_bounds__(32 * kSplitRowsPerWg) void combine_both_kernel(
-    const float* __restrict__ o_part_p, const float* __restrict__ ml_part_p, int64_t rows_p, int n_parts, uint16_t* __restrict__ out_p,
-    const float* __restrict__ o_part_d, const float* __restrict__ ml_part_d, const int2* __restrict__ plan, int dec_rows,
+    const float* __restrict__ o_part_p, const float* __restrict__ ml_part_p, int64_t rows_p, int n_parts,
+    const int32_t* __restrict__ tokens_p, uint16_t* __restrict__ out_p, const float* __restrict__ o_part_d, const float* __restrict__ ml_part_d, const int2* __restrict__ plan, int dec_rows,
     uint16_t* __restrict__ out_d, int hq_l, int G, int64_t out_stride, float out_scale) {
     const int wg = blockIdx.x;
     if (wg < dec_rows) combine_flat_body<kSplitRowsPerWg>(o_part_d, ml_part_d, plan, hq_l, G, out_d, out_stride, out_scale, wg);
-    else combine_splits_body(o_part_p, ml_part_p, rows_p, hq_l, n_parts, out_p, out_stride, out_scale, wg - dec_rows);
+    else combine_splits_body(o_part_p, ml_part_p, rows_p, hq_l, n_parts, tokens_p, out_p, out_stride, out_scale, wg - dec_rows);
 }
 
 }  // namespace
 
-hipError_t launch_combine_both(const float* o_part_p, const float* ml_part_p, int n_rows_p, int n_parts, void* out_p, const float* o_part_d,
-                               const float* ml_part_d, const int2* plan, int num_dec, void* out_d, const AttnShape& a, hipStream_t st) {
+hipError_t launch_combine_both(const float* o_part_p, const float* ml_part_p, int n_rows_p, int n_parts, const int32_t* tokens_p, void* out_p,
+                               const float* o_part_d, const float* ml_part_d, const int2* plan, int num_dec, void* out_d, const AttnShape& a, hipStream_t st) {
     const int G = a.hq_l / a.hkv_l;
     if (n_parts == 1) return launch_combine_flat(o_part_d, ml_part_d, plan, num_dec, a.hq_l, G, out_d, a.out_stride, a.v_scale, st);
     const int64_t rows_p = static_cast<int64_t>(n_rows_p) * a.hq_l, rows_d = static_cast<int64_t>(num_dec) * a.hq_l;
     const unsigned grid = static_cast<unsigned>(rows_d + (rows_p + kSplitRowsPerWg - 1) / kSplitRowsPerWg);
-    combine_both_kernel<<<grid, 32 * kSplitRowsPerWg, 0, st>>>(o_part_p, ml_part_p, rows_p, n_parts, static_cast<uint16_t*>(out_p), o_part_d,
-                                                             ml_part_d, plan, static_cast<int>(rows_d), static_cast<uint16_t*>(out_d),
+    combine_both_kernel<<<grid, 32 * kSplitRowsPerWg, 0, st>>>(o_part_p, ml_part_p, rows_p, n_parts, tokens_p, static_cast<uint16_t*>(out_p),
+                                                             o_part_d, ml_part_d, plan, static_cast<int>(rows_d), static_cast<uint16_t*>(out_d),
                                                              a.hq_l, G, a.out_stride, a.v_scale);
     return hipGetLastError();
 }
@@ -459,22 +454,22 @@ hipError_t launch_attn_generic(const void* q, const void* cache, const int32_t* 
 }
 
 hipError_t launch_combine(const float* o_part, const float* ml_part, int n_rows, int hq_l, int D, int n_parts,
-                          int mode, const int32_t* seq_lens, int chunk, void* out, int64_t out_stride, int elem,
-                          float out_scale, hipStream_t st) {
+                          int mode, const int32_t* seq_lens, int chunk, const int32_t* tokens, void* out, int64_t out_stride,
+                          int elem, float out_scale, hipStream_t st) {
     const int64_t rows = static_cast<int64_t>(n_rows) * hq_l;
     if (rows == 0) return hipSuccess;
-    if (elem == 2 && D == 128 && mode == 0 && n_parts <= kCombineMaxParts && (out_stride % 4) == 0) {
+    if (elem == 2 && D == 128 && mode == 0 && tokens && n_parts <= kCombineMaxParts && (out_stride % 4) == 0) {
         combine_splits_kernel<<<static_cast<unsigned>((rows + kSplitRowsPerWg - 1) / kSplitRowsPerWg), 32 * kSplitRowsPerWg, 0, st>>>(
-            o_part, ml_part, rows, hq_l, n_parts, static_cast<uint16_t*>(out), out_stride, out_scale);
+            o_part, ml_part, rows, hq_l, n_parts, tokens, static_cast<uint16_t*>(out), out_stride, out_scale);
         return hipGetLastError();
     }
     if (elem == 2)
         combine_kernel<uint16_t><<<static_cast<unsigned>(rows), 128, 0, st>>>(
-            o_part, ml_part, n_rows, hq_l, D, n_parts, mode, seq_lens, chunk, static_cast<uint16_t*>(out), out_stride,
+            o_part, ml_part, n_rows, hq_l, D, n_parts, mode, seq_lens, chunk, tokens, static_cast<uint16_t*>(out), out_stride,
             out_scale);
     else
         combine_kernel<float><<<static_cast<unsigned>(rows), 128, 0, st>>>(o_part, ml_part, n_rows, hq_l, D, n_parts,
-                                                                          mode, seq_lens, chunk,
+                                                                          mode, seq_lens, chunk, tokens,
                                                                           static_cast<float*>(out), out_stride, out_scale);
     return hipGetLastError();
 }

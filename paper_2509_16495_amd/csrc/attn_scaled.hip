@@ -13,6 +13,7 @@
 // workgroups there are, 16 / 8 / 4: 64 workgroups 14.2 / 14.7 / 20.0 us, 400 19.9 / 14.7 / 16.7, 1200 53 / 40 / 35.  One wavefront per (row,
 // head) that walked the whole context alone took 97 us for the 16 rows.
 #include "block_scale.h"
+#include "query_rows.h"
 
 #include <type_traits>
 
@@ -67,20 +68,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void attn_scaled_rows_kernel(const 
     const int tok = blockIdx.x / per_row, rest = blockIdx.x - tok * per_row, g = rest / head_groups, hg = rest - g * head_groups;
     const int G = a.hq_l / a.hkv_l, D = a.D, h0 = g * G + hg * HG, heads = min(HG, G - hg * HG);
 
-    int s, pos;
-    if (cu_seqlens_q == nullptr) {
-        s = tok;
-        pos = seq_lens[s] - 1;
-    } else {
-        int lo = 0, hi = num_seqs;  // last s with cu[s] <= tok
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (cu_seqlens_q[mid] <= tok) lo = mid; else hi = mid;
-        }
-        s = lo;
-        const int q_len = cu_seqlens_q[s + 1] - cu_seqlens_q[s];
-        pos = seq_lens[s] - q_len + (tok - cu_seqlens_q[s]);
-    }
+    const auto [s, pos] = query_row(cu_seqlens_q, seq_lens, num_seqs, tok);
+    if (s < 0) return;   // uniform
     const int32_t* table = block_table + static_cast<size_t>(s) * a.max_blocks;
     const Elem* q_row = q + static_cast<size_t>(tok) * a.q_stride + static_cast<size_t>(h0) * D;
     for (int i = threadIdx.x; i < HG * D; i += blockDim.x) q_s[i] = i < heads * D ? to_float(q_row[i]) : 0.f;

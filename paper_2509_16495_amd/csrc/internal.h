@@ -69,14 +69,15 @@ hipError_t launch_attn_generic(const void* q, const void* cache, const int32_t* 
 // Merge of split-context partial results (shared by decode and split prefill).
 // Partials: o[part][row][D] fp32 un-normalised, ml[part][row][2] = (reference logit * log2e*scale, sum).
 // mode 0: every row has n_parts parts.  mode 1 (decode): row = (sequence, head), the number of
-// parts of a row is ceil(seq_lens[sequence] / chunk).
+// parts of a row is ceil(seq_lens[sequence] / chunk).  tokens (device, mode 0): how many of the n_rows stand for a token; nothing is
+// stored for the others.
 hipError_t launch_combine(const float* o_part, const float* ml_part, int n_rows, int hq_l, int D,
-                          int n_parts, int mode, const int32_t* seq_lens, int chunk, void* out,
+                          int n_parts, int mode, const int32_t* seq_lens, int chunk, const int32_t* tokens, void* out,
                           int64_t out_stride, int elem, float out_scale, hipStream_t st);
 
-// both merges of launch_prefill_and_decode in one launch (n_parts 1: the prefill part has none)
-hipError_t launch_combine_both(const float* o_part_p, const float* ml_part_p, int n_rows_p, int n_parts, void* out_p, const float* o_part_d,
-                               const float* ml_part_d, const int2* plan, int num_dec, void* out_d, const AttnShape& a, hipStream_t st);
+// both merges of launch_prefill_and_decode in one launch (n_parts 1: the prefill part has none); tokens_p as above
+hipError_t launch_combine_both(const float* o_part_p, const float* ml_part_p, int n_rows_p, int n_parts, const int32_t* tokens_p, void* out_p,
+                               const float* o_part_d, const float* ml_part_d, const int2* plan, int num_dec, void* out_d, const AttnShape& a, hipStream_t st);
 
 // Merge for the flat decode kernel (bf16, D = 128): see combine_flat_kernel.
 hipError_t launch_combine_flat(const float* o_part, const float* ml_part, const int2* plan, int num_seqs, int hq_l, int G,

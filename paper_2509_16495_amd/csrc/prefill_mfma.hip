@@ -1063,7 +1063,7 @@ hipError_t launch_prefill_mfma(const void* q, const void* cache, const int32_t* 
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (pl.n_splits > 1)
-        return launch_combine(p.o_part, p.ml_part, total_q, a.hq_l, kD, pl.n_splits, 0, nullptr, 0, out, a.out_stride,
+        return launch_combine(p.o_part, p.ml_part, total_q, a.hq_l, kD, pl.n_splits, 0, nullptr, 0, cu_seqlens_q + num_seqs, out, a.out_stride,
                               a.elem, a.v_scale, st);
     return hipSuccess;
 }
@@ -1258,7 +1258,7 @@ bool launch_prefill_and_decode(const void* q, void* cache, const int32_t* block_
         *err = hipGetLastError();
     }
     if (*err != hipSuccess) return true;
-    *err = launch_combine_both(o_part, ml_part, total_q, n_splits, out, d.o_part, d.ml_part, d.plan, num_dec,
+    *err = launch_combine_both(o_part, ml_part, total_q, n_splits, cu_seqlens_q + num_seqs, out, d.o_part, d.ml_part, d.plan, num_dec,
                                static_cast<uint16_t*>(out) + static_cast<size_t>(total_q) * a.out_stride, a, st);
     return true;
 }

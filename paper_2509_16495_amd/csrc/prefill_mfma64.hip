@@ -1179,7 +1179,7 @@ hipError_t launch_prefill_mfma64(const void* q, const void* cache, const int32_t
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (pl.n_splits > 1)
-        return launch_combine(p.o_part, p.ml_part, total_q, a.hq_l, kD, pl.n_splits, 0, nullptr, 0, out, a.out_stride, a.elem,
+        return launch_combine(p.o_part, p.ml_part, total_q, a.hq_l, kD, pl.n_splits, 0, nullptr, 0, cu_seqlens_q + num_seqs, out, a.out_stride, a.elem,
                               out_scale, st);
     return hipSuccess;
 }
