@@ -86,9 +86,10 @@ __global__ __launch_bounds__(kWaves * 64) void attn_rows_kernel(
             }
             logit = dot * (a.scale * a.k_scale);
         }
-        const float m_new = fmaxf(m_run, wave_max(logit));  // finite: key t0 is always visible
-        const float p = (t <= pos) ? expf(logit - m_new) : 0.f;
-        const float alpha = expf(m_run - m_new);             // exp(-inf) = 0 on the first chunk
+        const float m_new = fmaxf(m_run, wave_max(logit));
+        const float m_ref = m_new == -INFINITY ? 0.f : m_new;  // (no logit above minus infinity yet)
+        const float p = (t <= pos) ? expf(logit - m_ref) : 0.f;
+        const float alpha = expf(m_run - m_ref);             // exp(-inf) = 0 on the first chunk
         l_run = l_run * alpha + wave_sum(p);
         m_run = m_new;
         p_s[wave][lane] = p;

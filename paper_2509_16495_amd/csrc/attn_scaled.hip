@@ -115,8 +115,9 @@ __global__ __launch_bounds__(64 * kMaxWaves) void attn_scaled_rows_kernel(const 
 #pragma unroll
         for (int h = 0; h < HG; ++h) {
             const float m_new = fmaxf(m_run[h], wave_max(logit[h]));
-            const float p = sees ? expf(logit[h] - m_new) : 0.f;
-            const float alpha = expf(m_run[h] - m_new);   // exp(-inf) = 0 on the first chunk
+            const float m_ref = m_new == -INFINITY ? 0.f : m_new;   // (no logit above minus infinity yet)
+            const float p = sees ? expf(logit[h] - m_ref) : 0.f;
+            const float alpha = expf(m_run[h] - m_ref);   // exp(-inf) = 0 on the first chunk
             l_lane[h] = fmaf(l_lane[h], alpha, p);
             m_run[h] = m_new;
             p_w[h * kChunk + lane] = p;

@@ -317,6 +317,7 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
     float m_run, l_run;          // reference of the sums, sum of P
     float m_max = -INFINITY;     // kGroupRef: largest logit so far
     const float ref_drop = 8.f / c;
+    const float ref_least = -3e38f / fmaxf(c, 1.f);   // the reference stays finite (times c too) where all logits are minus infinity
     auto reset = [&]() {
 #pragma unroll
         for (int mt = 0; mt < 8; ++mt) o[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -561,9 +562,9 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
         float m_new;
         if constexpr (kGroupRef) {
             m_max = fmaxf(m_max, mx);
-            m_new = fmaxf(m_max - ref_drop, mx);
+            m_new = fmaxf(fmaxf(m_max - ref_drop, mx), ref_least);
         } else {
-            m_new = fmaxf(m_run, mx);
+            m_new = fmaxf(fmaxf(m_run, mx), ref_least);
         }
         const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c);
         const float mc = m_new * c;
