@@ -5,7 +5,8 @@
 // them; its wavefronts take the context in chunks of 64 tokens in turn, each with a running maximum and sum of its own, and
 // meet in LDS at the end, in wavefront order.  Within a chunk lanes are tokens for q.k (a lane walks its token's row of codes, q comes from
 // LDS for all lanes at once) and head-dim rows for p.V (a lane's 16 bytes are 16 tokens of its row, the probabilities come from LDS).
-// The scales are powers of two: multiplying the sums instead of the elements is exact.  All sums are float32.
+// The scales are applied by the widening instruction, which costs nothing and keeps the products in range: a query times a code may
+// overflow where the query times the element does not.  All sums are float32.
 // Bound: the LDS reads that hand q and the probabilities round (16 bytes for four multiply-adds of a wavefront; a compute unit's wavefronts share
 // one LDS), and for few rows the walk over a context.  So a workgroup takes one head, and four only where rows fill the chip many times
 // over and fetching and widening K and V four times weighs more: 2000 rows x 8 heads of 256 734 -> 474 us, but 16 decode rows x 4 heads
@@ -46,10 +47,10 @@ __device__ inline float wave_sum(float v) {
     return v;
 }
 
-// values of four codes
-__device__ inline f32x4 widen4(uint32_t codes) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(codes), false);
-    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(codes), true);
+// values of four codes times their block's scale
+__device__ inline f32x4 widen4(uint32_t codes, float scale) {
+    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(static_cast<int>(codes), scale, false);
+    const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(static_cast<int>(codes), scale, true);
     return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void attn_scaled_rows_kernel(const 
         if (sees) {
             const size_t at = static_cast<size_t>(table[t / kBlockSize]) * a.hkv_l + g;
             const uint8_t* k_row = cache + at * 2 * kBlockSize * D + static_cast<size_t>(t % kBlockSize) * D;
-            const float scale = scales[at * 2] * a.scale;
+            const float k_scale = scales[at * 2];
             f32x4 acc[HG];   // four sums a head: shorter chains, smaller rounding errors
 #pragma unroll
             for (int h = 0; h < HG; ++h) acc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void attn_scaled_rows_kernel(const 
                 const u32x4 codes = *reinterpret_cast<const u32x4*>(k_row + d);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const f32x4 k4 = widen4(codes[w]);
+                    const f32x4 k4 = widen4(codes[w], k_scale);
 #pragma unroll
                     for (int h = 0; h < HG; ++h) {
                         const f32x4 q4 = *reinterpret_cast<const f32x4*>(q_s + h * D + d + 4 * w);
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void attn_scaled_rows_kernel(const 
                 }
             }
 #pragma unroll
-            for (int h = 0; h < HG; ++h) logit[h] = ((acc[h][0] + acc[h][1]) + (acc[h][2] + acc[h][3])) * scale;
+            for (int h = 0; h < HG; ++h) logit[h] = ((acc[h][0] + acc[h][1]) + (acc[h][2] + acc[h][3])) * a.scale;
         }
 #pragma unroll
         for (int h = 0; h < HG; ++h) {
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void attn_scaled_rows_kernel(const 
                 }
                 f32x4 v4[4];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) v4[w] = widen4(codes[w]);
+                for (int w = 0; w < 4; ++w) v4[w] = widen4(codes[w], v_scale);
 #pragma unroll
                 for (int h = 0; h < HG; ++h) {
                     f32x4 part = {0.f, 0.f, 0.f, 0.f};
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void attn_scaled_rows_kernel(const 
 #pragma unroll
                         for (int e = 0; e < 4; ++e) part[e] = fmaf(p4[e], v4[w][e], part[e]);
                     }
-                    o[h][x] = fmaf((part[0] + part[1]) + (part[2] + part[3]), v_scale, o[h][x]);
+                    o[h][x] += (part[0] + part[1]) + (part[2] + part[3]);
                 }
             }
         }

@@ -1,6 +1,7 @@
-"""Attention where float32 ends: keys whose logits are minus infinity.
+"""Attention where float32 ends: keys whose logits are minus infinity, and queries and keys whose products leave the range of float32 unless
+the keys' scale is in them.
 
-Element 0 of q is 3e38, that of some keys -4 and that of the others 0: the former's logits are minus infinity in float32
+In the first tests element 0 of q is 3e38, that of some keys -4 and that of the others 0: the former's logits are minus infinity in float32
 (beyond -1e38 in 64 bits: a weight of 0 there too), the latter's are those of the remaining elements, exactly.  So the result is the softmax over
 the others, and its error is bounded as that of a batch without element 0."""
 import numpy as np
@@ -102,3 +103,32 @@ def test_decode_rows_beside_chunks_over_keys_far_below(B, fmt):
     B.mixed(q, b.codes, table, _dev(np.array([0, 300], np.int32)), lens, 1, 300, 2000, 2000, out, 128 ** -0.5, **b.kw)
     for i in (0, 31, 59):
         b.check(out[300 + i:301 + i])
+
+
+@pytest.mark.parametrize("dtype,D", [("f32", 64), ("f32", 128), ("bf16", 64), ("bf16", 256)])
+@pytest.mark.parametrize("q_size,k_size", [(2.0 ** 122, 2.0 ** -95), (2.0 ** -123, 2.0 ** 116)])
+def test_products_are_of_what_the_cache_stands_for(B, dtype, D, q_size, k_size):
+    """q times a code would pass 2^128 where the block's scale is small, and lie at the bottom of the range where it is large; q times the
+    key's value stays near 1."""
+    import torch
+    rng = np.random.Generator(np.random.PCG64(D))
+    length, rows, scale = 200, 5, 1.0 / (q_size * k_size) / D ** 0.5
+    t = np.arange(length)
+    cache = P.Cache(13, 1, D)
+    kv = _rows(rng, length, 1, 2 * D, dtype=dtype)
+    kv[..., :D] *= np.float32(k_size)
+    table = rng.permutation(13).astype(np.int32)[None]
+    cache.append(kv[..., :D], kv[..., D:], table[0, t // 16].astype(np.int64) * 16 + t % 16)
+    q = _rows(rng, rows, 4, D, dtype=dtype) * np.float32(q_size)
+    out = torch.empty((rows, 4, D), dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    codes, scales = _dev(cache.codes), _dev(cache.scales)
+    for call in ("prefill", "decode"):
+        if call == "prefill":
+            B.prefill(_dev(q, dtype), codes, _dev(table), _dev(np.array([0, rows], np.int32)), _dev(np.array([length], np.int32)), rows, length, out, scale, kv_scales=scales)
+            got, want = out, P.attend(q, cache, table[0], length, scale)
+        else:
+            B.decode(_dev(q[-1:], dtype), codes, _dev(table), _dev(np.array([length], np.int32)), length, out[:1], scale, kv_scales=scales)
+            got, want = out[:1], P.attend(q[-1:], cache, table[0], length, scale)
+        got = got.float().cpu().numpy().astype(np.float64)
+        off = np.abs(got - want[0]) / P.bound(dtype, *want, D, length)
+        assert np.isfinite(got).all() and off.max() <= 1.0, (call, off.max())
