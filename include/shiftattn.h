@@ -411,7 +411,7 @@ typedef struct shiftattn_tables {
  *   free_count.  Blocks leave the stack from the top in the order of sequences and tokens.
  * tables_truncate: sequence s keeps its first keep_lens[s] tokens (device, in, int32 [num_seqs]) and gives the blocks behind them
  *   back: 0 for a finished or preempted one, fewer than it has for rejected speculative tokens; negative, or not below
- *   seq_lens[s]: unchanged.  The blocks go back in the order that undoes an append (sequence 0's first block ends on top), so that
+ *   seq_lens[s], or a seq_lens[s] that exceeds its row of block_table: unchanged.  The blocks go back in the order that undoes an append (sequence 0's first block ends on top), so that
  *   a truncate to the lengths before an append restores the stack.  Entries of block_table are left as they are.
  * workspace (device, scratch): shiftattn_tables_workspace_bytes(num_seqs) bytes, 4-byte aligned (SIZE_MAX for a negative
  *   count).  Calls that share a workspace or the tables must not overlap. */

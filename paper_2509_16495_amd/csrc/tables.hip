@@ -54,6 +54,11 @@ __device__ inline uint32_t scan(uint32_t v, uint32_t& carry, uint32_t* wave_sum)
     return add_sat(v, front);
 }
 
+// tokens that a sequence's row of block_table can hold (lengths are int32)
+__device__ inline int64_t room_of(const shiftattn_tables& t) {
+    return min(static_cast<int64_t>(t.max_blocks_per_seq) * kBlockSize, static_cast<int64_t>(kMost));
+}
+
 __device__ inline int blocks_of(int tokens) { return tokens / kBlockSize + (tokens % kBlockSize != 0); }
 
 // last index in [0, n) with from[index] <= x, for from[0] <= x and a non-decreasing array
@@ -106,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void tables_append_kernel(shiftattn_table
     __shared__ uint32_t wave_sum[kThreads / 64];
     __shared__ int given_s;
     __shared__ Shared sh;
-    const int64_t room = min(static_cast<int64_t>(t.max_blocks_per_seq) * kBlockSize, static_cast<int64_t>(kMost));   // (lengths are int32)
+    const int64_t room = room_of(t);
     const int height = min(max(*t.free_count, 0), t.num_blocks);
     uint32_t asked_c = 0, need_c = 0, rows_c = 0;
     if (threadIdx.x == 0) given_s = 0;
@@ -206,13 +211,14 @@ template <bool kOne, int kThreads>
 __global__ __launch_bounds__(kThreads) void tables_truncate_kernel(shiftattn_tables t, const int32_t* keep_lens, int32_t* ws) {
     __shared__ uint32_t wave_sum[kThreads / 64];
     __shared__ Shared sh;
+    const int64_t room = room_of(t);
     const int height = min(max(*t.free_count, 0), t.num_blocks);
     uint32_t gone_c = 0;
     for (int base = 0; base < t.num_seqs; base += kThreads) {
         const int s = base + threadIdx.x;
         const bool there = s < t.num_seqs;
         const int had = there ? t.seq_lens[s] : 0, keep = there ? keep_lens[s] : -1;
-        const bool cut = keep >= 0 && keep < had;
+        const bool cut = keep >= 0 && keep < had && had <= room;   // (blocks behind the row are nobody's to give back)
         const uint32_t gone = cut ? blocks_of(had) - blocks_of(keep) : 0;
         const uint32_t all = scan<kThreads>(gone, gone_c, wave_sum);
         if (!there) continue;
