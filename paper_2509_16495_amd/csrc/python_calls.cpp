@@ -269,6 +269,7 @@ SHIFTATTN_CALL(prefill) {
         rows_of(q, out, k, v, slots, cache);
         const int32_t mq = whole(a[5]), ms = whole(a[6]);
         const at::Tensor* ws = workspace(a[12], a[0], own, [&] { return lib.prefill_bytes(cut(seqs), cut(q.size(0)), mq, ms, &d); });
+        if (scales) here({&cu, &lens, v, slots, ws});
         return [d, pq = ptr(q), pk = ptr(k), pv = ptr(v), ps = ptr(slots), pc = ptr(cache), pt = ptr(table), pu = ptr(cu), pl = ptr(lens), seqs = cut(seqs),
                 rows = cut(q.size(0)), mq, ms, po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream(), pb = static_cast<float*>(ptr(scales))] {
             if (d.kv_format == SHIFTATTN_KV_FP8_E4M3_BLOCKS)
@@ -296,6 +297,7 @@ PyObject* decode_call(PyObject* const* a, Py_ssize_t n, bool owned) {
         rows_of(q, out, k, v, slots, cache);
         const int32_t ms = whole(a[4]);
         const at::Tensor* ws = owned ? nullptr : workspace(a[10], a[0], own, [&] { return lib.decode_bytes(cut(q.size(0)), ms, &d); });
+        if (scales) here({&lens, v, slots, ws});
         return [d, pq = ptr(q), pk = ptr(k), pv = ptr(v), ps = ptr(slots), pc = ptr(cache), pt = ptr(table), pl = ptr(lens), seqs = cut(q.size(0)), ms,
                 po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream(), owned, pb = static_cast<float*>(ptr(scales))] {
             const auto* slot = static_cast<int64_t*>(ps);
@@ -326,6 +328,7 @@ SHIFTATTN_CALL(mixed) {
         rows_of(q, out, k, v, slots, cache);
         const int32_t mq = whole(a[6]), mp = whole(a[7]), md = whole(a[8]);
         const at::Tensor* ws = workspace(a[14], a[0], own, [&] { return lib.mixed_bytes(cut(chunks), cut(chunk_rows), mq, mp, cut(rows), md, &d); });
+        if (scales) here({&cu, &lens, v, slots, ws});
         return [d, pq = ptr(q), pk = ptr(k), pv = ptr(v), ps = ptr(slots), pc = ptr(cache), pt = ptr(table), pu = ptr(cu), pl = ptr(lens),
                 chunks = cut(chunks), chunk_rows = cut(chunk_rows), mq, mp, rows = cut(rows), md, po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream(),
                 pb = static_cast<float*>(ptr(scales))] {
@@ -415,6 +418,7 @@ SHIFTATTN_CALL(tables_append) {
         here({&fresh, &cu, &slots, &taken});
         const shiftattn_tables t = tables_of(lens, table, free, count);
         const at::Tensor* ws = workspace(a[10], a[3], own, [&] { return lib.tables_bytes(t.num_seqs); });
+        here({ws});
         return [t = placed(t, lens, table, free, count), pn = ptr(fresh), chunks, chunk_rows, rows = cut(slots.size(0)), pu = ptr(cu), ps = ptr(slots), pt = ptr(taken), pw = ptr(ws), nw = bytes(ws),
                 st = stream()] {
             return lib.tables_append(&t, static_cast<int32_t*>(pn), chunks, chunk_rows, rows, static_cast<int32_t*>(pu), static_cast<int64_t*>(ps),
@@ -433,6 +437,7 @@ SHIFTATTN_CALL(tables_truncate) {
         here({&keep});
         const shiftattn_tables t = tables_of(lens, table, free, count);
         const at::Tensor* ws = workspace(a[5], a[1], own, [&] { return lib.tables_bytes(t.num_seqs); });
+        here({ws});
         return [t = placed(t, lens, table, free, count), pk = ptr(keep), pw = ptr(ws), nw = bytes(ws), st = stream()] { return lib.tables_truncate(&t, static_cast<int32_t*>(pk), pw, nw, st); };
     });
 }
