@@ -59,14 +59,15 @@ template <typename Elem, int HG, int DV>
 __global__ __launch_bounds__(64 * kMaxWaves) void attn_scaled_rows_kernel(const Elem* __restrict__ q, const uint8_t* __restrict__ cache,
                                                                          const float* __restrict__ scales, const int32_t* __restrict__ block_table,
                                                                          const int32_t* __restrict__ cu_seqlens_q, const int32_t* __restrict__ seq_lens,
-                                                                         int num_seqs, int head_groups, Elem* __restrict__ out, AttnShape a) {
+                                                                         int num_seqs, int head_groups, int first_row, Elem* __restrict__ out, AttnShape a) {
     __shared__ __attribute__((aligned(16))) float q_s[HG * kMaxD];
     constexpr int kPerWave = HG > DV ? HG * kChunk : DV * 64;                       // a chunk's probabilities, then one head's sums
     __shared__ __attribute__((aligned(16))) float p_s[kMaxWaves * kPerWave];
     __shared__ float m_s[kMaxWaves][HG], l_s[kMaxWaves][HG];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int per_row = a.hkv_l * head_groups;
-    const int tok = blockIdx.x / per_row, rest = blockIdx.x - tok * per_row, g = rest / head_groups, hg = rest - g * head_groups;
+    const int row = blockIdx.x / per_row, rest = blockIdx.x - row * per_row, g = rest / head_groups, hg = rest - g * head_groups;
+    const int tok = first_row + row;
     const int G = a.hq_l / a.hkv_l, D = a.D, h0 = g * G + hg * HG, heads = min(HG, G - hg * HG);
 
     const auto [s, pos] = query_row(cu_seqlens_q, seq_lens, num_seqs, tok);
@@ -200,14 +201,20 @@ hipError_t launch_attn_scaled(const void* q, const void* cache, const int32_t* b
         constexpr int HG = decltype(hg)::value;
         const int groups = (G + HG - 1) / HG;
         const int64_t wgs = static_cast<int64_t>(rows) * a.hkv_l * groups;
-        if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;
         const int chunks = max_seq_len / kChunk + (max_seq_len % kChunk != 0);
         int waves = wgs <= 256 ? 16 : wgs <= 1024 ? 8 : 4;
         while (waves > 1 && waves >= 2 * chunks) waves /= 2;   // (none without a chunk)
-        attn_scaled_rows_kernel<Elem, HG, decltype(dv)::value><<<static_cast<unsigned>(wgs), 64 * waves, 0, st>>>(
-            static_cast<const Elem*>(q), static_cast<const uint8_t*>(cache), a.kv_scales, block_table, cu_seqlens_q, seq_lens, num_seqs, groups,
-            static_cast<Elem*>(out), a);
-        return hipGetLastError();
+        const int per_row = a.hkv_l * groups;
+        const int64_t piece = most_workgroups(64 * waves) / per_row;   // rows a launch
+        if (piece == 0) return hipErrorInvalidValue;
+        for (int64_t row = 0; row < rows; row += piece) {
+            const int n = static_cast<int>(rows - row < piece ? rows - row : piece);
+            attn_scaled_rows_kernel<Elem, HG, decltype(dv)::value><<<static_cast<unsigned>(n) * per_row, 64 * waves, 0, st>>>(
+                static_cast<const Elem*>(q), static_cast<const uint8_t*>(cache), a.kv_scales, block_table, cu_seqlens_q, seq_lens, num_seqs, groups,
+                static_cast<int>(row), static_cast<Elem*>(out), a);
+            if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        }
+        return hipSuccess;
     };
     auto by_heads = [&](auto elem, auto dv) {
         if (G > 1 && static_cast<int64_t>(rows) * a.hq_l >= 8192) return run(elem, std::integral_constant<int, 4>{}, dv);

@@ -13,6 +13,9 @@ constexpr int kBlockSize = 16;         // tokens per KV-cache block
 constexpr int kPrefillKvTile = 64;     // keys per prefill inner-loop step
 constexpr int kMaxParts = 1024;        // most partial results the merge kernel takes per output row
 
+// workgroups of so many threads that one launch can have: 2^32 threads and more are not refused, the rest is dropped
+constexpr int64_t most_workgroups(int threads) { return 0xFFFFFFFFll / threads; }
+
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));  // one 16-byte vector
 
 struct XchgShape {

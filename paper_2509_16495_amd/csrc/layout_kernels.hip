@@ -567,14 +567,24 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_int8_kernel(const uint
     else store_all([&](float v) -> uint32_t { return fabsf(v) < INFINITY ? nearest(v) : v != v ? 0u : v > 0.f ? 127u : static_cast<uint32_t>(-127); });
 }
 
+// a workgroup per row; rows beyond the threads of one launch in further ones
+template <class Kernel>
+static hipError_t quantize_in_pieces(Kernel kernel, const void* x, void* codes, float* scales, int rows, int cols, int seg_len, int64_t seg_stride,
+                                     int64_t row_stride, hipStream_t st) {
+    constexpr int64_t kPiece = most_workgroups(kThreads);
+    for (int64_t row = 0; row < rows; row += kPiece) {
+        kernel<<<static_cast<unsigned>(rows - row < kPiece ? rows - row : kPiece), kThreads, 0, st>>>(
+            static_cast<const uint16_t*>(x) + row * row_stride, static_cast<uint8_t*>(codes) + row * row_stride, scales + row, cols, seg_len,
+            seg_stride, row_stride);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 hipError_t launch_quantize_rows_int8(const void* x, void* codes, float* scales, int rows, int cols, int seg_len,
                                      int64_t seg_stride, int64_t row_stride, hipStream_t st) {
     if (rows == 0) return hipSuccess;
-    auto run = [&](auto kernel) {
-        kernel<<<static_cast<unsigned>(rows), kThreads, 0, st>>>(static_cast<const uint16_t*>(x), static_cast<uint8_t*>(codes), scales,
-                                                                 cols, seg_len, seg_stride, row_stride);
-        return hipGetLastError();
-    };
+    auto run = [&](auto kernel) { return quantize_in_pieces(kernel, x, codes, scales, rows, cols, seg_len, seg_stride, row_stride, st); };
     switch ((cols / 8 + kThreads - 1) / kThreads) {
         case 0: case 1: return run(quantize_rows_int8_kernel<1>);
         case 2: return run(quantize_rows_int8_kernel<2>);
@@ -588,11 +598,7 @@ hipError_t launch_quantize_rows_int8(const void* x, void* codes, float* scales, 
 hipError_t launch_quantize_rows_fp8(const void* x, void* codes, float* scales, int rows, int cols, int seg_len,
                                     int64_t seg_stride, int64_t row_stride, hipStream_t st) {
     if (rows == 0) return hipSuccess;
-    auto run = [&](auto kernel) {
-        kernel<<<static_cast<unsigned>(rows), kThreads, 0, st>>>(static_cast<const uint16_t*>(x), static_cast<uint8_t*>(codes), scales,
-                                                                 cols, seg_len, seg_stride, row_stride);
-        return hipGetLastError();
-    };
+    auto run = [&](auto kernel) { return quantize_in_pieces(kernel, x, codes, scales, rows, cols, seg_len, seg_stride, row_stride, st); };
     switch ((cols / 8 + kThreads - 1) / kThreads) {
         case 0: case 1: return run(quantize_rows_fp8_kernel<1>);
         case 2: return run(quantize_rows_fp8_kernel<2>);

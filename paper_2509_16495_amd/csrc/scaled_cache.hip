@@ -26,9 +26,9 @@ __device__ inline uint32_t wave_max_bits(uint32_t v) {
 template <typename Elem>
 __global__ __launch_bounds__(64 * kWavesPerWg) void kv_write_scaled_kernel(const Elem* __restrict__ k_new, const Elem* __restrict__ v_new,
                                                                            const int64_t* __restrict__ slots, int n_tokens, uint8_t* cache,
-                                                                           float* scales, int hkv_l, int D, int64_t kv_stride) {
+                                                                           float* scales, int hkv_l, int D, int64_t kv_stride, int64_t first) {
     const int lane = threadIdx.x & 63;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * kWavesPerWg + (threadIdx.x >> 6);
+    const int64_t id = first + static_cast<int64_t>(blockIdx.x) * kWavesPerWg + (threadIdx.x >> 6);
     if (id >= static_cast<int64_t>(n_tokens) * hkv_l) return;
     const int64_t i = id / hkv_l;
     const int g = static_cast<int>(id - i * hkv_l);
@@ -245,10 +245,11 @@ hipError_t launch_kv_write_scaled(const void* k_new, const void* v_new, const in
                                   const AttnShape& a, hipStream_t st) {
     const int64_t waves = static_cast<int64_t>(n_tokens) * a.hkv_l;
     if (waves == 0) return hipSuccess;
-    if (a.elem == 2 && (a.D == 128 || a.D == 64) && a.hkv_l <= 65535) {
-        const int window = static_cast<int64_t>(chunk_rows) * a.hkv_l <= 4096 ? 1 : 8;
-        const int64_t windows = (static_cast<int64_t>(chunk_rows) + window - 1) / window + n_tokens - chunk_rows;
-        const dim3 grid(static_cast<unsigned>((windows + kWavesPerWg - 1) / kWavesPerWg), static_cast<unsigned>(a.hkv_l));
+    const int window = static_cast<int64_t>(chunk_rows) * a.hkv_l <= 4096 ? 1 : 8;
+    const int64_t windows = (static_cast<int64_t>(chunk_rows) + window - 1) / window + n_tokens - chunk_rows;
+    const int64_t wgs = (windows + kWavesPerWg - 1) / kWavesPerWg;
+    if (a.elem == 2 && (a.D == 128 || a.D == 64) && a.hkv_l <= 65535 && wgs <= most_workgroups(64 * kWavesPerWg)) {
+        const dim3 grid(static_cast<unsigned>(wgs), static_cast<unsigned>(a.hkv_l));
         auto rows = [&](auto kernel) {
             kernel<<<grid, 64 * kWavesPerWg, 0, st>>>(static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), slots, n_tokens, window,
                                                       chunk_rows, static_cast<uint8_t*>(cache), a.kv_scales, a.hkv_l, a.kv_stride);
@@ -256,14 +257,17 @@ hipError_t launch_kv_write_scaled(const void* k_new, const void* v_new, const in
         };
         return a.D == 128 ? rows(kv_write_scaled_rows_kernel<128>) : rows(kv_write_scaled_rows_kernel<64>);
     }
-    const int64_t wgs = (waves + kWavesPerWg - 1) / kWavesPerWg;
-    if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;
     auto run = [&](auto elem) {
         using Elem = decltype(elem);
-        kv_write_scaled_kernel<Elem><<<static_cast<unsigned>(wgs), 64 * kWavesPerWg, 0, st>>>(
-            static_cast<const Elem*>(k_new), static_cast<const Elem*>(v_new), slots, n_tokens, static_cast<uint8_t*>(cache), a.kv_scales,
-            a.hkv_l, a.D, a.kv_stride);
-        return hipGetLastError();
+        const int64_t piece = most_workgroups(64 * kWavesPerWg) * kWavesPerWg;   // (token, head) a launch
+        for (int64_t first = 0; first < waves; first += piece) {
+            const int64_t n = waves - first < piece ? waves - first : piece;
+            kv_write_scaled_kernel<Elem><<<static_cast<unsigned>((n + kWavesPerWg - 1) / kWavesPerWg), 64 * kWavesPerWg, 0, st>>>(
+                static_cast<const Elem*>(k_new), static_cast<const Elem*>(v_new), slots, n_tokens, static_cast<uint8_t*>(cache), a.kv_scales,
+                a.hkv_l, a.D, a.kv_stride, first);
+            if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        }
+        return hipSuccess;
     };
     return a.elem == 2 ? run(uint16_t{}) : run(float{});
 }
