@@ -48,12 +48,12 @@ template <typename Elem, typename KvElem>
 __global__ __launch_bounds__(kWaves * 64) void attn_rows_kernel(
     const Elem* __restrict__ q, const KvElem* __restrict__ cache, const int32_t* __restrict__ block_table,
     const int32_t* __restrict__ cu_seqlens_q, const int32_t* __restrict__ seq_lens, int num_seqs, int total_q,
-    Elem* __restrict__ out, AttnShape a) {
+    int64_t first_row, Elem* __restrict__ out, AttnShape a) {
     constexpr int kPer = 16 / sizeof(KvElem);  // cache elements per 16-byte vector
     __shared__ float q_s[kWaves][kMaxD];
     __shared__ float p_s[kWaves][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
+    const int64_t row = first_row + static_cast<int64_t>(blockIdx.x) * kWaves + wave;
     if (row >= static_cast<int64_t>(total_q) * a.hq_l) return;  // whole wavefront leaves together
     const int tok = static_cast<int>(row / a.hq_l);
     const int j = static_cast<int>(row % a.hq_l);
@@ -431,27 +431,21 @@ hipError_t launch_attn_generic(const void* q, const void* cache, const int32_t* 
                                void* out, const AttnShape& a, hipStream_t st) {
     const int64_t rows = static_cast<int64_t>(total_q) * a.hq_l;
     if (rows == 0) return hipSuccess;
-    const unsigned grid = static_cast<unsigned>((rows + kWaves - 1) / kWaves);
-    if (a.kv_fp8()) {
-        if (a.elem == 2)
-            attn_rows_kernel<uint16_t, uint8_t><<<grid, kWaves * 64, 0, st>>>(
-                static_cast<const uint16_t*>(q), static_cast<const uint8_t*>(cache), block_table, cu_seqlens_q, seq_lens,
-                num_seqs, total_q, static_cast<uint16_t*>(out), a);
-        else
-            attn_rows_kernel<float, uint8_t><<<grid, kWaves * 64, 0, st>>>(
-                static_cast<const float*>(q), static_cast<const uint8_t*>(cache), block_table, cu_seqlens_q, seq_lens,
-                num_seqs, total_q, static_cast<float*>(out), a);
-    } else if (a.elem == 2) {
-        attn_rows_kernel<uint16_t, uint16_t><<<grid, kWaves * 64, 0, st>>>(
-            static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(cache), block_table, cu_seqlens_q, seq_lens,
-            num_seqs, total_q, static_cast<uint16_t*>(out), a);
-    } else {
-        attn_rows_kernel<float, float><<<grid, kWaves * 64, 0, st>>>(static_cast<const float*>(q),
-                                                                   static_cast<const float*>(cache), block_table,
-                                                                   cu_seqlens_q, seq_lens, num_seqs, total_q,
-                                                                   static_cast<float*>(out), a);
-    }
-    return hipGetLastError();
+    constexpr int64_t kPiece = most_workgroups(kWaves * 64) * kWaves;   // rows a launch
+    auto run = [&](auto elem, auto kv_elem) {
+        using Elem = decltype(elem);
+        using KvElem = decltype(kv_elem);
+        for (int64_t first = 0; first < rows; first += kPiece) {
+            const int64_t n = rows - first < kPiece ? rows - first : kPiece;
+            attn_rows_kernel<Elem, KvElem><<<static_cast<unsigned>((n + kWaves - 1) / kWaves), kWaves * 64, 0, st>>>(
+                static_cast<const Elem*>(q), static_cast<const KvElem*>(cache), block_table, cu_seqlens_q, seq_lens, num_seqs, total_q, first,
+                static_cast<Elem*>(out), a);
+            if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    };
+    if (a.kv_fp8()) return a.elem == 2 ? run(uint16_t{}, uint8_t{}) : run(float{}, uint8_t{});
+    return a.elem == 2 ? run(uint16_t{}, uint16_t{}) : run(float{}, float{});
 }
 
 hipError_t launch_combine(const float* o_part, const float* ml_part, int n_rows, int hq_l, int D, int n_parts,

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 import plain_8bit as P
-from test_gpu_spare_rows import _dev, _rows
+from test_gpu_spare_rows import Values, _dev, _rows
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +101,25 @@ def test_quantiser_of_many_rows(B):
     whole = rows // len(part) * len(part)
     for got, part in ((codes, want), (scales, scale)):
         assert bool((got[:whole].view(-1, *part.shape) == part).all()) and torch.equal(got[whole:], part[:rows - whole])
+
+
+def test_general_kernel_on_many_padding_rows(B):
+    """A cache without scales, four heads a row."""
+    import torch
+    rng, rows, at = np.random.Generator(np.random.PCG64(5)), (1 << 24) + 37, [3, (1 << 24) - 2, (1 << 24) + 2]
+    lengths = [70, 40, 33]
+    cache, small = Values(15, 1, D), np.arange(15, dtype=np.int32).reshape(3, 5)
+    for s, n in enumerate(lengths):
+        x = _rows(rng, n, 1, 2 * D, dtype="bf16")
+        cache.append(x[..., :D], x[..., D:], small[s, np.arange(n) // 16].astype(np.int64) * 16 + np.arange(n) % 16)
+    table, lens = torch.zeros((rows, 5), dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    table[at], lens[at] = _dev(small), _dev(np.array(lengths, np.int32))
+    qs = _rows(rng, 3, 4, D, dtype="bf16")
+    q = torch.zeros((rows, 4, D), dtype=torch.bfloat16, device="cuda")
+    q[at] = _dev(qs, "bf16")
+    out = torch.full_like(q, 7.0)
+    B.decode(q, cache.device("bf16"), table, lens, 70, out, SCALE)
+    for i, (row, n) in enumerate(zip(at, lengths)):
+        _close(out[row:row + 1], P.attend(qs[i:i + 1], cache, small[i], n, SCALE), n)
+    out[at] = 0
+    assert not bool(out.any())
