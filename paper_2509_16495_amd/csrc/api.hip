@@ -434,7 +434,8 @@ int decode(bool scaled, float* kv_scales, const void* q, const void* k_new, cons
     // the tuned kernel appends the new tokens itself where it can; otherwise a write kernel runs in front
     const bool fused_append = new_kv && mfma && decode_mfma_appends(num_seqs, s);
     if (new_kv && !fused_append) {
-        e = launch_kv_write(k_new, v_new, slot_mapping, num_seqs, kv_cache, s, st);
+        e = scaled ? launch_kv_write_scaled(k_new, v_new, slot_mapping, num_seqs, 0, kv_cache, s, st)
+                   : launch_kv_write(k_new, v_new, slot_mapping, num_seqs, kv_cache, s, st);
         if (e != hipSuccess) return hip_fail(e, "kv_write launch");
     }
     if (mfma)
