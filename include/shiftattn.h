@@ -397,7 +397,7 @@ typedef struct shiftattn_tables {
 /* tables_append: gives every sequence the blocks that its new tokens need and says where the tokens go.
  *   new_lens (device, in)       : int32 [num_seqs], new tokens per sequence (< 0: 0); decode rows bring one or none
  *   num_prefill_seqs (host)     : the first so many sequences are chunks, the others decode rows
- *   total_prefill_q (host)      : rows that the chunks have together; rows: length of slot_mapping, at least total_prefill_q and
+ *   total_prefill_q (host)      : rows that the chunks have together, below 2^31 - 1; rows: length of slot_mapping, at least total_prefill_q and
  *                                 one row for each decode sequence (more: padding to a multiple of the SP degree)
  *   cu_seqlens_q (device, out)  : int32 [num_prefill_seqs + 1]
  *   slot_mapping (device, out)  : int64 [rows]; row cu_seqlens_q[s] + i is token i of chunk s, row total_prefill_q + j the token

@@ -901,6 +901,8 @@ int shiftattn_tables_append(const shiftattn_tables* t, const int32_t* new_lens, 
     if (int rc = check_tables(t, workspace, workspace_bytes)) return rc;
     if (num_prefill_seqs < 0 || num_prefill_seqs > t->num_seqs || total_prefill_q < 0 || rows < 0)
         return fail(SHIFTATTN_EINVAL, "num_prefill_seqs = %d of %d, total_prefill_q = %d, rows = %d", num_prefill_seqs, t->num_seqs, total_prefill_q, rows);
+    if (total_prefill_q == INT32_MAX)   // where sums of lengths saturate: more than that could not be told from as many
+        return fail(SHIFTATTN_EINVAL, "total_prefill_q = %d: at most 2^31 - 2", total_prefill_q);
     if (static_cast<int64_t>(total_prefill_q) + t->num_seqs - num_prefill_seqs > rows)
         return fail(SHIFTATTN_EINVAL, "rows = %d: %d rows of chunks and %d decode rows do not fit", rows, total_prefill_q, t->num_seqs - num_prefill_seqs);
     if (!cu_seqlens_q || (rows > 0 && !slot_mapping) || (t->num_seqs > 0 && (!new_lens || !taken)))
