@@ -378,7 +378,8 @@ def prefill(q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Tensor, 
             k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
             slot_mapping: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, k_scale: float = 1.0,
             v_scale: float = 1.0, kv_scales: Optional[torch.Tensor] = None) -> None:
-    """Causal attention of prefill chunks; q/out [total_q, hq_l, D] (row-strided views allowed)."""
+    """Causal attention of prefill chunks; q/out [total_q, hq_l, D] (row-strided views allowed).  Rows from cu_seqlens_q[-1] on stand for
+    no token: their place in out stays as it was, and their slots must be negative."""
     _check(_native().prefill(q, kv_cache, block_table, cu_seqlens_q, seq_lens, max_q_len, max_seq_len, out, softmax_scale, k_new, v_new,
                              slot_mapping, workspace, k_scale, v_scale, kv_scales))
 

@@ -317,7 +317,7 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
     float m_run, l_run;          // reference of the sums, sum of P
     float m_max = -INFINITY;     // kGroupRef: largest logit so far
     const float ref_drop = 8.f / c;
-    const float ref_least = -3e38f / fmaxf(c, 1.f);   // the reference stays finite (times c too) where all logits are minus infinity
+    const float ref_least = -3.4e38f / fmaxf(c, 1.f);   // the reference stays finite (times c too) where all logits are minus infinity
     auto reset = [&]() {
 #pragma unroll
         for (int mt = 0; mt < 8; ++mt) o[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
