@@ -12,6 +12,7 @@
  *   shiftattn_mixed             a unified batch of chunks and decode rows in one call
  *   shiftattn_unpack_head2seq   receive side of the head->sequence all-to-all (SP mode only)
  *   shiftattn_{kv_write,prefill,decode,mixed}_scaled   the same over an FP8 cache with a scale for each block and head
+ *   shiftattn_decode_shared     decode rows whose sequences share the first blocks of their tables, those read once for all
  *   shiftattn_tables_append / shiftattn_tables_truncate   block tables and slot maps from request lengths, on the GPU
  *
  * and, next to the exchange, the two projections fused with its layouts (bf16, or FP8 E4M3 operands):
@@ -20,6 +21,8 @@
  *   shiftattn_unpack_o_proj[_fp8]   embed = unpack(recv) * W_o^T read in place from the receive buffers
  *   shiftattn_quantize_rows_fp8 / shiftattn_quantize_recv_fp8   per-row FP8 quantisation for the above
  *   shiftattn_..._int8              the same projections and quantisers over 8-bit integers
+ *   shiftattn_add_rms_norm          residual addition and norm in front of them, in 16, 32 or 8 bits
+ *   shiftattn_rotary[_mixed]        rotary positions of the query and key rows behind them, in place
  *
  * In TP mode (the shift configuration, SP=1) a rank calls only kv_write/prefill/decode on the
  * fused rows its own QKV projection produced; in SP mode it packs, exchanges, attends,
@@ -260,6 +263,75 @@ int shiftattn_unpack_o_proj_int8_ws(const void *recv_codes, const float *a_scale
                                     const float *w_scales, void *out, int32_t T, int32_t T_pad, int32_t d_model,
                                     const shiftattn_xchg *xc, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Residual addition and root-mean-square norm, in front of a projection ------------------------------------------------
+ * For every row: h = x + residual in float32, rounded to the residual's type and stored there (residual NULL: h = x);
+ * inv = 1 / sqrt(sum_k h[k]^2 / cols + eps), the sum in 64 bits, rounded once to float32; y[k] = (h[k] * inv) * (weight[k] + weight_offset),
+ * each operation in float32.  Written as y rounded to bf16 or as it is (out_format SHIFTATTN_BF16 / _F32), or as the codes and the scale
+ * that shiftattn_quantize_rows_fp8 / _int8 name for the row y (SHIFTATTN_CODES_FP8 / _INT8), from y's float32 values: what the
+ * projections over 8-bit operands take.  The results do not depend on how rows are shared out: they are those bits.
+ *   x (device, in)               : [rows][cols], bf16 or float32, row stride x_stride
+ *   residual (device, in/out)    : [rows][cols], bf16 or float32, row stride residual_stride, or NULL
+ *   weight (device, in)          : [cols], bf16 or float32; weight_offset 1 is for weights stored as their difference from 1
+ *   out (device, out)            : [rows][cols] in out_format, row stride out_stride.  May be x itself where type and stride are the same
+ *   scales (device, out)         : float32 [rows] for codes, else NULL
+ * A NaN in h makes all of the row's y NaN, an infinity makes them 0 but for a NaN in its own place (scale 1 in both cases).
+ * cols: a multiple of 8 up to 65536 (else EUNSUPPORTED); eps > 0.  Pointers 16-byte aligned (scales: 4), row strides multiples of 16 bytes (codes: 8).  0 as a stride stands for dense rows. */
+enum { SHIFTATTN_CODES_FP8 = 2, SHIFTATTN_CODES_INT8 = 3 };  /* out_format, beside SHIFTATTN_BF16 and SHIFTATTN_F32 */
+typedef struct shiftattn_norm {
+    int32_t cols;
+    int32_t x_dtype, residual_dtype, weight_dtype;  /* SHIFTATTN_BF16 | SHIFTATTN_F32 (residual_dtype is not read without a residual) */
+    int32_t out_format;
+    float eps, weight_offset;
+    int32_t reserved;                               /* must be 0 */
+    int64_t x_stride, residual_stride, out_stride;  /* elements between consecutive rows; 0 = cols */
+} shiftattn_norm;
+int shiftattn_add_rms_norm(const void *x, void *residual, const void *weight, void *out, float *scales, int32_t rows,
+                           const shiftattn_norm *n, void *stream);
+
+/* ---- Rotary positions of query and key rows, in place, in front of the append and attention calls ------------------------------
+ * Of every head's first rot_dim elements the pairs (a, b) become (m (a cos t - b sin t), m (b cos t + a sin t)), t = p * frequencies[i]
+ * for pair i of a row at position p, m = magnitude, in float32, rounded once; t is reduced in 64 bits (exact to float32 at any
+ * position).  Pair i is elements i and i + rot_dim / 2 (SHIFTATTN_ROTARY_HALVES) or 2 i and 2 i + 1 (SHIFTATTN_ROTARY_PAIRS).
+ *   q, k (device, in/out)      : [rows][heads][head_dim], row strides q_stride, k_stride: views into one fused buffer as the attention
+ *                                calls take them (K is cached turned).  Either may be NULL.
+ *   frequencies (device, in)   : float64 [rot_dim / 2], radians per position (shiftattn_rotary_frequencies makes them)
+ * rotary: positions (device, in): int32 [rows]; a negative one (padding) leaves the row as it is.
+ * rotary_mixed: the rows of a unified batch, positions from what shiftattn_mixed takes: row cu_seqlens_q[s] + i is token i of the
+ *   last cu_seqlens_q[s + 1] - cu_seqlens_q[s] of chunk s's seq_lens[s], row total_prefill_q + j the last token of sequence
+ *   num_prefill_seqs + j.  Rows that stand for no token (chunk rows behind the last chunk, sequences of length <= 0) stay as they are.
+ *   (num_prefill_seqs = 0: decode rows alone; num_decode_seqs = 0: those of shiftattn_prefill.)
+ * rot_dim: a multiple of 16 up to head_dim (else EUNSUPPORTED); q, k 16-byte aligned, strides multiples of 16 bytes, 0 = dense. */
+enum { SHIFTATTN_ROTARY_HALVES = 0, SHIFTATTN_ROTARY_PAIRS = 1 };
+typedef struct shiftattn_rotary_desc {
+    int32_t num_q_heads, num_kv_heads, head_dim, rot_dim;
+    int32_t dtype;               /* SHIFTATTN_BF16 | SHIFTATTN_F32 */
+    int32_t layout;              /* SHIFTATTN_ROTARY_HALVES | SHIFTATTN_ROTARY_PAIRS */
+    float magnitude;             /* 1, or what a scaling for long contexts asks for; finite */
+    int32_t reserved;            /* must be 0 */
+    int64_t q_stride, k_stride;  /* elements between consecutive rows; 0 = heads * head_dim */
+} shiftattn_rotary_desc;
+int shiftattn_rotary(void *q, void *k, const int32_t *positions, int32_t rows, const double *frequencies,
+                     const shiftattn_rotary_desc *r, void *stream);
+int shiftattn_rotary_mixed(void *q, void *k, const int32_t *cu_seqlens_q, const int32_t *seq_lens, int32_t num_prefill_seqs,
+                           int32_t total_prefill_q, int32_t num_decode_seqs, const double *frequencies,
+                           const shiftattn_rotary_desc *r, void *stream);
+
+/* Frequencies (host only, no GPU work): n = rot_dim / 2 float64 values into `frequencies` (host), the magnitude that goes with them into
+ * `magnitude`.  With f_i = base^(-2 i / rot_dim), L = original_len (the context that the model was trained for):
+ *   PLAIN        f_i
+ *   LINEAR       f_i / factor
+ *   BASE         base * factor^(rot_dim / (rot_dim - 2)) in place of base: the highest frequency stays, the lowest is divided by factor
+ *   WAVELENGTHS  s f_i + (1 - s) f_i / factor, s = (L f_i / (2 pi) - low) / (high - low) cut to [0, 1]: pairs that turn more than
+ *                `high` times over L stay, those that turn less than `low` times are divided by factor
+ *   PARTS        the same with s = 1 - (i - i_high) / (i_low - i_high) cut to [0, 1], linear in i between the indices
+ *                i_x = rot_dim ln(L / (2 pi x)) / (2 ln base) of pairs that turn x = high and low times, rounded outward to whole
+ *                numbers and cut to [0, rot_dim - 1]; magnitude 0.1 ln(factor) + 1 (factor > 1)
+ * EINVAL unless rot_dim >= 2 is even (BASE: > 2), base > 1, factor >= 1, and, where they are read, L > 0 and high > low > 0. */
+enum { SHIFTATTN_ROTARY_PLAIN = 0, SHIFTATTN_ROTARY_LINEAR = 1, SHIFTATTN_ROTARY_BASE = 2, SHIFTATTN_ROTARY_WAVELENGTHS = 3,
+       SHIFTATTN_ROTARY_PARTS = 4 };
+int shiftattn_rotary_frequencies(int32_t kind, int32_t rot_dim, double base, double factor, double original_len, double low,
+                                 double high, double *frequencies, float *magnitude);
+
 /* ---- KV-cache append (Sec. 2.2: prefill initialises the cache, decoding appends to it) --------
  * k_new, v_new (device, in): [n_tokens][hkv_l][D] with row stride a->kv_stride.
  * slot_mapping (device, in): int64 [n_tokens]; token i goes to slot slot_mapping[i];
@@ -335,6 +407,26 @@ int shiftattn_decode(const void *q, const void *k_new, const void *v_new, const 
 int shiftattn_decode_static(const void *q, const void *k_new, const void *v_new, const int64_t *slot_mapping,
                             void *kv_cache, const int32_t *block_table, const int32_t *seq_lens, int32_t num_seqs,
                             int32_t max_seq_len, void *out, const shiftattn_attn *a, void *stream);
+
+/* ---- Decode rows of sequences that share a prefix -------------------------------------------------------------------------
+ * shiftattn_decode (or, with kv_scales, shiftattn_decode_scaled) of a batch whose sequences come in groups with a prompt in common: the
+ * blocks in common are read once for a group, and meet all its query rows in matrix products, instead of once for every sequence.  The
+ * result is that of the plain call, up to the order in which partial sums are added and the references against which probabilities are
+ * rounded (bitwise reproducible).
+ *   group_offsets (device, in): int32 [num_groups + 1], non-decreasing, between 0 and num_seqs: group i is sequences
+ *                 group_offsets[i] .. group_offsets[i + 1] - 1; sequences outside all groups share nothing
+ *   shared_lens (device, in)  : int32 [num_groups]: so many first tokens the sequences of a group have in common.  Of those the whole blocks
+ *                 are shared: entries 0 .. shared_lens[i] / 16 - 1 of the sequences' rows of block_table name the same blocks
+ *                 (as far as a sequence has tokens; entries of padding rows are not read).  What remains of shared_lens[i] / 16 lies in blocks of
+ *                 each sequence's own.  <= 0: nothing in common
+ *   kv_scales: the scales of a cache with block scales (a->kv_format = SHIFTATTN_KV_FP8_E4M3_BLOCKS), NULL for any other
+ *   All else as in shiftattn_decode; a token that is appended must lie behind the blocks in common.
+ * bf16 rows with head_dim 128 and up to 16 query heads per KV head, and up to 1024 groups, take the kernel that shares; any other call is
+ * served as the plain one.  workspace: shiftattn_decode_shared_workspace_bytes(...) bytes, 16-byte aligned. */
+int shiftattn_decode_shared(const void *q, const void *k_new, const void *v_new, const int64_t *slot_mapping, void *kv_cache,
+                            float *kv_scales, const int32_t *block_table, const int32_t *seq_lens, int32_t num_seqs,
+                            int32_t max_seq_len, const int32_t *group_offsets, const int32_t *shared_lens, int32_t num_groups,
+                            void *out, void *workspace, size_t workspace_bytes, const shiftattn_attn *a, void *stream);
 
 /* ---- Algorithm 1, boxed line, on a unified batch: prefill chunks and decode rows in one call ------
  * A chunked-prefill engine (Sec. 5, related work on chunked prefill) puts both kinds of rows into one
@@ -427,6 +519,7 @@ int shiftattn_tables_truncate(const shiftattn_tables *t, const int32_t *keep_len
 size_t shiftattn_prefill_workspace_bytes(int32_t num_seqs, int32_t total_q, int32_t max_q_len,
                                          int32_t max_seq_len, const shiftattn_attn *a);
 size_t shiftattn_decode_workspace_bytes(int32_t num_seqs, int32_t max_seq_len, const shiftattn_attn *a);
+size_t shiftattn_decode_shared_workspace_bytes(int32_t num_seqs, int32_t max_seq_len, int32_t num_groups, const shiftattn_attn *a);
 size_t shiftattn_mixed_workspace_bytes(int32_t num_prefill_seqs, int32_t total_prefill_q, int32_t max_q_len,
                                        int32_t max_prefill_seq_len, int32_t num_decode_seqs,
                                        int32_t max_decode_seq_len, const shiftattn_attn *a);

@@ -51,6 +51,17 @@ class Tables(ctypes.Structure):
                 ("free_blocks", ctypes.c_void_p), ("free_count", ctypes.c_void_p)]
 
 
+class Norm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("cols", "x_dtype", "residual_dtype", "weight_dtype", "out_format")] + [
+        ("eps", ctypes.c_float), ("weight_offset", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "out_stride")]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_q_heads", "num_kv_heads", "head_dim", "rot_dim", "dtype", "layout")] + [
+        ("magnitude", ctypes.c_float), ("reserved", ctypes.c_int32), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64)]
+
+
 class PrefillPlan(ctypes.Structure):
     _fields_ = [("tile_columns", ctypes.c_int32), ("wave_columns", ctypes.c_int32), ("key_ranges", ctypes.c_int32),
                 ("tiles_per_wg", ctypes.c_int32), ("decode_wgs", ctypes.c_int32)]
@@ -144,6 +155,13 @@ def lib() -> ctypes.CDLL:
         L.shiftattn_tables_workspace_bytes.restype = sz
         L.shiftattn_tables_append.argtypes = [ctypes.POINTER(Tables), vp, i32, i32, i32, vp, i64p, vp, vp, sz, vp]
         L.shiftattn_tables_truncate.argtypes = [ctypes.POINTER(Tables), vp, vp, sz, vp]
+        L.shiftattn_add_rms_norm.argtypes = [vp, vp, vp, vp, vp, i32, ctypes.POINTER(Norm), vp]
+        L.shiftattn_rotary.argtypes = [vp, vp, vp, i32, vp, ctypes.POINTER(Rotary), vp]
+        L.shiftattn_rotary_mixed.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, ctypes.POINTER(Rotary), vp]
+        L.shiftattn_rotary_frequencies.argtypes = [i32, i32] + [ctypes.c_double] * 5 + [vp, ctypes.POINTER(ctypes.c_float)]
+        L.shiftattn_decode_shared.argtypes = [vp, vp, vp, i64p, vp, vp, vp, vp, i32, i32, vp, vp, i32, vp, vp, sz, ap, vp]
+        L.shiftattn_decode_shared_workspace_bytes.argtypes = [i32, i32, i32, ap]
+        L.shiftattn_decode_shared_workspace_bytes.restype = sz
         L.shiftattn_last_error.restype = ctypes.c_char_p
         _calls = importlib.import_module("._calls", __package__)
         _calls.bind(_workspace, *[ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _calls.names])
@@ -282,6 +300,46 @@ def unpack_head2seq(recv: torch.Tensor, out: torch.Tensor) -> None:
     _check(_native().unpack_head2seq(recv, out))
 
 
+# ---- norm in front of a projection, rotary positions behind it --------------------------------------------
+CODES_FP8, CODES_INT8 = 2, 3
+
+
+def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, out: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                 scales: Optional[torch.Tensor] = None, weight_offset: float = 0.0) -> None:
+    """residual += x (in place, in its type), then out = residual / rms(residual) * (weight + weight_offset); without a residual the norm of x.
+    x, residual, out [rows, cols] (row-strided views allowed).  out bfloat16 or float32; or uint8 (FP8 E4M3 codes) or int8 with scales float32
+    [rows], as quantize_rows_fp8 / quantize_rows_int8 make them: what the projections over 8-bit operands take."""
+    _check(_native().add_rms_norm(x, weight, out, eps, residual, scales, weight_offset))
+
+
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "wavelengths": 3, "parts": 4}
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, original_len: float = 0.0,
+                       low: float = 1.0, high: float = 32.0):
+    """Radians per position of rot_dim / 2 pairs (float64, on the host) and the magnitude that goes with them; `scaling` for contexts longer
+    than original_len: "linear", "base", "wavelengths", "parts" (host only)."""
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling: one of {', '.join(ROTARY_SCALINGS)}, not {scaling!r}")
+    f, m = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.float64), ctypes.c_float(1.0)
+    _check(lib().shiftattn_rotary_frequencies(ROTARY_SCALINGS[scaling], rot_dim, base, factor, original_len, low, high, f.data_ptr(), ctypes.byref(m)))
+    return f, m.value
+
+
+def rotary(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, frequencies: torch.Tensor, pairs: bool = False,
+           magnitude: float = 1.0) -> None:
+    """Turns q [rows, hq_l, D] and k [rows, hkv_l, D] (row-strided views allowed, either may be None) in place by positions int32 [rows] times
+    frequencies float64 [rot_dim / 2]: pair i is elements i and i + rot_dim / 2 of a head, or 2 i and 2 i + 1 (pairs=True).  Rows with a
+    negative position stay as they are."""
+    _check(_native().rotary(q, k, positions, frequencies, pairs, magnitude))
+
+
+def rotary_mixed(q: Optional[torch.Tensor], k: Optional[torch.Tensor], cu_seqlens_q: torch.Tensor, seq_lens: torch.Tensor, num_prefill_seqs: int,
+                 frequencies: torch.Tensor, pairs: bool = False, magnitude: float = 1.0) -> None:
+    """rotary() of a unified batch's rows, their positions taken from what mixed() takes (chunks first, then one row per other sequence)."""
+    _check(_native().rotary_mixed(q, k, cu_seqlens_q, seq_lens, num_prefill_seqs, frequencies, pairs, magnitude))
+
+
 # ---- KV cache and attention -------------------------------------------------------------------------
 def proj_workspace_bytes(rows: int, n_features: int, k: int, fp8: bool = False) -> int:
     """Bytes of workspace that a projection of `rows` token rows with an [n_features, k] matrix makes good use of (or more than it uses)."""
@@ -404,6 +462,21 @@ def decode_static(q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Te
     """decode() without a workspace: the library's own static device array takes the split partials."""
     _check(_native().decode_static(q, kv_cache, block_table, seq_lens, max_seq_len, out, softmax_scale, k_new, v_new, slot_mapping, None,
                                    k_scale, v_scale, None))
+
+
+def decode_shared_workspace_bytes(num_seqs: int, max_seq_len: int, num_groups: int, a: Attn) -> int:
+    return int(lib().shiftattn_decode_shared_workspace_bytes(num_seqs, max_seq_len, num_groups, ctypes.byref(a)))
+
+
+def decode_shared(q: torch.Tensor, kv_cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor, max_seq_len: int,
+                  group_offsets: torch.Tensor, shared_lens: torch.Tensor, out: torch.Tensor, softmax_scale: float,
+                  k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None, slot_mapping: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, k_scale: float = 1.0, v_scale: float = 1.0,
+                  kv_scales: Optional[torch.Tensor] = None) -> None:
+    """decode() of a batch in which group i, sequences group_offsets[i] .. group_offsets[i + 1] - 1, has its first shared_lens[i] tokens in
+    common: the whole blocks of those, the same in the group's rows of block_table, are read once for all of it."""
+    _check(_native().decode_shared(q, kv_cache, block_table, seq_lens, max_seq_len, group_offsets, shared_lens, out, softmax_scale, k_new, v_new,
+                                   slot_mapping, workspace, k_scale, v_scale, kv_scales))
 
 
 def mixed_workspace_bytes(num_prefill_seqs: int, total_prefill_q: int, max_q_len: int, max_prefill_seq_len: int,

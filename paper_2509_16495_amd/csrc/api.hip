@@ -8,6 +8,7 @@
 #include <stdlib.h>
 
 #include <atomic>
+#include <cmath>
 #include <mutex>
 
 #include "internal.h"
@@ -783,6 +784,144 @@ size_t shiftattn_decode_workspace_bytes(int32_t num_seqs, int32_t max_seq_len, c
     if (check_attn(a, &s) || num_seqs < 0 || max_seq_len < 0) return SIZE_MAX;
     if (!use_decode_mfma(s, num_seqs, max_seq_len) || num_seqs == 0) return 0;
     return decode_mfma_workspace(num_seqs, max_seq_len, s);
+}
+
+// ---- norm, rotary positions, decode behind a shared prefix ---------------------------------------------------------------
+int shiftattn_add_rms_norm(const void* x, void* residual, const void* weight, void* out, float* scales, int32_t rows,
+                           const shiftattn_norm* n, void* stream) {
+    if (!n) return fail(SHIFTATTN_EINVAL, "norm descriptor is NULL");
+    const int ex = elem_size(n->x_dtype), ew = elem_size(n->weight_dtype), er = residual ? elem_size(n->residual_dtype) : 2;
+    if (!ex || !ew || !er) return fail(SHIFTATTN_EINVAL, "unknown dtype: x %d, weight %d, residual %d", n->x_dtype, n->weight_dtype, n->residual_dtype);
+    if (n->out_format < SHIFTATTN_BF16 || n->out_format > SHIFTATTN_CODES_INT8) return fail(SHIFTATTN_EINVAL, "unknown out_format %d", n->out_format);
+    const bool codes = n->out_format == SHIFTATTN_CODES_FP8 || n->out_format == SHIFTATTN_CODES_INT8;
+    if (n->reserved != 0) return fail(SHIFTATTN_EINVAL, "reserved field must be 0");
+    if (rows < 0 || n->cols < 1) return fail(SHIFTATTN_EINVAL, "rows = %d, cols = %d", rows, n->cols);
+    if (n->cols % 8 || n->cols > 65536) return fail(SHIFTATTN_EUNSUPPORTED, "cols = %d: need a multiple of 8 up to 65536", n->cols);
+    if (!(n->eps > 0.f) || n->eps > 3.0e38f) return fail(SHIFTATTN_EINVAL, "eps must be positive and finite");
+    if (!(n->weight_offset >= -3.0e38f && n->weight_offset <= 3.0e38f)) return fail(SHIFTATTN_EINVAL, "weight_offset must be finite");
+    NormShape s{n->cols, ex == 4, er == 4, ew == 4, n->out_format, n->eps, n->weight_offset, n->x_stride ? n->x_stride : n->cols,
+                n->residual_stride ? n->residual_stride : n->cols, n->out_stride ? n->out_stride : n->cols};
+    const int eo = codes ? 1 : elem_size(n->out_format);
+    if (s.x_stride < s.cols || s.out_stride < s.cols || (residual && s.res_stride < s.cols))
+        return fail(SHIFTATTN_EINVAL, "a row stride is smaller than the row it strides over");
+    if ((s.x_stride * ex) % 16 || (residual && (s.res_stride * er) % 16) || (s.out_stride * eo) % (codes ? 8 : 16))
+        return fail(SHIFTATTN_EINVAL, "row strides must be multiples of 16 bytes (codes: 8)");
+    if (rows == 0) return SHIFTATTN_OK;
+    if (!x || !weight || !out || (codes && !scales)) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (out == residual) return fail(SHIFTATTN_EINVAL, "out and residual are the same rows");
+    if (!codes && scales) return fail(SHIFTATTN_EINVAL, "scales belong to codes: must be NULL for values");
+    if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned_to(out, codes ? 8 : 16) || !aligned_to(scales, 4))
+        return fail(SHIFTATTN_EINVAL, "x / residual / weight / out must be 16-byte aligned (codes: 8), scales 4-byte");
+    hipError_t e = launch_add_rms_norm(x, residual, weight, out, scales, rows, s, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "add_rms_norm launch");
+}
+
+namespace {
+
+int check_rotary(const shiftattn_rotary_desc* r, const void* q, const void* k, int64_t rows, const double* frequencies, RotaryShape* s) {
+    if (!r) return fail(SHIFTATTN_EINVAL, "rotary descriptor is NULL");
+    const int e = elem_size(r->dtype);
+    if (!e) return fail(SHIFTATTN_EINVAL, "unknown dtype %d", r->dtype);
+    if (r->layout != SHIFTATTN_ROTARY_HALVES && r->layout != SHIFTATTN_ROTARY_PAIRS) return fail(SHIFTATTN_EINVAL, "unknown layout %d", r->layout);
+    if (r->reserved != 0) return fail(SHIFTATTN_EINVAL, "reserved field must be 0");
+    if ((q && r->num_q_heads < 1) || (k && r->num_kv_heads < 1) || r->num_q_heads > 65536 || r->num_kv_heads > 65536)
+        return fail(SHIFTATTN_EINVAL, "num_q_heads = %d, num_kv_heads = %d", r->num_q_heads, r->num_kv_heads);
+    if (r->head_dim < 1 || r->rot_dim < 1 || r->rot_dim > r->head_dim) return fail(SHIFTATTN_EINVAL, "need 1 <= rot_dim (%d) <= head_dim (%d)", r->rot_dim, r->head_dim);
+    if (r->rot_dim % 16 || r->head_dim % 8 || r->head_dim > 256)
+        return fail(SHIFTATTN_EUNSUPPORTED, "rot_dim = %d, head_dim = %d: need multiples of 16 and of 8 up to 256", r->rot_dim, r->head_dim);
+    if (!(r->magnitude >= -3.0e38f && r->magnitude <= 3.0e38f)) return fail(SHIFTATTN_EINVAL, "magnitude must be finite");
+    *s = RotaryShape{r->num_q_heads, r->num_kv_heads, r->head_dim, r->rot_dim, e, r->layout == SHIFTATTN_ROTARY_PAIRS, r->magnitude,
+                     r->q_stride ? r->q_stride : static_cast<int64_t>(r->num_q_heads) * r->head_dim,
+                     r->k_stride ? r->k_stride : static_cast<int64_t>(r->num_kv_heads) * r->head_dim};
+    if ((q && s->q_stride < static_cast<int64_t>(s->hq) * s->head_dim) || (k && s->k_stride < static_cast<int64_t>(s->hkv) * s->head_dim))
+        return fail(SHIFTATTN_EINVAL, "a row stride is smaller than the row it strides over");
+    if ((q && (s->q_stride * e) % 16) || (k && (s->k_stride * e) % 16)) return fail(SHIFTATTN_EINVAL, "row strides must be multiples of 16 bytes");
+    if (rows < 0) return fail(SHIFTATTN_EINVAL, "negative size argument");
+    if (rows > 0x7FFFFFFF) return fail(SHIFTATTN_EUNSUPPORTED, "more than 2^31-1 rows");
+    if (rows == 0) return 0;
+    if ((!q && !k) || !frequencies) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (!aligned16(q) || !aligned16(k) || !aligned_to(frequencies, 8)) return fail(SHIFTATTN_EINVAL, "q / k must be 16-byte aligned, frequencies 8-byte");
+    return 0;
+}
+
+}  // namespace
+
+int shiftattn_rotary(void* q, void* k, const int32_t* positions, int32_t rows, const double* frequencies, const shiftattn_rotary_desc* r,
+                     void* stream) {
+    RotaryShape s;
+    if (int rc = check_rotary(r, q, k, rows, frequencies, &s)) return rc;
+    if (rows == 0) return SHIFTATTN_OK;
+    if (!positions || !aligned_to(positions, 4)) return fail(SHIFTATTN_EINVAL, "positions is NULL or not 4-byte aligned");
+    hipError_t e = launch_rotary(s, q, k, positions, nullptr, nullptr, 0, 0, rows, frequencies, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "rotary launch");
+}
+
+int shiftattn_rotary_mixed(void* q, void* k, const int32_t* cu_seqlens_q, const int32_t* seq_lens, int32_t num_prefill_seqs,
+                           int32_t total_prefill_q, int32_t num_decode_seqs, const double* frequencies, const shiftattn_rotary_desc* r,
+                           void* stream) {
+    if (num_prefill_seqs < 0 || total_prefill_q < 0 || num_decode_seqs < 0) return fail(SHIFTATTN_EINVAL, "negative size argument");
+    const int64_t rows = static_cast<int64_t>(total_prefill_q) + num_decode_seqs;
+    RotaryShape s;
+    if (int rc = check_rotary(r, q, k, rows, frequencies, &s)) return rc;
+    if (rows == 0) return SHIFTATTN_OK;
+    if ((num_prefill_seqs > 0 && total_prefill_q > 0 && !cu_seqlens_q) || (num_prefill_seqs + static_cast<int64_t>(num_decode_seqs) > 0 && !seq_lens))
+        return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (!aligned_to(cu_seqlens_q, 4) || !aligned_to(seq_lens, 4)) return fail(SHIFTATTN_EINVAL, "cu_seqlens_q / seq_lens must be 4-byte aligned");
+    hipError_t e = launch_rotary(s, q, k, nullptr, cu_seqlens_q, seq_lens, num_prefill_seqs, total_prefill_q, static_cast<int>(rows), frequencies,
+                                 static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "rotary_mixed launch");
+}
+
+int shiftattn_rotary_frequencies(int32_t kind, int32_t rot_dim, double base, double factor, double original_len, double low, double high,
+                                 double* frequencies, float* magnitude) {
+    if (kind < SHIFTATTN_ROTARY_PLAIN || kind > SHIFTATTN_ROTARY_PARTS) return fail(SHIFTATTN_EINVAL, "unknown kind %d", kind);
+    if (!frequencies || !magnitude) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (rot_dim < 2 || rot_dim % 2 || (kind == SHIFTATTN_ROTARY_BASE && rot_dim == 2)) return fail(SHIFTATTN_EINVAL, "rot_dim = %d", rot_dim);
+    if (!(base > 1.0) || !std::isfinite(base)) return fail(SHIFTATTN_EINVAL, "base must be above 1 and finite");
+    const bool by_turns = kind == SHIFTATTN_ROTARY_WAVELENGTHS || kind == SHIFTATTN_ROTARY_PARTS;
+    if (kind != SHIFTATTN_ROTARY_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return fail(SHIFTATTN_EINVAL, "factor must be at least 1 and finite");
+    if (by_turns && (!(original_len > 0.0) || !std::isfinite(original_len) || !(low > 0.0) || !(high > low) || !std::isfinite(high)))
+        return fail(SHIFTATTN_EINVAL, "need original_len > 0 and high > low > 0, finite");
+    constexpr double kTurn = 6.283185307179586;
+    if (kind == SHIFTATTN_ROTARY_BASE) base *= std::pow(factor, static_cast<double>(rot_dim) / (rot_dim - 2));
+    if (!std::isfinite(base)) return fail(SHIFTATTN_EINVAL, "base and factor are too large");
+    auto index_of = [&](double turns) { return rot_dim * std::log(original_len / (kTurn * turns)) / (2.0 * std::log(base)); };
+    double from = 0.0, to = 0.0;   // PARTS: indices up to which pairs stay, and from which they are divided
+    if (kind == SHIFTATTN_ROTARY_PARTS) {
+        from = std::fmax(std::floor(index_of(high)), 0.0);
+        to = std::fmin(std::ceil(index_of(low)), rot_dim - 1.0);
+        if (!(to > from)) to = from + 0.001;   // a step
+    }
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rot_dim);
+        double stays = 1.0;
+        if (kind == SHIFTATTN_ROTARY_LINEAR) stays = 0.0;
+        if (kind == SHIFTATTN_ROTARY_WAVELENGTHS) stays = (original_len * f / kTurn - low) / (high - low);
+        if (kind == SHIFTATTN_ROTARY_PARTS) stays = 1.0 - (i - from) / (to - from);
+        stays = std::fmin(std::fmax(stays, 0.0), 1.0);
+        frequencies[i] = stays * f + (1.0 - stays) * (f / (kind == SHIFTATTN_ROTARY_PLAIN || kind == SHIFTATTN_ROTARY_BASE ? 1.0 : factor));
+    }
+    *magnitude = kind == SHIFTATTN_ROTARY_PARTS && factor > 1.0 ? static_cast<float>(0.1 * std::log(factor) + 1.0) : 1.0f;
+    return SHIFTATTN_OK;
+}
+
+int shiftattn_decode_shared(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache, float* kv_scales,
+                            const int32_t* block_table, const int32_t* seq_lens, int32_t num_seqs, int32_t max_seq_len,
+                            const int32_t* group_offsets, const int32_t* shared_lens, int32_t num_groups, void* out, void* workspace,
+                            size_t workspace_bytes, const shiftattn_attn* a, void* stream) {
+    AttnShape s;
+    if (int rc = check_attn(a, &s)) return rc;
+    if (!s.block_scales && kv_scales) return fail(SHIFTATTN_EINVAL, "kv_scales must be NULL for a cache without a scale for each block");
+    if (num_groups < 0) return fail(SHIFTATTN_EINVAL, "num_groups = %d", num_groups);
+    if (num_groups > 0 && (!group_offsets || !shared_lens || !aligned_to(group_offsets, 4) || !aligned_to(shared_lens, 4)))
+        return fail(SHIFTATTN_EINVAL, "group_offsets or shared_lens is NULL or not 4-byte aligned");
+    return decode(s.block_scales, kv_scales, q, k_new, v_new, slot_mapping, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, out,
+                  workspace, workspace_bytes, a, stream);
+}
+
+size_t shiftattn_decode_shared_workspace_bytes(int32_t num_seqs, int32_t max_seq_len, int32_t num_groups, const shiftattn_attn* a) {
+    if (num_groups < 0) return SIZE_MAX;
+    return shiftattn_decode_workspace_bytes(num_seqs, max_seq_len, a);
 }
 
 int shiftattn_decode_static(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,

@@ -5,6 +5,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/shiftattn.h"
 #include "../../include/shiftattn_probe.h"
 
 namespace shiftattn {
@@ -62,6 +63,28 @@ size_t tables_workspace(int num_seqs);
 hipError_t launch_tables_append(const shiftattn_tables& t, const int32_t* new_lens, int num_prefill, int total_prefill_q, int rows, int32_t* cu,
                                 int64_t* slots, int32_t* taken, void* workspace, hipStream_t st);
 hipError_t launch_tables_truncate(const shiftattn_tables& t, const int32_t* keep_lens, void* workspace, hipStream_t st);
+
+// residual_norm.hip : residual addition and root-mean-square norm of rows
+struct NormShape {
+    int cols;
+    bool x_f32, res_f32, w_f32;
+    int out_kind;      // SHIFTATTN_BF16, SHIFTATTN_F32, SHIFTATTN_CODES_FP8, SHIFTATTN_CODES_INT8
+    float eps, offset;
+    int64_t x_stride, res_stride, out_stride;   // in elements
+};
+hipError_t launch_add_rms_norm(const void* x, void* residual, const void* weight, void* out, float* scales, int rows, const NormShape& s,
+                               hipStream_t st);
+
+// rotary.hip : query and key rows turned by their positions, in place (q or k null: without them; positions null: from cu_seqlens_q and
+// seq_lens of a unified batch)
+struct RotaryShape {
+    int hq, hkv, head_dim, rot_dim, elem;
+    bool pairs;
+    float magnitude;
+    int64_t q_stride, k_stride;   // in elements
+};
+hipError_t launch_rotary(const RotaryShape& s, void* q, void* k, const int32_t* positions, const int32_t* cu_seqlens_q, const int32_t* seq_lens,
+                         int num_prefill, int total_prefill_q, int rows, const double* frequencies, hipStream_t st);
 
 // attn_generic.hip : any dtype / head_dim / head ratio, one wavefront per (token, head) row
 hipError_t launch_attn_generic(const void* q, const void* cache, const int32_t* block_table,

@@ -27,6 +27,8 @@ namespace {
     F(kv_write_scaled, kv_write_scaled) F(tables_append, tables_append) F(tables_truncate, tables_truncate)                 \
     F(qkv_int8, qkv_proj_pack_int8_ws) F(o_proj_int8, unpack_o_proj_int8_ws) F(quantize_rows_int8, quantize_rows_int8)       \
     F(quantize_recv_int8, quantize_recv_int8) F(tables_bytes, tables_workspace_bytes)                                                                                 \
+    F(norm, add_rms_norm) F(rotary, rotary) F(rotary_mixed, rotary_mixed) F(decode_shared, decode_shared)                     \
+    F(shared_bytes, decode_shared_workspace_bytes)                                                                            \
     F(prefill_bytes, prefill_workspace_bytes) F(decode_bytes, decode_workspace_bytes) F(mixed_bytes, mixed_workspace_bytes)
 struct Library {
 #define SHIFTATTN_POINTER(member, name) decltype(&shiftattn_##name) member;
@@ -574,6 +576,127 @@ PyObject* o_codes_call(PyObject* const* a, Py_ssize_t n, bool int8) {
 SHIFTATTN_CALL(unpack_o_proj_fp8) { return o_codes_call(a, n, false); }
 SHIFTATTN_CALL(unpack_o_proj_int8) { return o_codes_call(a, n, true); }
 
+// elements between consecutive rows of a [rows, cols] view whose rows are dense
+int64_t norm_stride(const at::Tensor& t, const char* name) {
+    dims(t, 2, name);
+    need(t.size(1) == 1 || t.stride(1) == 1, "x, residual, out: rows must be dense");
+    apart(t);
+    return t.size(0) > 1 ? t.stride(0) : t.size(1);
+}
+
+// x, weight, out, eps, residual, scales, weight_offset
+SHIFTATTN_CALL(add_rms_norm) {
+    return run(n, 7, [&] {
+        const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]), &out = tensor(a[2]);
+        const at::Tensor *res = tensor_or_none(a[4]), *scales = tensor_or_none(a[5]);
+        shiftattn_norm d{};
+        d.x_stride = norm_stride(x, "x"), d.out_stride = norm_stride(out, "out"), d.residual_stride = res ? norm_stride(*res, "residual") : 0;
+        d.cols = cut(x.size(1)), d.x_dtype = dtype_code(x), d.weight_dtype = dtype_code(w), d.residual_dtype = res ? dtype_code(*res) : SHIFTATTN_BF16;
+        const bool codes = out.scalar_type() == at::kByte || out.scalar_type() == at::kChar;
+        d.out_format = out.scalar_type() == at::kByte ? SHIFTATTN_CODES_FP8 : out.scalar_type() == at::kChar ? SHIFTATTN_CODES_INT8 : dtype_code(out);
+        need(x.size(0) <= INT32_MAX && x.size(1) <= INT32_MAX, "x: fewer than 2^31 rows and columns");
+        need(out.sizes() == x.sizes() && (!res || res->sizes() == x.sizes()), "out, residual: shape of x");
+        need(w.dim() == 1 && w.size(0) == x.size(1) && w.is_contiguous(), "weight: contiguous [cols]");
+        need(codes == (scales != nullptr), "scales: beside codes (out uint8: FP8, or int8), and only there");
+        need(!scales || (scales->scalar_type() == at::kFloat && scales->dim() == 1 && scales->size(0) == x.size(0) && scales->is_contiguous()),
+             "scales: contiguous float32 [rows]");
+        here({&x, &w, &out, res, scales});
+        d.eps = real(a[3]), d.weight_offset = real(a[6]);
+        return [d, px = ptr(x), pr = ptr(res), pw = ptr(w), po = ptr(out), ps = ptr(scales), rows = cut(x.size(0)), st = stream()] {
+            return lib.norm(px, pr, pw, po, static_cast<float*>(ps), rows, &d, st);
+        };
+    });
+}
+
+// what both rotary calls take: q, k (either may be None), frequencies, pairs, magnitude
+shiftattn_rotary_desc rotary_of(const at::Tensor* q, const at::Tensor* k, const at::Tensor& f, PyObject* pairs, PyObject* magnitude) {
+    need(q || k, "q or k is wanted");
+    const at::Tensor& one = q ? *q : *k;
+    dims(one, 3, q ? "q" : "k");
+    shiftattn_rotary_desc d{};
+    for (const at::Tensor* t : {q, k}) {
+        if (!t) continue;
+        dims(*t, 3, t == q ? "q" : "k");
+        need(t->size(0) == one.size(0) && t->size(2) == one.size(2) && t->scalar_type() == one.scalar_type(), "q, k: as many rows, one head_dim and type");
+        need(t->size(0) <= INT32_MAX && t->size(1) <= INT32_MAX && t->size(2) <= INT32_MAX, "q, k: sizes below 2^31");
+        apart(*t);
+    }
+    need(f.scalar_type() == at::kDouble && f.dim() == 1 && f.is_contiguous() && 2 * f.size(0) <= one.size(2), "frequencies: contiguous float64 [rot_dim / 2], rot_dim <= head_dim");
+    here({q, k, &f});
+    d.num_q_heads = q ? cut(q->size(1)) : 0, d.num_kv_heads = k ? cut(k->size(1)) : 0, d.head_dim = cut(one.size(2)), d.rot_dim = cut(2 * f.size(0));
+    d.dtype = dtype_code(one);
+    const int in_pairs = PyObject_IsTrue(pairs);
+    if (in_pairs < 0) throw PythonError{};
+    d.layout = in_pairs ? SHIFTATTN_ROTARY_PAIRS : SHIFTATTN_ROTARY_HALVES;
+    d.magnitude = real(magnitude);
+    d.q_stride = q ? row_stride(*q) : 0, d.k_stride = k ? row_stride(*k) : 0;
+    return d;
+}
+
+// q, k, positions, frequencies, pairs, magnitude
+SHIFTATTN_CALL(rotary) {
+    return run(n, 6, [&] {
+        const at::Tensor *q = tensor_or_none(a[0]), *k = tensor_or_none(a[1]);
+        const at::Tensor &pos = tensor(a[2]), &f = tensor(a[3]);
+        const shiftattn_rotary_desc d = rotary_of(q, k, f, a[4], a[5]);
+        const int64_t rows = (q ? q : k)->size(0);
+        need(pos.scalar_type() == at::kInt && pos.dim() == 1 && pos.size(0) == rows && pos.is_contiguous(), "positions: contiguous int32 [rows]");
+        here({&pos});
+        return [d, pq = ptr(q), pk = ptr(k), pp = ptr(pos), rows = cut(rows), pf = ptr(f), st = stream()] {
+            return lib.rotary(pq, pk, static_cast<int32_t*>(pp), rows, static_cast<double*>(pf), &d, st);
+        };
+    });
+}
+
+// q, k, cu_seqlens_q, seq_lens, num_prefill_seqs, frequencies, pairs, magnitude
+SHIFTATTN_CALL(rotary_mixed) {
+    return run(n, 8, [&] {
+        const at::Tensor *q = tensor_or_none(a[0]), *k = tensor_or_none(a[1]);
+        const at::Tensor &cu = tensor(a[2]), &lens = tensor(a[3]), &f = tensor(a[5]);
+        const int64_t chunks = whole(a[4]);
+        const shiftattn_rotary_desc d = rotary_of(q, k, f, a[6], a[7]);
+        need(cu.scalar_type() == at::kInt && lens.scalar_type() == at::kInt && cu.dim() == 1 && lens.dim() == 1 && cu.is_contiguous() && lens.is_contiguous(),
+             "cu_seqlens_q, seq_lens: contiguous int32");
+        const int64_t decodes = lens.size(0) - chunks, chunk_rows = (q ? q : k)->size(0) - decodes;
+        need(chunks >= 0 && decodes >= 0 && chunk_rows >= 0 && cu.size(0) == chunks + 1, "cu_seqlens_q: [num_prefill_seqs + 1], one row per other sequence");
+        here({&cu, &lens});
+        return [d, pq = ptr(q), pk = ptr(k), pu = ptr(cu), pl = ptr(lens), chunks = cut(chunks), chunk_rows = cut(chunk_rows), decodes = cut(decodes), pf = ptr(f),
+                st = stream()] {
+            return lib.rotary_mixed(pq, pk, static_cast<int32_t*>(pu), static_cast<int32_t*>(pl), chunks, chunk_rows, decodes, static_cast<double*>(pf), &d, st);
+        };
+    });
+}
+
+// q, kv_cache, block_table, seq_lens, max_seq_len, group_offsets, shared_lens, out, softmax_scale, k_new, v_new, slot_mapping, workspace,
+// k_scale, v_scale, kv_scales
+SHIFTATTN_CALL(decode_shared) {
+    Owned own;
+    return run(n, 16, [&] {
+        const at::Tensor &q = tensor(a[0]), &cache = tensor(a[1]), &table = tensor(a[2]), &lens = tensor(a[3]), &out = tensor(a[7]);
+        const at::Tensor &offsets = tensor(a[5]), &shared = tensor(a[6]);
+        const at::Tensor *k = tensor_or_none(a[9]), *v = tensor_or_none(a[10]), *slots = tensor_or_none(a[11]);
+        dims(q, 3, "q");
+        need(lens.scalar_type() == at::kInt && lens.dim() == 1 && lens.size(0) == q.size(0) && lens.is_contiguous(), "seq_lens: contiguous int32 [num_seqs]");
+        need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type(), "out: shape and type of q");
+        need(offsets.scalar_type() == at::kInt && shared.scalar_type() == at::kInt && offsets.dim() == 1 && shared.dim() == 1 && offsets.is_contiguous() &&
+                 shared.is_contiguous() && offsets.size(0) == shared.size(0) + 1,
+             "group_offsets, shared_lens: contiguous int32 [num_groups + 1], [num_groups]");
+        const at::Tensor* scales = tensor_or_none(a[15]);
+        const shiftattn_attn d = describe(q, cache, table, a[8], k, &out, a[13], a[14], scales);
+        need(table.size(0) >= q.size(0), "block_table: a row per sequence");
+        rows_of(q, out, k, v, slots, cache);
+        const int32_t ms = whole(a[4]), groups = cut(shared.size(0));
+        here({&q, &cache, &table, &lens, &out, &offsets, &shared, k, v, slots, scales});
+        const at::Tensor* ws = workspace(a[12], a[0], own, [&] { return lib.shared_bytes(cut(q.size(0)), ms, groups, &d); });
+        here({ws});
+        return [d, pq = ptr(q), pk = ptr(k), pv = ptr(v), ps = ptr(slots), pc = ptr(cache), pt = ptr(table), pl = ptr(lens), seqs = cut(q.size(0)), ms,
+                pg = ptr(offsets), ph = ptr(shared), groups, po = ptr(out), pw = ptr(ws), nw = bytes(ws), st = stream(), pb = static_cast<float*>(ptr(scales))] {
+            return lib.decode_shared(pq, pk, pv, static_cast<int64_t*>(ps), pc, pb, static_cast<int32_t*>(pt), static_cast<int32_t*>(pl), seqs, ms,
+                                     static_cast<int32_t*>(pg), static_cast<int32_t*>(ph), groups, po, pw, nw, &d, st);
+        };
+    });
+}
+
 #define SHIFTATTN_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SHIFTATTN_METHOD(bind), SHIFTATTN_METHOD(pack_seq2head), SHIFTATTN_METHOD(unpack_head2seq), SHIFTATTN_METHOD(prefill),
                          SHIFTATTN_METHOD(decode), SHIFTATTN_METHOD(decode_static), SHIFTATTN_METHOD(mixed), SHIFTATTN_METHOD(kv_write),
@@ -581,7 +704,8 @@ PyMethodDef methods[] = {SHIFTATTN_METHOD(bind), SHIFTATTN_METHOD(pack_seq2head)
                          SHIFTATTN_METHOD(quantize_recv_fp8), SHIFTATTN_METHOD(qkv_proj_pack_fp8), SHIFTATTN_METHOD(unpack_o_proj_fp8),
                          SHIFTATTN_METHOD(attn_desc), SHIFTATTN_METHOD(tables_append), SHIFTATTN_METHOD(tables_truncate),
                          SHIFTATTN_METHOD(quantize_rows_int8), SHIFTATTN_METHOD(quantize_recv_int8), SHIFTATTN_METHOD(qkv_proj_pack_int8),
-                         SHIFTATTN_METHOD(unpack_o_proj_int8),
+                         SHIFTATTN_METHOD(unpack_o_proj_int8), SHIFTATTN_METHOD(add_rms_norm), SHIFTATTN_METHOD(rotary), SHIFTATTN_METHOD(rotary_mixed),
+                         SHIFTATTN_METHOD(decode_shared),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
