@@ -421,7 +421,7 @@ int shiftattn_decode_static(const void *q, const void *k_new, const void *v_new,
  *                 each sequence's own.  <= 0: nothing in common
  *   kv_scales: the scales of a cache with block scales (a->kv_format = SHIFTATTN_KV_FP8_E4M3_BLOCKS), NULL for any other
  *   All else as in shiftattn_decode; a token that is appended must lie behind the blocks in common.
- * bf16 rows with head_dim 128 and up to 16 query heads per KV head, and up to 1024 groups, take the kernel that shares; any other call is
+ * bf16 rows with head_dim 128 and up to 16 query heads per KV head, and up to 512 groups, take the kernel that shares; any other call is
  * served as the plain one.  workspace: shiftattn_decode_shared_workspace_bytes(...) bytes, 16-byte aligned. */
 int shiftattn_decode_shared(const void *q, const void *k_new, const void *v_new, const int64_t *slot_mapping, void *kv_cache,
                             float *kv_scales, const int32_t *block_table, const int32_t *seq_lens, int32_t num_seqs,

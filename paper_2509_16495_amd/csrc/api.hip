@@ -182,6 +182,10 @@ bool use_decode_mfma(const AttnShape& s, int num_seqs, int max_seq_len) {
     return !force_generic() && decode_mfma_supported(s, num_seqs, max_seq_len);
 }
 
+bool use_decode_shared(const AttnShape& s, int num_seqs, int max_seq_len, int num_groups) {
+    return !force_generic() && decode_shared_supported(s, num_seqs, max_seq_len, num_groups);
+}
+
 // Argument checks of a prefill / decode call that need no launch (shared with the mixed entry point, which must
 // not have written the cache when one of them fails).
 int check_prefill_args(const void* q, const void* kv_cache, const int32_t* block_table, const int32_t* cu_seqlens_q,
@@ -915,13 +919,26 @@ int shiftattn_decode_shared(const void* q, const void* k_new, const void* v_new,
     if (num_groups < 0) return fail(SHIFTATTN_EINVAL, "num_groups = %d", num_groups);
     if (num_groups > 0 && (!group_offsets || !shared_lens || !aligned_to(group_offsets, 4) || !aligned_to(shared_lens, 4)))
         return fail(SHIFTATTN_EINVAL, "group_offsets or shared_lens is NULL or not 4-byte aligned");
-    return decode(s.block_scales, kv_scales, q, k_new, v_new, slot_mapping, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, out,
-                  workspace, workspace_bytes, a, stream);
+    if (num_seqs <= 0 || max_seq_len < 0 || !use_decode_shared(s, num_seqs, max_seq_len, num_groups))
+        return decode(s.block_scales, kv_scales, q, k_new, v_new, slot_mapping, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, out,
+                      workspace, workspace_bytes, a, stream);
+    if (int rc = check_scales(s.block_scales, kv_scales, &s)) return rc;
+    bool new_kv;
+    if (int rc = check_new_kv(k_new, v_new, slot_mapping, &new_kv)) return rc;
+    if (int rc = check_decode_args(q, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, out, s)) return rc;
+    const size_t need = decode_shared_workspace(num_seqs, max_seq_len, num_groups, s);
+    if (!workspace || workspace_bytes < need || !aligned16(workspace))
+        return fail(SHIFTATTN_EWORKSPACE, "decode_shared needs %zu workspace bytes, got %zu", need, workspace ? workspace_bytes : static_cast<size_t>(0));
+    hipError_t e = launch_decode_shared(q, k_new, v_new, slot_mapping, kv_cache, block_table, seq_lens, num_seqs, max_seq_len, group_offsets,
+                                        shared_lens, num_groups, out, workspace, s, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SHIFTATTN_OK : hip_fail(e, "decode_shared launch");
 }
 
 size_t shiftattn_decode_shared_workspace_bytes(int32_t num_seqs, int32_t max_seq_len, int32_t num_groups, const shiftattn_attn* a) {
-    if (num_groups < 0) return SIZE_MAX;
-    return shiftattn_decode_workspace_bytes(num_seqs, max_seq_len, a);
+    AttnShape s;
+    if (check_attn(a, &s) || num_seqs < 0 || max_seq_len < 0 || num_groups < 0) return SIZE_MAX;
+    if (num_seqs == 0 || !use_decode_shared(s, num_seqs, max_seq_len, num_groups)) return shiftattn_decode_workspace_bytes(num_seqs, max_seq_len, a);
+    return decode_shared_workspace(num_seqs, max_seq_len, num_groups, s);
 }
 
 int shiftattn_decode_static(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,

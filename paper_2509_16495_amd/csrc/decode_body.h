@@ -116,29 +116,33 @@ struct AppendArgs {
 // beside chunks would else make them 1.5 % less exact than in a launch of their own (20 unified batches, two seeds each, relative
 // 2-norm against float64: 2.12e-3 against 2.09e-3; with it 2.03e-3), at the same speed.
 // kScales: block scales of an FP8 cache: 0 none, 1 there are some, 2 there are if `scales` is set.
-template <bool kFp8, bool kAppend, int kWaves, bool kGroupRef, int kScales = 0>
+// kMaxPairs: pairs that the index holds (kMaxPairs + 1 + 16 ints).  kFrom: a sequence's first from[s] blocks are another's work (LDS;
+// fewer tokens than it has): the rows attend to the tokens behind them.
+template <bool kFp8, bool kAppend, int kWaves, bool kGroupRef, int kScales = 0, int kMaxPairs = kFlatMaxPairs, bool kFrom = false>
 __device__ __attribute__((always_inline)) inline void decode_flat_body(
     const uint16_t* __restrict__ q, int64_t q_stride, uint16_t* __restrict__ cache,
     const int32_t* __restrict__ block_table, int max_blocks, const int32_t* __restrict__ seq_lens,
     float* __restrict__ o_part, float* __restrict__ ml_part, int2* __restrict__ plan, int num_seqs, int hq_l, int hkv_l,
-    float c, int r_min, const AppendArgs& ap, unsigned char* smem, int* index, int wg, int n_wg, const float* __restrict__ scales = nullptr) {
+    float c, int r_min, const AppendArgs& ap, unsigned char* smem, int* index, int wg, int n_wg, const float* __restrict__ scales = nullptr,
+    const int* from = nullptr) {
     constexpr bool kBlockScales = kScales != 0;
     static_assert(!kBlockScales || kFp8, "block scales belong to FP8 codes");
-    int* cum = index;                             // [kFlatMaxPairs + 1]
-    int* wave_sum = index + kFlatMaxPairs + 1;    // [kWaves]
+    int* cum = index;                         // [kMaxPairs + 1]
+    int* wave_sum = index + kMaxPairs + 1;    // [kWaves]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int n_pairs = num_seqs * hkv_l;
     const int G = hq_l / hkv_l;
 
     // ---- padded prefix sums of the context lengths: thread t owns kPer pairs from kPer t on -----
     {
-        constexpr int kPer = kFlatMaxPairs / (kWaves * 64);  // 8 with four wavefronts, 4 with eight
+        constexpr int kPer = kMaxPairs / (kWaves * 64);  // 2048 pairs: 8 with four wavefronts, 4 with eight
         int len[kPer], pad[kPer];
         int mine = 0;
 #pragma unroll
         for (int x = 0; x < kPer; ++x) {
             const int i = threadIdx.x * kPer + x;
             len[x] = i < n_pairs ? max(seq_lens[i / hkv_l], 0) : 0;
+            if constexpr (kFrom) len[x] = max(len[x] - (i < n_pairs ? kBlockSize * from[i / hkv_l] : 0), 0);
         }
 #pragma unroll
         for (int x = 0; x < kPer; ++x) {
@@ -267,6 +271,7 @@ __device__ __attribute__((always_inline)) inline void decode_flat_body(
         const int b0 = (ps - sb) / kBlockSize;
         const int last_block = (cx - 1) / kBlockSize;
         const int32_t* table = block_table + static_cast<size_t>(s) * max_blocks;
+        if constexpr (kFrom) table += __builtin_amdgcn_readfirstlane(from[s]);
         blk0 = table[b0];
         blk1 = table[min(b0 + 1, last_block)];
     };

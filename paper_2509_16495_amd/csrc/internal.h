@@ -126,6 +126,13 @@ hipError_t launch_decode_mfma(const void* q, const void* k_new, const void* v_ne
                               const int32_t* block_table, const int32_t* seq_lens, int num_seqs, int max_seq_len,
                               void* out, void* workspace, const AttnShape& a, hipStream_t st);
 
+// decode_shared.hip : the same operation where groups of sequences have the first blocks of their tables in common
+bool decode_shared_supported(const AttnShape& a, int num_seqs, int max_seq_len, int num_groups);
+size_t decode_shared_workspace(int num_seqs, int max_seq_len, int num_groups, const AttnShape& a);
+hipError_t launch_decode_shared(const void* q, const void* k_new, const void* v_new, const int64_t* slots, void* cache, const int32_t* block_table,
+                                const int32_t* seq_lens, int num_seqs, int max_seq_len, const int32_t* group_offsets, const int32_t* shared_lens,
+                                int num_groups, void* out, void* workspace, const AttnShape& a, hipStream_t st);
+
 // prefill_mfma.hip : bf16 q/out, D = 128; cache bf16, or FP8 E4M3 widened into workspace first
 bool prefill_mfma_supported(const AttnShape& a, int num_seqs, int max_seq_len);
 // the workspace with which a launch takes the plan that is fastest, and the least one it is accepted with (it then takes

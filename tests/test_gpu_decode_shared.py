@@ -1,0 +1,342 @@
+"""Decode behind shared prefixes: against softmax attention in 64 bits over what the cache holds, and against the plain decode call.
+
+How far an output may be off: a probability is rounded to bf16 against its range's reference, by at most 2^-8 of it, so the numerator by
+2^-8 sum_t p_t |v_t|; the output is rounded once more, by at most 2^-8 of it; logits are float32 sums of 128 exact products (the drift
+below: 16 roundings of 2^-24 of at most sum |q_i k_i| scale, which moves a probability and the sum under it); exp2 and the float32
+sums add below 1e-5 of sum_t p_t |v_t| at these lengths.  Float32 rows have no bf16 roundings: 2^-20 stands for exp and their sums."""
+import math
+
+import numpy as np
+import pytest
+
+import plain_8bit as P
+
+pytestmark = pytest.mark.gpu
+DEV, BLOCK = "cuda:0", 16
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2509_16495_amd import binding
+    binding.lib()
+    return binding
+
+
+class Case:
+    """A batch on the host: groups of (shared tokens, lengths); a length <= 0 is a padding row whose table row is nonsense."""
+
+    def __init__(self, groups, alone=(), hq=8, hkv=1, D=128, dtype="bf16", cache="same", seed=1, alone_first=False, spread=1.0, loose=0):
+        rng = self.rng = np.random.Generator(np.random.PCG64(seed))
+        self.hq, self.hkv, self.D, self.dtype, self.kind = hq, hkv, D, dtype, cache
+        lens, sizes, shared = [], [], []
+        if alone_first:
+            lens += list(alone)
+        first = len(lens)
+        for pre, members in groups:
+            shared.append(pre)
+            sizes.append(len(members))
+            lens += list(members)
+        if not alone_first:
+            lens += list(alone)
+        self.lens, self.shared_lens = np.array(lens, np.int64), np.array(shared, np.int64)
+        self.offsets = first + np.concatenate([[0], np.cumsum(sizes)]).astype(np.int64)
+        n = len(lens)
+        self.wide = max(1, max((max(l, 0) + BLOCK - 1) // BLOCK for l in lens)) + loose
+        need = sum((max(l, 0) + BLOCK - 1) // BLOCK for l in lens) + 3
+        order = list(rng.permutation(need))
+        self.num_blocks = need
+        self.table = rng.integers(0, need, (n, self.wide))
+        for s, l in enumerate(lens):
+            for i in range((max(l, 0) + BLOCK - 1) // BLOCK):
+                self.table[s, i] = order.pop()
+        for g, pre in enumerate(shared):
+            members = [s for s in range(self.offsets[g], self.offsets[g + 1]) if lens[s] > 0]
+            for s in members[1:]:
+                most = min(pre // BLOCK, (lens[members[0]] - 1) // BLOCK, (lens[s] - 1) // BLOCK)
+                self.table[s, :max(most, 0)] = self.table[members[0], :max(most, 0)]
+                # (a longer member than the first: the rest of the common blocks are its own, so the call's claim ends where the shortest does)
+            if members:
+                assert min(lens[s] for s in members) > 0
+        for s, l in enumerate(lens):
+            if l <= 0:
+                self.table[s] = -(10 ** 6)      # never read
+        rnd = lambda *sh: P.bf16(rng.standard_normal(sh).astype(np.float32)) if dtype == "bf16" else rng.standard_normal(sh).astype(np.float32)
+        self.q, self.k_new, self.v_new = rnd(n, hq, D) * np.float32(spread), rnd(n, hkv, D), rnd(n, hkv, D)
+        if dtype == "bf16":
+            self.q = P.bf16(self.q)
+        self.slots = np.array([self.table[s, (l - 1) // BLOCK] * BLOCK + (l - 1) % BLOCK if l > 0 else -1 for s, l in enumerate(lens)], np.int64)
+        self.factors = (1.0, 1.0)
+        if cache == "same":
+            self.pages = rnd(need, hkv, 2, BLOCK, D)                    # [block, head, part, token, d], values
+        else:
+            self.codes = rng.integers(0, 256, (need, hkv, 2, BLOCK, D)).astype(np.uint8)
+            self.codes[(self.codes & 0x7F) == 0x7F] = 0x30
+            self.codes[(self.codes & 0x78) > 0x48] &= 0xBF                   # magnitudes below 8
+            if cache == "fp8":
+                self.factors = (0.25, 0.5)
+                self.scales = None
+            else:
+                self.scales = (2.0 ** rng.integers(-4, 1, (need, hkv, 2))).astype(np.float32)
+        self.scale = 1.0 / math.sqrt(D)
+
+    def device(self):
+        import torch
+        t = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+        dt = torch.bfloat16 if self.dtype == "bf16" else torch.float32
+        d = {}
+        d["rows"] = torch.cat([t(self.q), t(self.k_new), t(self.v_new)], 1).to(dt)
+        d["q"], d["k"], d["v"] = d["rows"][:, :self.hq], d["rows"][:, self.hq:self.hq + self.hkv], d["rows"][:, self.hq + self.hkv:]
+        pages = self.pages if self.kind == "same" else self.codes
+        flat = np.stack([pages[:, :, 0].reshape(*pages.shape[:2], -1), pages[:, :, 1].swapaxes(2, 3).reshape(*pages.shape[:2], -1)], 2)
+        d["cache"] = t(flat).to(dt) if self.kind == "same" else t(flat)
+        d["scales"] = t(self.scales) if self.kind == "blocks" else None
+        i = lambda a: t(np.asarray(a, np.int32))
+        d["table"], d["lens"], d["offsets"], d["shared"] = i(self.table), i(self.lens), i(self.offsets), i(self.shared_lens)
+        d["slots"] = t(self.slots)
+        d["out"] = torch.full((len(self.lens), self.hq, self.D), 7.0, dtype=dt, device=DEV)
+        return d
+
+    def call(self, B, d, append=True, shared=True, workspace=None, **kw):
+        new = dict(k_new=d["k"], v_new=d["v"], slot_mapping=d["slots"]) if append else {}
+        new.update(workspace=workspace, k_scale=self.factors[0], v_scale=self.factors[1], kv_scales=d["scales"])
+        ms = int(max(self.lens.max(), 0))
+        if shared:
+            B.decode_shared(d["q"], d["cache"], d["table"], d["lens"], ms, kw.get("offsets", d["offsets"]), kw.get("shared", d["shared"]), d["out"], self.scale, **new)
+        else:
+            B.decode(d["q"], d["cache"], d["table"], d["lens"], ms, d["out"], self.scale, **new)
+
+    def values(self, d):
+        """[block, head, part, token, d] in 64 bits of what the cache on the device holds."""
+        c = d["cache"].cpu()
+        c = c.double().numpy() if self.kind == "same" else P.e4m3_values()[c.numpy()]
+        n, h = c.shape[:2]
+        v = np.stack([c[:, :, 0].reshape(n, h, BLOCK, self.D), c[:, :, 1].reshape(n, h, self.D, BLOCK).swapaxes(2, 3)], 2)
+        if self.kind == "blocks":
+            v = v * d["scales"].cpu().double().numpy()[..., None, None]
+        return v * np.array(self.factors)[None, None, :, None, None]
+
+    def check(self, d):
+        """The device's outputs against 64 bits over the cache as it is now."""
+        import torch
+        torch.cuda.synchronize()
+        out, pages, G = d["out"].double().cpu().numpy(), self.values(d), self.hq // self.hkv
+        eps = 2.0 ** -8 if self.dtype == "bf16" else 2.0 ** -20
+        for s, l in enumerate(self.lens):
+            if l <= 0:
+                assert (out[s] == 0).all(), s
+                continue
+            kv = pages[self.table[s, :(l + BLOCK - 1) // BLOCK]]                    # [blocks, head, part, token, d]
+            for g in range(self.hkv):
+                k, v = (kv[:, g, x].reshape(-1, self.D)[:l] for x in (0, 1))
+                q = self.q[s, g * G:(g + 1) * G].astype(np.float64)
+                z = q @ k.T * self.scale
+                p = np.exp(z - z.max(-1, keepdims=True))
+                p /= p.sum(-1, keepdims=True)
+                want, size = p @ v, p @ np.abs(v)
+                # logits in float32: 128 products and sums, 2^-24 each of at most sum |q_i k_i| scale
+                drift = np.expm1(2.0 ** -24 * 16 * (np.abs(q) @ np.abs(k).T * self.scale).max(-1, keepdims=True))
+                bound = (eps + 1e-5 + 2 * drift) * size + eps * np.abs(want) + 1e-30
+                bad = np.abs(out[s, g * G:(g + 1) * G] - want) > bound
+                assert not bad.any(), (s, g, np.abs(out[s, g * G:(g + 1) * G] - want).max(), bound.max(), int(bad.sum()))
+
+
+BATCHES = {
+    "pair": dict(groups=[(32, [33, 40])]),
+    "one block": dict(groups=[(16, [17, 18, 30])]),
+    "nothing whole in common": dict(groups=[(15, [20, 33]), (0, [5, 6]), (-4, [40, 41])]),
+    "four answers": dict(groups=[(1000, [1003, 1100, 1001, 1064])]),
+    "no multiple of a step": dict(groups=[(64 * 5 + 16, [400, 401, 352, 337]), (64 * 3 + 48, [300, 241])]),
+    "tile edges": dict(groups=[(300, [320] * 8), (300, [310] * 9), (333, [340] * 16), (330, [345] * 17)]),
+    "alone behind": dict(groups=[(500, [520, 600, 777])], alone=[1, 16, 17, 900, 33]),
+    "alone in front": dict(groups=[(500, [520, 600, 777]), (64, [65, 66])], alone=[1, 16, 1900], alone_first=True),
+    "alone only": dict(groups=[(300, [301])], alone=[7, 3000]),
+    "padding": dict(groups=[(200, [0, 210, -1, 260, 0]), (100, [0, 0]), (90, [101, 0])], alone=[0, 12]),
+    "all padding": dict(groups=[(200, [0, -5])], alone=[0]),
+    "empty groups": dict(groups=[(200, []), (200, [230, 240]), (9, []), (50, []), (100, [120, 130, 101])]),
+    "a member that is shorter": dict(groups=[(600, [700, 100, 650])]),
+    "a shared length behind every member": dict(groups=[(5000, [161, 170, 200])]),
+    "ends with a block": dict(groups=[(160, [176, 161, 192])]),
+    "many groups": dict(groups=[(48 + 16 * (i % 5), [140 + i % 7, 150, 141]) for i in range(70)]),
+    "long": dict(groups=[(40000, [40010, 40700, 41000]), (9000, [9100] * 5)], alone=[30000]),
+    "large group": dict(groups=[(700, [701 + i for i in range(150)])]),
+}
+
+
+@pytest.mark.parametrize("cache", ["same", "fp8", "blocks"])
+@pytest.mark.parametrize("name", BATCHES)
+def test_batches(B, name, cache):
+    case = Case(seed=len(name), cache=cache, **BATCHES[name])
+    d = case.device()
+    case.call(B, d)
+    case.check(d)
+    # the cache is what the plain call leaves
+    e = case.device()
+    case.call(B, e, shared=False)
+    import torch
+    torch.cuda.synchronize()
+    assert torch.equal(d["cache"].view(torch.uint8), e["cache"].view(torch.uint8))
+    assert cache != "blocks" or torch.equal(d["scales"], e["scales"])
+    if d["out"].numel():
+        assert (d["out"].float() - e["out"].float()).abs().max() <= 0.05
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (5, 1), (16, 1), (3, 3), (16, 2), (10, 2), (32, 8), (12, 4)])
+def test_heads(B, hq, hkv):
+    case = Case([(150, [160, 170, 155]), (333, [340 + i for i in range(13)])], [40], hq, hkv, seed=hq, spread=2.0)
+    d = case.device()
+    case.call(B, d)
+    case.check(d)
+
+
+@pytest.mark.parametrize("hq,hkv,D,dtype,cache", [(4, 1, 64, "bf16", "same"), (4, 2, 128, "f32", "same"), (32, 1, 128, "bf16", "same"), (2, 1, 256, "bf16", "same"), (4, 1, 64, "f32", "blocks")])
+def test_shapes_that_take_the_plain_kernels(B, hq, hkv, D, dtype, cache):
+    case = Case([(64, [70, 80]), (32, [33, 0])], [5], hq, hkv, D, dtype, cache, seed=D)
+    d = case.device()
+    case.call(B, d)
+    case.check(d)
+
+
+def test_without_an_append_and_with_some_rows_that_append_nothing(B):
+    import torch
+    case = Case([(200, [208, 224, 300]), (64, [80, 81])], [17], seed=3)
+    d = case.device()
+    before = d["cache"].clone()
+    case.call(B, d, append=False)
+    case.check(d)
+    assert torch.equal(before.view(torch.uint8), d["cache"].view(torch.uint8))
+    d["slots"][1] = d["slots"][4] = -1
+    case.call(B, d)
+    case.check(d)
+
+
+@pytest.mark.parametrize("cache", ["same", "blocks"])
+def test_more_pairs_than_one_launch_takes(B, cache):
+    """Runs of 256 sequences of four KV heads; groups are cut where a run ends."""
+    groups = [(48, [60 + (i + g) % 9 for i in range(40 + 37 * (g % 3))]) for g in range(9)]
+    case = Case(groups, [33] * 11, 8, 4, cache=cache, seed=7)
+    assert len(case.lens) > 512
+    d = case.device()
+    case.call(B, d)
+    case.check(d)
+
+
+def test_more_groups_than_the_index_holds(B):
+    case = Case([(32, [33 + i % 3]) for i in range(513)], seed=8)
+    d = case.device()
+    case.call(B, d)
+    case.check(d)
+    case = Case([(32, [35 + i % 3] * (1 + i % 2)) for i in range(512)], seed=9)
+    d = case.device()
+    case.call(B, d)
+    case.check(d)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_what_no_row_sees_does_not_matter(B, bad):
+    """Slots behind the last token and other sequences' blocks hold infinities and NaN."""
+    import torch
+    case = Case([(100, [130, 120, 109]), (64, [70, 77])], [21], seed=11)
+    good, d = case.device(), case.device()
+    seen = np.zeros((case.num_blocks, BLOCK), bool)
+    for s, l in enumerate(case.lens):
+        p = np.arange(l)
+        seen[case.table[s, p // BLOCK], p % BLOCK] = True
+    pages = case.pages.copy()
+    pages[~np.broadcast_to(seen[:, None, None, :, None], pages.shape)] = bad
+    case.pages = pages
+    d = case.device()
+    case.call(B, good)
+    case.call(B, d)
+    torch.cuda.synchronize()
+    assert torch.equal(good["out"], d["out"])
+
+
+def test_logits_of_minus_infinity_and_far_apart(B):
+    """Keys that no query likes at all: whole steps without weight, in front of and behind those that have it."""
+    import torch
+    for flip in (False, True):
+        case = Case([(640, [650, 700, 660])], seed=12)
+        case.q[...] = 1
+        dead = case.table[0, :20] if flip else case.table[0, 20:40]
+        case.pages[dead, :, 0] = -np.inf
+        d = case.device()
+        case.call(B, d)
+        torch.cuda.synchronize()
+        alive = Case([(640, [650, 700, 660])], seed=12)
+        alive.q[...] = 1
+        alive.pages[dead, :, 0] = -3e5        # a logit of -3e6: no weight either
+        e = alive.device()
+        alive.call(B, e)
+        alive.check(e)
+        assert torch.equal(d["out"], e["out"])
+
+
+def test_strided_rows_of_any_kind(B):
+    import torch
+    case = Case([(128, [130, 150, 140])], [20], 8, 2, seed=13)
+    d = case.device()
+    wide = torch.zeros((len(case.lens), 21, 128), dtype=torch.bfloat16, device=DEV)
+    wide[:, 1:13] = d["rows"]
+    d["q"], d["k"], d["v"] = wide[:, 1:9], wide[:, 9:11], wide[:, 11:13]
+    full = torch.full((len(case.lens), 11, 128), 5.0, dtype=torch.bfloat16, device=DEV)
+    d["out"] = full[:, 2:10]
+    case.call(B, d)
+    case.check(d)
+    assert (full[:, :2] == 5).all() and (full[:, 10:] == 5).all()
+
+
+def test_results_are_the_same_bits_each_time(B):
+    import torch
+    case = Case([(3000, [3010 + i for i in range(21)]), (500, [600] * 3)], [700], seed=14)
+    outs = []
+    for _ in range(4):
+        d = case.device()
+        case.call(B, d)
+        torch.cuda.synchronize()
+        outs.append(d["out"].clone())
+    assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+def test_groups_that_change_between_replays(B):
+    """A captured call follows the offsets, shared lengths, tables and lengths that are in device memory when it is replayed."""
+    import torch
+    cases = [Case([(300, [320 + i for i in range(6)]), (0, [])], [50, 400], seed=s, loose=l) for s, l in ((20, 5), (21, 5))]
+    other = Case([(64, [70, 75]), (200, [330, 240, 250, 260])], [17, 325], seed=22, loose=0)
+    n = len(other.lens)
+    assert all(len(c.lens) == n for c in cases)
+    ds = [c.device() for c in cases] + [other.device()]
+    width, blocks = max(d["table"].shape[1] for d in ds), max(d["cache"].shape[0] for d in ds)
+    buf = {k: v.clone() for k, v in ds[0].items() if k in ("rows", "lens", "offsets", "shared", "slots", "out")}
+    buf["table"] = torch.zeros((n, width), dtype=torch.int32, device=DEV)
+    buf["cache"] = torch.zeros((blocks,) + tuple(ds[0]["cache"].shape[1:]), dtype=torch.bfloat16, device=DEV)
+    q, k, v = buf["rows"][:, :8], buf["rows"][:, 8:9], buf["rows"][:, 9:]
+    a = B.attn_desc(q, buf["cache"], buf["table"], cases[0].scale, k, buf["out"])
+    ws = torch.empty(B.decode_shared_workspace_bytes(n, 480, 2, a), dtype=torch.uint8, device=DEV)
+    step = lambda: B.decode_shared(q, buf["cache"], buf["table"], buf["lens"], 480, buf["offsets"], buf["shared"], buf["out"], cases[0].scale, k, v, buf["slots"], ws)
+
+    def fill(d):
+        for name in ("rows", "lens", "offsets", "shared", "slots"):
+            buf[name].copy_(d[name])
+        buf["table"].zero_()
+        buf["table"][:, :d["table"].shape[1]] = d["table"]
+        buf["cache"].zero_()
+        buf["cache"][:d["cache"].shape[0]] = d["cache"]
+    fill(ds[0])
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for c, d in list(zip(cases + [other], ds)) * 2:
+        fill(d)
+        step()
+        torch.cuda.synchronize()
+        want = buf["out"].clone(), buf["cache"].clone()
+        fill(d)
+        buf["out"].zero_()
+        _ = (d["q"].float() * 2).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(buf["out"], want[0]) and torch.equal(buf["cache"], want[1])
+        view = dict(d, out=buf["out"], cache=buf["cache"][:d["cache"].shape[0]])
+        c.check(view)
