@@ -422,7 +422,7 @@ int shiftattn_decode_static(const void *q, const void *k_new, const void *v_new,
  *   kv_scales: the scales of a cache with block scales (a->kv_format = SHIFTATTN_KV_FP8_E4M3_BLOCKS), NULL for any other
  *   All else as in shiftattn_decode; a token that is appended must lie behind the blocks in common.
  * bf16 rows with head_dim 128 and up to 16 query heads per KV head, and up to 512 groups, take the kernel that shares; any other call is
- * served as the plain one.  workspace: shiftattn_decode_shared_workspace_bytes(...) bytes, 16-byte aligned. */
+ * served as the plain one, and so is a small batch (num_seqs * max_seq_len tokens of up to 40 MB of cache), where the plain one is faster.  workspace: shiftattn_decode_shared_workspace_bytes(...) bytes, 16-byte aligned. */
 int shiftattn_decode_shared(const void *q, const void *k_new, const void *v_new, const int64_t *slot_mapping, void *kv_cache,
                             float *kv_scales, const int32_t *block_table, const int32_t *seq_lens, int32_t num_seqs,
                             int32_t max_seq_len, const int32_t *group_offsets, const int32_t *shared_lens, int32_t num_groups,
@@ -560,9 +560,11 @@ int32_t shiftattn_use_base_config(int32_t n_tokens, int32_t threshold);
  *                                probability of a row is no longer exactly 1: outputs of magnitude 2 and more
  *                                can land one bf16 step from the correctly rounded value.  Tiles whose softmax
  *                                sums leave [2^-40, 2^40] are recomputed on Q as given.  Off by default
+ *   SHIFTATTN_OPT_DECODE_SHARED  1 | 2: shiftattn_decode_shared takes the kernel that shares wherever it can (1), or never (2),
+ *                                whatever the size of the batch
  *   set returns EINVAL for an unknown option or value; get returns -1 for an unknown option. */
 enum { SHIFTATTN_OPT_PREFILL_TILE = 0, SHIFTATTN_OPT_PREFILL_SPLITS = 1, SHIFTATTN_OPT_GENERIC_ONLY = 2,
-       SHIFTATTN_OPT_PREFILL_PAIRING = 3, SHIFTATTN_OPT_PREFILL_SCALED_Q = 4, SHIFTATTN_OPT_COUNT = 5 };
+       SHIFTATTN_OPT_PREFILL_PAIRING = 3, SHIFTATTN_OPT_PREFILL_SCALED_Q = 4, SHIFTATTN_OPT_DECODE_SHARED = 5, SHIFTATTN_OPT_COUNT = 6 };
 int shiftattn_init(void);
 int shiftattn_set_option(int32_t option, int32_t value);
 int32_t shiftattn_get_option(int32_t option);

@@ -11,22 +11,27 @@ constexpr int kWaves = 4;
 constexpr int kWorkgroups = 512;      // two resident per compute unit
 constexpr int kMaxPairs = 1024;       // (sequence, KV head) pairs of a launch
 constexpr int kMaxGroups = 512;
-constexpr int kStep = 64;             // keys a workgroup takes at once: four blocks, one loaded by each wavefront
-constexpr int kTileCols = 128;        // (sequence, head) columns of a tile; groups of up to 64 take the two halves of a step's keys apart
-constexpr int kMaxRanges = 240;       // ranges that the shared keys of a tile are cut into
-constexpr int kMinSteps = 4;          // steps of a range
-constexpr int kPrefixWeight = 1, kSuffixWeight = 3;   // time of a step, and of 32 tokens for each of a workgroup's wavefronts
+constexpr int64_t kPlainBytes = 40000000;   // cache up to which a batch is the plain kernel's
+constexpr int kMostShared = 508;      // of which take shared keys at most
+constexpr int kStep = 64;             // keys that shared ranges are counted in
+constexpr int kTileCols = 128;        // (sequence, head) columns of a tile whose keys a workgroup's wavefronts share
+constexpr int kNarrowCols = 32;       // and of one that every wavefront takes with keys of its own, where a group has no more than kNarrowMost
+constexpr int kNarrowMost = 64;
+constexpr int kMaxRanges = 480;       // ranges that the shared keys of a tile are cut into
+constexpr int kMinSteps = 2;          // steps of a range
+constexpr float kRangeRoot = 0.25f;   // least steps of a range, by the square root of a group's steps
+constexpr int kWideCost = 3, kNarrowCost = 1, kOwnCost = 2;   // time of a step of either kind of tile, and of 32 tokens for each of a workgroup's wavefronts
 
-// the shared part of a sequence, for the merge: items (tile, KV head) of its group start at line0, `steps` each
+// the shared part of a sequence, for the merge: `parts` partial results in units base + (tile + tiles * head) * ranges and on
 struct alignas(32) SharedRow {
-    int line0, steps, tiles, base, col0, range, wide, reserved;   // tiles 0: it shares nothing
+    int base, ranges, parts, tiles, col0, cols, reserved[2];   // tiles 0: it shares nothing; cols: of a tile
 };
 
 struct GroupIndex {
-    int eff[kMaxGroups];               // blocks in common
-    int line[kMaxGroups + 1];          // steps of all items of the groups in front
-    uint16_t offs[kMaxGroups + 1], base[kMaxGroups + 1], leader[kMaxGroups];   // first sequence, items in front, the sequence whose table is read
-    int sums[2][kWaves];
+    int eff[kMaxGroups];                                       // blocks in common
+    int units[kMaxGroups + 1];                                 // units (tile, KV head, range) of the groups in front
+    uint16_t offs[kMaxGroups + 1], ranges[kMaxGroups], leader[kMaxGroups];   // first sequence, ranges of an item, the sequence whose table is read
+    int sums[3][kWaves];
 };
 
 struct SharedArgs {
@@ -40,7 +45,7 @@ struct SharedArgs {
     float* o_part;        // partial results of the sequences' own keys, as in decode_flat_body
     float* ml_part;
     int2* plan;
-    float* o_shared;      // [workgroup + item][column][D], and (reference, sum) pairs
+    float* o_shared;      // [unit][column of the tile][D], and (reference, sum) pairs
     float* ml_shared;
     SharedRow* rows;
     int64_t q_stride;
@@ -58,261 +63,486 @@ __device__ inline int wave_scan(int v) {   // inclusive
     return v;
 }
 
-// items (tiles) of a group of m sequences for one KV head
-__device__ inline int tiles_of(int m, int G) { return (m * G + kTileCols - 1) / kTileCols; }
+// columns of a tile of a group that has so many, and its tiles
+__device__ inline int tile_cols(int cols) { return cols > kNarrowMost ? kTileCols : kNarrowCols; }
+__device__ inline int tiles_of(int cols) { return (cols + tile_cols(cols) - 1) / tile_cols(cols); }
 
-// A workgroup's share of the line of shared keys: steps [start, end).
-template <bool kFp8, int kScales>
-__device__ __attribute__((always_inline)) inline void shared_keys_body(const SharedArgs& a, const GroupIndex& gi, unsigned char* smem, int start, int end, int wg) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int G = a.hq_l / a.hkv_l;
-    const int col = lane & 15, grp = lane >> 4;
-    // LDS: two buffers of a step, each two groups of 32 tokens parked as in decode_flat_body (its comment has the layout)
-    const int b = wave & 1;                         // this wavefront's block of its group
-    unsigned char* const park = smem + (wave >> 1) * kStageBytes;
-    int kw[4], kr[4];
-    {
-        const int r0 = lane >> 4, p = lane & 15;
-        const int at = r0 * 256 + ((p ^ r0) << 4);
-        const int tau_a = ((col >> 2) << 3) + (col & 3);
-        const int k_sel = tau_a >> 4, k_off_a = tau_a & 15;
-        const int rat = k_sel * 4096 + k_off_a * 256 + ((grp ^ k_off_a ^ (4 * k_sel)) << 4);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            kw[x] = at ^ (64 * x) ^ (64 * b);
-            kr[x] = rat ^ (64 * x);
-        }
-    }
-    const int vw = 8192 + ((lane ^ ((lane >> 4) & 1)) << 4);
-    const int vr = 8192 + (grp >> 1) * 4096 + (((2 * col + (grp & 1)) ^ ((col >> 3) & 1)) << 4);
-    int kw8 = 0, vw8 = 0;
-    if constexpr (kFp8) {
-        const int r8 = lane >> 3, pc = lane & 7;
-        kw8 = r8 * 256 + (((2 * pc) ^ (r8 & 3) ^ (4 * (lane >> 5))) << 4);
-        const int l31 = lane & 31;
-        vw8 = 8192 + 1024 * (lane >> 5) + (((2 * l31) ^ ((l31 >> 3) & 1)) << 4);
-    }
+// One unit: the keys of blocks [first_block, end_block) of a group's table for one KV head, met by the columns [col_first, col_end) of
+// the group ((sequence, head) pairs of that KV head's heads), up to 128, or up to 32 (kNarrow).
+struct Unit {
+    const int32_t* table;
+    int first_block, end_block, head, col_first, col_end, seq_first, slot;
+};
 
-    // ---- a position on the line: its group, item and the item's first and last step (all scalar) ----
-    struct Item {
-        int group, local, begin, end;
-    };
-    auto item_at = [&](int pos) -> Item {
-        int g = 0;
-        for (int at = 0; at < a.num_groups; at += 64) {   // the last group that starts at or before pos and is not empty
-            const int i = at + lane;
-            const uint64_t m = __builtin_amdgcn_ballot_w64(i < a.num_groups && gi.line[i] <= pos && gi.line[min(i, a.num_groups - 1) + 1] > pos);
-            if (m) {
-                g = at + __builtin_ctzll(m);
-                break;
-            }
-        }
-        g = __builtin_amdgcn_readfirstlane(g);
-        const int line0 = __builtin_amdgcn_readfirstlane(gi.line[g]);
-        const int steps = (__builtin_amdgcn_readfirstlane(gi.eff[g]) + 3) / 4;
-        const int local = (pos - line0) / steps;
-        return {g, local, line0 + local * steps, line0 + (local + 1) * steps};
-    };
-    u32x4 fk[4], fv[4];
-    float sc_k = 1.f, sc_v = 1.f;
-    auto load_step = [&](const Item& it, int pos) {
-        const int eff = __builtin_amdgcn_readfirstlane(gi.eff[it.group]);
-        const int m = __builtin_amdgcn_readfirstlane(gi.offs[it.group + 1]) - __builtin_amdgcn_readfirstlane(gi.offs[it.group]);
-        const int head = it.local / tiles_of(m, G);
-        const int leader = __builtin_amdgcn_readfirstlane(gi.leader[it.group]);
-        const int64_t blk = a.block_table[static_cast<size_t>(leader) * a.max_blocks + min((pos - it.begin) * 4 + wave, eff - 1)];
-        if constexpr (kFp8) {
-            if constexpr (kScales != 0) {
-                sc_k = a.scales[(static_cast<size_t>(blk) * a.hkv_l + head) * 2];
-                sc_v = a.scales[(static_cast<size_t>(blk) * a.hkv_l + head) * 2 + 1];
-            }
-            const u32x4* src = reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(a.cache) + cache_part_offset(blk, head, 0, a.hkv_l, kD)) + lane;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) fk[j] = src[64 * j], fv[j] = src[128 + 64 * j];
-        } else {
-            const u32x4* src = reinterpret_cast<const u32x4*>(a.cache + cache_part_offset(blk, head, 0, a.hkv_l, kD)) + lane;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) fk[j] = src[64 * j], fv[j] = src[256 + 64 * j];
-        }
-    };
-    auto park_step = [&](int buffer) {
-        unsigned char* my = park + buffer * 2 * kStageBytes;
-        if constexpr (kFp8) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                u32x4 lo, hi;
-                widen_fp8(fk[j], lo, hi, sc_k);
-                const int ka = (kw8 ^ (64 * ((2 * j) ^ b))) + 4096 * b + 2048 * j;
-                *reinterpret_cast<u32x4*>(my + ka) = lo;
-                *reinterpret_cast<u32x4*>(my + (ka ^ 16)) = hi;
-                widen_fp8(fv[j], lo, hi, sc_v);
-                const int va = vw8 + 4096 * b + 2048 * j;
-                *reinterpret_cast<u32x4*>(my + va) = lo;
-                *reinterpret_cast<u32x4*>(my + (va ^ 16)) = hi;
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                *reinterpret_cast<u32x4*>(my + kw[j] + 4096 * b + 1024 * j) = fk[j];
-                *reinterpret_cast<u32x4*>(my + vw + 4096 * b + 1024 * j) = fv[j];
-            }
-        }
-    };
-
-    bf16x8 qf[2][4];
+// A wavefront's 32 columns: queries, sums and references.  S^T = K Q^T and O^T += V^T P^T as in decode_flat_body, two tiles of 16 columns
+// for each K and V operand read from LDS.
+struct Columns {
+    bf16x8 q[2][4];
     f32x4 o[2][8];
-    float m_run[2], l_run[2];
-    const float ref_least = -3.4e38f / fmaxf(a.c, 1.f);   // the reference stays finite (times c too) where all logits are minus infinity
-    int cols = 0, col0 = 0, first = 0, head = 0;          // columns of the group, this wavefront's first one, the group's first sequence
-    bool wide = true;
-    auto open_item = [&](const Item& it) {
-        first = __builtin_amdgcn_readfirstlane(gi.offs[it.group]);
-        const int m = __builtin_amdgcn_readfirstlane(gi.offs[it.group + 1]) - first;
-        const int tiles = tiles_of(m, G);
-        head = it.local / tiles;
-        cols = m * G;
-        wide = cols > kTileCols / 2;
-        col0 = (it.local - head * tiles) * kTileCols + 32 * (wide ? wave : wave & 1);
+    float m[2], l[2];
+
+    __device__ void open(const SharedArgs& a, const Unit& u, int col0, int G) {
+        const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const int cc = col0 + 16 * x + col;
-            const int member = cc / G;
+            const int cc = col0 + 16 * x + col, member = cc / G;
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
                 u32x4 v = {0u, 0u, 0u, 0u};
-                if (cc < cols)
-                    v = *reinterpret_cast<const u32x4*>(a.q + static_cast<size_t>(first + member) * a.q_stride +
-                                                        static_cast<size_t>(head * G + cc - member * G) * kD + 8 * (grp + 4 * kk));
-                qf[x][kk] = as_bf16x8(v);
+                if (cc < u.col_end)
+                    v = *reinterpret_cast<const u32x4*>(a.q + static_cast<size_t>(u.seq_first + member) * a.q_stride +
+                                                        static_cast<size_t>(u.head * G + cc - member * G) * kD + 8 * (grp + 4 * kk));
+                q[x][kk] = as_bf16x8(v);
             }
 #pragma unroll
             for (int mt = 0; mt < 8; ++mt) o[x][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
-            m_run[x] = -INFINITY;
-            l_run[x] = 0.f;
+            m[x] = -INFINITY;
+            l[x] = 0.f;
         }
-    };
-    auto close_item = [&](const Item& it) {   // this workgroup's partial of the item
-        const size_t slot = static_cast<size_t>(wg) + __builtin_amdgcn_readfirstlane(gi.base[it.group]) + it.local;
+    }
+
+    // logits of the 32 tokens parked at `my`: of column tile x, tokens 8 grp .. 8 grp + 3 in s[x] and the next four in s[2 + x]
+    __device__ __attribute__((always_inline)) void scores(const unsigned char* my, const int (&kr)[4], f32x4 (&s)[4]) const {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            float l = l_run[x] + __shfl_xor(l_run[x], 16);
-            l += __shfl_xor(l, 32);
-            if (col0 + 16 * x + col < cols) {
-                const size_t row = slot * kTileCols + 32 * wave + 16 * x + col;   // (narrow: the second half of the keys is 64 columns on)
-                float* dst = a.o_shared + row * kD + 4 * grp;
-#pragma unroll
-                for (int mt = 0; mt < 8; ++mt) *reinterpret_cast<f32x4*>(dst + 16 * mt) = o[x][mt];
-                if (grp == 0) {
-                    a.ml_shared[row * 2] = m_run[x] * a.c;
-                    a.ml_shared[row * 2 + 1] = l;
-                }
-            }
-        }
-    };
-    // the 32 tokens of a parked group, `there` of which exist
-    auto take_group = [&](const unsigned char* my, int there) {
-        f32x4 sa[2], sb[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) sa[x] = sb[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < 4; ++x) s[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
             const bf16x8 ka = as_bf16x8(*reinterpret_cast<const u32x4*>(my + kr[kk]));
             const bf16x8 kb = as_bf16x8(*reinterpret_cast<const u32x4*>(my + kr[kk ^ 1] + 1024));
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                sa[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[x][kk], sa[x], 0, 0, 0);
-                sb[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qf[x][kk], sb[x], 0, 0, 0);
+                s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, q[x][kk], s[x], 0, 0, 0);
+                s[2 + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, q[x][kk], s[2 + x], 0, 0, 0);
             }
         }
+    }
+
+    // P and O += V^T P^T of those tokens, `there` of which exist: 16 or all (blocks that do not are zeros).  kAhead: and the logits of the
+    // group parked at `ahead`, their matrix instructions one by one between those of the exponentials, which take about as long.
+    template <bool kAhead>
+    __device__ __attribute__((always_inline)) void weigh(const unsigned char* my, int vr, f32x4 (&s)[4], int there, float c, const unsigned char* ahead = nullptr,
+                                                         const int* kr = nullptr, f32x4* next = nullptr) {
         u32x4 vf[8];
+        // P is taken against a reference that moves when a sum says that logits are far above it (rounding to bf16 does not depend on the
+        // exponent): no maximum is looked for, which was a fifth of the instructions, and the sums are rarely scaled
+        float p[4][4], sum[2];
+        const float mc0 = m[0] * c, mc1 = m[1] * c;
+        auto exp_of = [&](int i) {
+            const int x = i & 1, h = (i >> 1) & 1, r = i >> 2;
+            p[x + 2 * h][r] = __builtin_amdgcn_exp2f(fmaf(s[x + 2 * h][r], c, x ? -mc1 : -mc0));
+        };
+        auto add_up = [&](int x) { sum[x] = ((p[x][0] + p[x][1]) + (p[x][2] + p[x][3])) + ((p[2 + x][0] + p[2 + x][1]) + (p[2 + x][2] + p[2 + x][3])); };
+        if constexpr (kAhead) {
+            bf16x8 kf[8];
 #pragma unroll
-        for (int mt = 0; mt < 8; ++mt) vf[mt] = *reinterpret_cast<const u32x4*>(my + vr + 512 * mt);
-        if (there < kGroup) {   // uniform; whole blocks are shared, so a lane's eight tokens exist or do not
-            const bool gone = 8 * grp >= there;
+            for (int kk = 0; kk < 4; ++kk) {
+                kf[2 * kk] = as_bf16x8(*reinterpret_cast<const u32x4*>(ahead + kr[kk]));
+                kf[2 * kk + 1] = as_bf16x8(*reinterpret_cast<const u32x4*>(ahead + kr[kk ^ 1] + 1024));
+            }
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < 4; ++x) next[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (gone) sa[x][r] = sb[x][r] = -INFINITY;
+            for (int i = 0; i < 16; ++i) {
+                const int kk = i >> 2, h = (i >> 1) & 1, x = i & 1;
+                __builtin_amdgcn_sched_barrier(0);
+                next[x + 2 * h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[2 * kk + h], q[x][kk], next[x + 2 * h], 0, 0, 0);
+                exp_of(i);
+                asm volatile("" : "+v"(p[x + 2 * h][kk]));   // (stays here: the compiler would put all of them behind the matrix instructions)
+                if (i & 1) vf[i >> 1] = *reinterpret_cast<const u32x4*>(my + vr + 512 * (i >> 1));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        } else {
 #pragma unroll
-            for (int mt = 0; mt < 8; ++mt)
-                if (gone) vf[mt] = u32x4{0u, 0u, 0u, 0u};
+            for (int mt = 0; mt < 8; ++mt) vf[mt] = *reinterpret_cast<const u32x4*>(my + vr + 512 * mt);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) exp_of(i);
+        }
+        add_up(0);
+        add_up(1);
+        if (there < kGroup || __builtin_amdgcn_ballot_w64(!(sum[0] < 0x1p40f) || !(sum[1] < 0x1p40f))) [[unlikely]] {
+            // the unit's first tokens, a reference that is too low, NaN, or a block that does not exist
+            const int grp = (threadIdx.x & 63) >> 4;
+            const float least = -3.4e38f / fmaxf(c, 1.f);   // the reference stays finite (times c too) where all logits are minus infinity
+            const bool gone = 8 * grp >= there;             // a lane's eight tokens exist or do not
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (gone) s[x][r] = s[2 + x][r] = -INFINITY;
+                    mx = fmaxf(mx, fmaxf(s[x][r], s[2 + x][r]));
+                }
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float m_new = fmaxf(fmaxf(m[x], mx), least);
+                const float alpha = __builtin_amdgcn_exp2f((m[x] - m_new) * c);
+                m[x] = m_new;
+                l[x] *= alpha;
+#pragma unroll
+                for (int mt = 0; mt < 8; ++mt) o[x][mt] *= alpha;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    p[x][r] = __builtin_amdgcn_exp2f(fmaf(s[x][r], c, -m_new * c));
+                    p[2 + x][r] = __builtin_amdgcn_exp2f(fmaf(s[2 + x][r], c, -m_new * c));
+                }
+                add_up(x);
+            }
         }
         bf16x8 pf[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            float mx = fmaxf(fmaxf(fmaxf(sa[x][0], sa[x][1]), fmaxf(sa[x][2], sa[x][3])), fmaxf(fmaxf(sb[x][0], sb[x][1]), fmaxf(sb[x][2], sb[x][3])));
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float m_new = fmaxf(fmaxf(m_run[x], mx), ref_least);
-            const float alpha = __builtin_amdgcn_exp2f((m_run[x] - m_new) * a.c);
-            const float mc = m_new * a.c;
-            float pa[4], pb[4];
+            l[x] += sum[x];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                pa[r] = __builtin_amdgcn_exp2f(fmaf(sa[x][r], a.c, -mc));
-                pb[r] = __builtin_amdgcn_exp2f(fmaf(sb[x][r], a.c, -mc));
+                pf[x][r] = static_cast<__bf16>(p[x][r]);
+                pf[x][4 + r] = static_cast<__bf16>(p[2 + x][r]);
             }
-            l_run[x] = l_run[x] * alpha + ((pa[0] + pa[1]) + (pa[2] + pa[3])) + ((pb[0] + pb[1]) + (pb[2] + pb[3]));
-            m_run[x] = m_new;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                pf[x][r] = static_cast<__bf16>(pa[r]);
-                pf[x][4 + r] = static_cast<__bf16>(pb[r]);
-            }
-#pragma unroll
-            for (int mt = 0; mt < 8; ++mt) o[x][mt] *= alpha;
         }
 #pragma unroll
         for (int mt = 0; mt < 8; ++mt)
 #pragma unroll
             for (int x = 0; x < 2; ++x) o[x][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vf[mt]), pf[x], o[x][mt], 0, 0, 0);
-    };
-
-    // ---- steps: while step i is computed from one buffer, step i + 1 is parked in the other and the loads of step i + 2 are in flight ----
-    Item now = item_at(start), next = now;
-    load_step(now, start);
-    open_item(now);
-    park_step(0);
-    if (start + 1 < end) {
-        if (start + 1 >= next.end) next = item_at(start + 1);
-        load_step(next, start + 1);
     }
-    __syncthreads();
-    for (int pos = start; pos < end; ++pos) {
-        const int buffer = (pos - start) & 1;
-        Item after = next;
-        if (pos + 1 < end) {   // uniform over the workgroup, as all branches around barriers here
-            park_step(buffer ^ 1);
-            if (pos + 2 < end) {
-                if (pos + 2 >= after.end) after = item_at(pos + 2);
-                load_step(after, pos + 2);
+
+    // the sums of P over all lanes of a column
+    __device__ void sum_lanes() {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            l[x] += __shfl_xor(l[x], 16);
+            l[x] += __shfl_xor(l[x], 32);
+        }
+    }
+};
+
+// A block of 16 tokens on its way from the cache to LDS, by one wavefront: eight (FP8: four) loads of 1 KiB, parked as decode_flat_body's
+// comment says (the block's place b in its group of 32 tokens is 0 or 1).
+template <bool kFp8, int kScales>
+struct Block {
+    static constexpr int kLoads = kFp8 ? 2 : 4;
+    u32x4 k[kLoads], v[kLoads];
+    float sc_k, sc_v;
+
+    __device__ void load(const SharedArgs& a, int64_t blk, int head) {
+        const int lane = threadIdx.x & 63;
+        if constexpr (kScales != 0) {
+            sc_k = a.scales[(static_cast<size_t>(blk) * a.hkv_l + head) * 2];
+            sc_v = a.scales[(static_cast<size_t>(blk) * a.hkv_l + head) * 2 + 1];
+        }
+        const size_t at = cache_part_offset(blk, head, 0, a.hkv_l, kD);
+        const u32x4* src = (kFp8 ? reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(a.cache) + at) : reinterpret_cast<const u32x4*>(a.cache + at)) + lane;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) k[j] = src[64 * j], v[j] = src[64 * (kLoads + j)];
+    }
+    __device__ void clear() {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) k[j] = v[j] = u32x4{0u, 0u, 0u, 0u};
+        sc_k = sc_v = 1.f;
+    }
+    __device__ void park(unsigned char* my, int kw, int vw, int b) const {
+        if constexpr (kFp8) {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                u32x4 lo, hi;
+                widen_fp8(k[j], lo, hi, kScales ? sc_k : 1.f);
+                const int ka = (kw ^ (64 * ((2 * j) ^ b))) + 4096 * b + 2048 * j;
+                *reinterpret_cast<u32x4*>(my + ka) = lo;
+                *reinterpret_cast<u32x4*>(my + (ka ^ 16)) = hi;
+                widen_fp8(v[j], lo, hi, kScales ? sc_v : 1.f);
+                const int va = vw + 4096 * b + 2048 * j;
+                *reinterpret_cast<u32x4*>(my + va) = lo;
+                *reinterpret_cast<u32x4*>(my + (va ^ 16)) = hi;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                *reinterpret_cast<u32x4*>(my + (kw ^ (64 * (j ^ b))) + 4096 * b + 1024 * j) = k[j];
+                *reinterpret_cast<u32x4*>(my + vw + 4096 * b + 1024 * j) = v[j];
             }
         }
-        const unsigned char* at = smem + buffer * 2 * kStageBytes;
-        const int left = (__builtin_amdgcn_readfirstlane(gi.eff[now.group]) - (pos - now.begin) * 4) * kBlockSize;
-        if (wide) {
-            take_group(at, left);
-            take_group(at + kStageBytes, left - kGroup);
+    }
+};
+
+// A unit's block ids, 64 at a time, one per lane: ids that came one by one through scalar loads made every wait for LDS data wait for them
+// too (they share a counter), 1 us a step.
+struct BlockIds {
+    const int32_t* table;
+    int last, at, now, next;   // the window from block `at` on, and the one behind it
+    __device__ void open(const Unit& u) {
+        table = u.table, last = u.end_block - 1, at = u.first_block;
+        now = fetch(at);
+        next = fetch(at + 64);
+    }
+    __device__ int fetch(int from) const { return table[min(from + static_cast<int>(threadIdx.x & 63), last)]; }
+    // the id of block i, between `at` and `at` + 127; blocks in front of i are not asked for again
+    __device__ int get(int i) {
+        if (i >= at + 64) {   // uniform
+            at += 64;
+            now = next;
+            next = fetch(at + 64);
+        }
+        return __builtin_amdgcn_readlane(now, i - at);
+    }
+};
+
+// LDS addresses of this lane's pieces
+struct Places {
+    int kw, vw, kr[4], vr;
+    template <bool kFp8>
+    __device__ static Places get() {
+        const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+        Places p;
+        if constexpr (kFp8) {
+            const int r8 = lane >> 3, pc = lane & 7, l31 = lane & 31;
+            p.kw = r8 * 256 + (((2 * pc) ^ (r8 & 3) ^ (4 * (lane >> 5))) << 4);
+            p.vw = 8192 + 1024 * (lane >> 5) + (((2 * l31) ^ ((l31 >> 3) & 1)) << 4);
         } else {
-            take_group(at + (wave >> 1) * kStageBytes, left - (wave >> 1) * kGroup);
+            p.kw = (lane >> 4) * 256 + (((lane & 15) ^ (lane >> 4)) << 4);
+            p.vw = 8192 + ((lane ^ ((lane >> 4) & 1)) << 4);
         }
-        if (pos + 1 >= end || pos + 1 >= now.end) {
-            close_item(now);
-            if (pos + 1 < end) open_item(next);
+        const int tau_a = ((col >> 2) << 3) + (col & 3), k_sel = tau_a >> 4, k_off_a = tau_a & 15;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) p.kr[x] = (k_sel * 4096 + k_off_a * 256 + ((grp ^ k_off_a ^ (4 * k_sel)) << 4)) ^ (64 * x);
+        p.vr = 8192 + (grp >> 1) * 4096 + (((2 * col + (grp & 1)) ^ ((col >> 3) & 1)) << 4);
+        return p;
+    }
+};
+
+// A tile of up to 128 columns, 32 per wavefront, all of which read every key.  LDS is a ring of four groups of 32 tokens (two blocks), of
+// which wavefront w brings block w / 2's K or V^T (w % 2).  While the weights and the second product of group g are computed, the
+// logits of group g + 1 are (matrix instructions between the vector ones), and groups g + 2 and g + 3 are on their way: straight into LDS, or
+// in two sets of registers where codes are widened.  One barrier per group: behind it group g + 1 is there for all, and all are done with
+// group g - 1, whose place the next load takes.
+// What bounds it: LDS, 64 KiB read for each group by the four wavefronts (512 clocks of a compute unit), two workgroups on a unit.
+template <bool kFp8, int kScales>
+__device__ __attribute__((always_inline)) inline void wide_unit(const SharedArgs& a, const Unit& u, unsigned char* smem) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+    const Places at = Places::get<kFp8>();
+    const int b = wave >> 1, part = wave & 1;
+    const int blocks = u.end_block - u.first_block, n = (blocks + 1) / 2;   // groups
+    // this lane's places in the 4 KiB of its wavefront's block and part: where it reads (loads into LDS: what belongs to its 16 bytes there) or writes
+    int place[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (kFp8) place[j] = j >= 2 ? 0 : (part ? at.vw : at.kw ^ (64 * ((2 * j) ^ b))) + 4096 * b + 2048 * j;
+        else place[j] = part ? (lane ^ ((lane >> 4) & 1)) << 4 : ((lane & 48) | ((lane & 15) ^ (lane >> 4) ^ (4 * (j ^ b)))) << 4;
+    }
+    const int zero_at = 8192 * part + 4096 * b;
+    BlockIds ids;
+    ids.open(u);
+    u32x4 set[2][kFp8 ? 2 : 1];
+    float scale[2] = {1.f, 1.f};
+    // groups come in order; the block that an odd count leaves out of the last one is zeros
+    auto fetch = [&](int g, int which) {
+        const int i = u.first_block + 2 * g + b;
+        if (i < u.end_block) {
+            const int64_t blk = ids.get(i);
+            const size_t from = cache_part_offset(blk, u.head, part, a.hkv_l, kD);
+            if constexpr (kFp8) {
+                if constexpr (kScales != 0) scale[which] = a.scales[(static_cast<size_t>(blk) * a.hkv_l + u.head) * 2 + part];
+                const u32x4* src = reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(a.cache) + from) + lane;
+                set[which][0] = src[0];
+                set[which][1] = src[64];
+            } else {
+                // (no registers are written; the compiler does not count these loads: they are waited for below)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\t"
+                             "global_load_lds_dwordx4 %1, %5\n\t"
+                             "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+                             "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+                             "global_load_lds_dwordx4 %4, %5 offset:3072"
+                             :: "s"(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem)) + (g & 3) * kStageBytes + zero_at), "v"(place[0]), "v"(place[1]), "v"(place[2]),
+                                "v"(place[3]), "s"(a.cache + from) : "memory");
+            }
+        } else if constexpr (kFp8) {
+            set[which][0] = set[which][1] = u32x4{0u, 0u, 0u, 0u};
+            scale[which] = 1.f;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4*>(smem + (g & 3) * kStageBytes + zero_at + 1024 * j + 16 * lane) = u32x4{0u, 0u, 0u, 0u};
         }
-        now = next;
-        next = after;
-        __syncthreads();
+    };
+    auto park = [&](int g, int which) {
+        if constexpr (kFp8) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                u32x4 lo, hi;
+                widen_fp8(set[which][j], lo, hi, kScales ? scale[which] : 1.f);
+                unsigned char* my = smem + (g & 3) * kStageBytes;
+                *reinterpret_cast<u32x4*>(my + place[j]) = lo;
+                *reinterpret_cast<u32x4*>(my + (place[j] ^ 16)) = hi;
+            }
+        }
+    };
+    // loads of all but the newest `kLeft` groups have arrived, LDS is written, for all wavefronts
+    auto meet = [&](auto left) {
+        if constexpr (kFp8) __syncthreads();
+        else if constexpr (decltype(left)::value == 2) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else if constexpr (decltype(left)::value == 1) asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    using Int0 = std::integral_constant<int, 0>;
+    using Int1 = std::integral_constant<int, 1>;
+    Columns c;
+    const int col0 = u.col_first + 32 * wave;
+    c.open(a, u, col0, a.hq_l / a.hkv_l);
+    fetch(0, 0);
+    if (n > 1) fetch(1, 1);
+    if constexpr (kFp8) {
+        park(0, 0);
+        if (n > 1) park(1, 1);
+        if (n > 2) fetch(2, 0);
+        if (n > 3) fetch(3, 1);
+    } else if (n > 2) {
+        fetch(2, 0);
+    }
+    // (the newest groups have no loads where their block does not exist: a wait by count is for those in front of the last one)
+    if (n > 3) meet(std::integral_constant<int, 2>{});
+    else meet(Int0{});
+    f32x4 s0[4], s1[4];
+    c.scores(smem, at.kr, s0);
+    auto group = [&](int g, f32x4 (&now)[4], f32x4 (&next)[4], auto which) {
+        if (g + 3 < n) meet(Int1{});
+        else meet(Int0{});
+        constexpr int w = decltype(which)::value;
+        if constexpr (kFp8) {
+            if (g + 2 < n) park(g + 2, w);
+            if (g + 4 < n) fetch(g + 4, w);
+        } else {
+            if (g + 3 < n) fetch(g + 3, 0);
+        }
+        // (behind the last group: logits of whatever lies there, not used)
+        c.weigh<true>(smem + (g & 3) * kStageBytes, at.vr, now, (blocks - 2 * g) * kBlockSize, a.c, smem + ((g + 1) & 3) * kStageBytes, at.kr, next);
+    };
+    int g = 0;
+#pragma unroll 1
+    for (; g + 1 < n; g += 2) {
+        group(g, s0, s1, Int0{});
+        group(g + 1, s1, s0, Int1{});
+    }
+    if (g < n) group(g, s0, s1, Int0{});
+    __syncthreads();   // (a next unit loads where this one reads)
+    c.sum_lanes();
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        if (col0 + 16 * x + col < u.col_end) {
+            const size_t row = static_cast<size_t>(u.slot) * kTileCols + 32 * wave + 16 * x + col;
+            float* dst = a.o_shared + row * kD + 4 * grp;
+#pragma unroll
+            for (int mt = 0; mt < 8; ++mt) *reinterpret_cast<f32x4*>(dst + 16 * mt) = c.o[x][mt];
+            if (grp == 0) *reinterpret_cast<f32x2*>(a.ml_shared + row * 2) = f32x2{c.m[x] * a.c, c.l[x]};
+        }
+    }
+    if constexpr (!kFp8) __builtin_amdgcn_s_waitcnt(0x0F70);   // (vmcnt(0): a next unit counts its own loads only)
+}
+
+// A tile of up to 32 columns, which all wavefronts take, each with every fourth group of 32 keys: nothing is shared until the end, where
+// their sums are added in LDS.
+template <bool kFp8, int kScales>
+__device__ __attribute__((always_inline)) inline void narrow_unit(const SharedArgs& a, const Unit& u, unsigned char* smem, float (&ref)[kWaves][kNarrowCols],
+                                                                 float (&sums)[kWaves][kNarrowCols]) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+    const Places at = Places::get<kFp8>();
+    unsigned char* const my = smem + wave * kStageBytes;
+    Block<kFp8, kScales> blk[2];
+    BlockIds ids;
+    ids.open(u);
+    auto load = [&](int first) {
+        blk[0].load(a, ids.get(first), u.head);
+        if (first + 1 < u.end_block) blk[1].load(a, ids.get(first + 1), u.head);
+        else blk[1].clear();
+    };
+    constexpr int kStride = 2 * kWaves;   // blocks from a wavefront's group to its next
+    int i = u.first_block + 2 * wave;
+    if (i < u.end_block) load(i);
+    Columns c;
+    c.open(a, u, u.col_first, a.hq_l / a.hkv_l);
+#pragma unroll 1
+    for (; i < u.end_block; i += kStride) {
+        blk[0].park(my, at.kw, at.vw, 0);
+        blk[1].park(my, at.kw, at.vw, 1);
+        if (i + kStride < u.end_block) load(i + kStride);
+        f32x4 s[4];
+        c.scores(my, at.kr, s);
+        c.weigh<false>(my, at.vr, s, (u.end_block - i) * kBlockSize, a.c);
+    }
+    c.sum_lanes();
+    if (grp == 0) ref[wave][col] = c.m[0], ref[wave][16 + col] = c.m[1];
+    __syncthreads();
+    float* mine = reinterpret_cast<float*>(my);   // [column][D], 16 bytes swizzled by the column so that the lanes of a column spread over the banks
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        float top = ref[0][16 * x + col];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ref[w][16 * x + col]);
+        const float f = c.m[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((c.m[x] - top) * a.c);
+#pragma unroll
+        for (int mt = 0; mt < 8; ++mt) *reinterpret_cast<f32x4*>(mine + (16 * x + col) * kD + 4 * ((grp + 4 * mt) ^ (col & 7))) = c.o[x][mt] * f;
+        if (grp == 0) sums[wave][16 * x + col] = c.l[x] * f;
+    }
+    __syncthreads();
+    // a wavefront adds eight columns, eight lanes each
+    {
+        const int cc = 8 * wave + (lane >> 3);
+        const size_t row = static_cast<size_t>(u.slot) * kTileCols + cc;
+        if (u.col_first + cc < u.col_end) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int piece = (lane & 7) + 8 * j;
+                f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w)
+                    v += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(smem + w * kStageBytes) + cc * kD + 4 * (piece ^ (cc & 7)));
+                *reinterpret_cast<f32x4*>(a.o_shared + row * kD + 4 * piece) = v;
+            }
+            if ((lane & 7) == 0) {
+                float top = ref[0][cc], l = sums[0][cc];
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ref[w][cc]), l += sums[w][cc];
+                *reinterpret_cast<f32x2*>(a.ml_shared + row * 2) = f32x2{top * a.c, l};
+            }
+        }
+    }
+    __syncthreads();   // (a next unit writes where this one reads)
+}
+
+// units [first, all) in strides of n_wg
+template <bool kFp8, int kScales>
+__device__ __attribute__((always_inline)) inline void shared_units(const SharedArgs& a, const GroupIndex& gi, unsigned char* smem, float (&ref)[kWaves][kNarrowCols],
+                                                                  float (&sums)[kWaves][kNarrowCols], int first, int n_wg, int all) {
+    const int lane = threadIdx.x & 63;
+    const int G = a.hq_l / a.hkv_l;
+    auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+#pragma unroll 1
+    for (int unit = first; unit < all; unit += n_wg) {
+        int g = 0;
+        for (int at = 0; at < a.num_groups; at += 64) {   // the group that the unit belongs to
+            const int i = min(at + lane, a.num_groups - 1);
+            const uint64_t m = __builtin_amdgcn_ballot_w64(gi.units[i] <= unit && gi.units[i + 1] > unit);
+            if (m) {
+                g = uniform(at + __builtin_ctzll(m));
+                break;
+            }
+        }
+        const int eff = uniform(gi.eff[g]), ranges = uniform(gi.ranges[g]), seq_first = uniform(gi.offs[g]), cols = (uniform(gi.offs[g + 1]) - seq_first) * G;
+        const int local = unit - uniform(gi.units[g]), item = uniform(local / ranges), range = local - item * ranges, tiles = tiles_of(cols);
+        const int per = uniform(((eff + 3) / 4 + ranges - 1) / ranges) * 4, head = uniform(item / tiles), col_first = (item - head * tiles) * tile_cols(cols);
+        Unit u = {a.block_table + static_cast<size_t>(uniform(gi.leader[g])) * a.max_blocks, range * per, min((range + 1) * per, eff), head, col_first,
+                  min(col_first + tile_cols(cols), cols), seq_first, unit};
+        if (u.first_block >= eff) continue;   // (uniform) the last ranges of a group may have no keys
+        if (cols > kNarrowMost) wide_unit<kFp8, kScales>(a, u, smem);
+        else narrow_unit<kFp8, kScales>(a, u, smem, ref, sums);
     }
 }
 
+// Every workgroup works out the same plan from the lengths and offsets (a launch of its own for that took longer), and takes its part of it:
+// the first ones units of shared keys, the others the sequences' own keys as decode_flat_body deals them out.
 template <bool kFp8, bool kAppend, bool kBlockScales>
 __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArgs a, AppendArgs ap) {
     __shared__ __attribute__((aligned(16))) unsigned char smem[kWaves * kStageBytes];
     __shared__ int index[kMaxPairs + 1 + 16];
     __shared__ int from[kMaxPairs];
     __shared__ GroupIndex gi;
+    float(&ref)[kWaves][kNarrowCols] = *reinterpret_cast<float(*)[kWaves][kNarrowCols]>(index);   // (a workgroup needs the index or these)
+    float(&sums)[kWaves][kNarrowCols] = *reinterpret_cast<float(*)[kWaves][kNarrowCols]>(index + kWaves * kNarrowCols);
     const int G = a.hq_l / a.hkv_l, n = a.num_seqs;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int kThreads = kWaves * 64, kSeqs = kMaxPairs / kThreads, kGroupsPer = kMaxGroups / kThreads;
@@ -325,107 +555,124 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
         gi.offs[g] = static_cast<uint16_t>(min(max(a.group_offsets[g] - a.first_seq, 0), n));
         if (g < a.num_groups) {
             gi.eff[g] = max(a.shared_lens[g], 0) / kBlockSize;
-            gi.line[g] = n;   // the first sequence that is no padding
+            gi.units[g] = n;   // the first sequence that is no padding
         }
     }
     __syncthreads();
     int mine[kSeqs];
+    {
+        const int first = gi.offs[0], end = gi.offs[a.num_groups];
 #pragma unroll
-    for (int x = 0; x < kSeqs; ++x) {
-        const int s = tid + x * kThreads;
-        mine[x] = -1;
-        if (s < n && len[x] > 0 && a.num_groups > 0 && s >= gi.offs[0] && s < gi.offs[a.num_groups]) {
-            int lo = 0, hi = a.num_groups;   // the last group with offs <= s: the one that is not empty among those that start alike
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (gi.offs[mid] <= s) lo = mid; else hi = mid;
+        for (int x = 0; x < kSeqs; ++x) {
+            const int s = tid + x * kThreads;
+            mine[x] = -1;
+            if (s < n && len[x] > 0 && s >= first && s < end) {
+                int lo = 0, hi = a.num_groups;   // the last group with offs <= s: the one that is not empty among those that start alike
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (gi.offs[mid] <= s) lo = mid; else hi = mid;
+                }
+                if (gi.offs[lo + 1] - gi.offs[lo] >= 2) {   // (a group of one shares nothing)
+                    mine[x] = lo;
+                    atomicMin(&gi.eff[lo], (len[x] - 1) / kBlockSize);
+                    atomicMin(&gi.units[lo], s);
+                }
             }
-            mine[x] = lo;
-            atomicMin(&gi.eff[lo], (len[x] - 1) / kBlockSize);
-            atomicMin(&gi.line[lo], s);
         }
     }
     __syncthreads();
-    int steps_of[kGroupsPer], items_of[kGroupsPer], line = 0, items = 0;
-#pragma unroll
-    for (int x = 0; x < kGroupsPer; ++x) {   // thread t owns kGroupsPer groups from kGroupsPer t on
-        const int g = tid * kGroupsPer + x;
-        steps_of[x] = items_of[x] = 0;
-        if (g < a.num_groups) {
-            const int m = gi.offs[g + 1] - gi.offs[g];
-            if (m < 2 || gi.line[g] >= n) gi.eff[g] = 0;
-            gi.leader[g] = static_cast<uint16_t>(gi.line[g]);
-            if (gi.eff[g] > 0) {
-                items_of[x] = a.hkv_l * tiles_of(m, G);
-                steps_of[x] = items_of[x] * ((gi.eff[g] + 3) / 4);
-            }
-        }
-        line += steps_of[x];
-        items += items_of[x];
-    }
-    const int line_incl = wave_scan(line), items_incl = wave_scan(items);
-    if (lane == 63) gi.sums[0][wave] = line_incl, gi.sums[1][wave] = items_incl;
-    __syncthreads();
-    int line_run = line_incl - line, items_run = items_incl - items, total = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) line_run += gi.sums[0][w], items_run += gi.sums[1][w];
-        total += gi.sums[0][w];
-    }
+    // ---- what there is to do: steps of all tiles, weighted, and groups of 32 tokens that the sequences have to themselves ----
+    int cols[kGroupsPer], steps[kGroupsPer];   // thread t owns groups kGroupsPer t and following
+    int weight = 0, own = 0;
 #pragma unroll
     for (int x = 0; x < kGroupsPer; ++x) {
         const int g = tid * kGroupsPer + x;
-        if (g <= a.num_groups) {
-            gi.line[g] = line_run;
-            gi.base[g] = static_cast<uint16_t>(items_run);
+        cols[x] = steps[x] = 0;
+        if (g < a.num_groups) {
+            const int leader = gi.units[g];
+            gi.leader[g] = static_cast<uint16_t>(leader);
+            if (leader < n) {
+                cols[x] = (gi.offs[g + 1] - gi.offs[g]) * G;
+                steps[x] = (gi.eff[g] + 3) / 4;
+            }
+            weight += steps[x] * a.hkv_l * tiles_of(cols[x]) * (cols[x] > kNarrowMost ? kWideCost : kNarrowCost);
         }
-        line_run += steps_of[x];
-        items_run += items_of[x];
     }
-    if (tid == 0 && a.num_groups == kMaxGroups) gi.line[kMaxGroups] = total;
-    int own = 0;   // groups of 32 tokens that the sequences have to themselves
 #pragma unroll
     for (int x = 0; x < kSeqs; ++x) {
-        const int s = tid + x * kThreads;
         const int f = mine[x] >= 0 ? gi.eff[mine[x]] : 0;
-        from[s] = f;
+        from[tid + x * kThreads] = f;
         own += (max(len[x], 0) - f * kBlockSize + kGroup - 1) / kGroup;
     }
+    weight = wave_scan(weight);
     own = wave_scan(own);
+    if (lane == 63) gi.sums[0][wave] = weight, gi.sums[1][wave] = own;
     __syncthreads();
-    if (lane == 63) gi.sums[0][wave] = own;
-    __syncthreads();
-    own = 0;
+    float cost_p = 0.f, cost_s = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) own += gi.sums[0][w];
-
-    // ---- how many workgroups take shared keys (the first ones), and how many steps each ----
-    const int64_t cost_p = static_cast<int64_t>(total) * kPrefixWeight, cost_s = static_cast<int64_t>(own) * a.hkv_l * kSuffixWeight / kWaves + 1;
-    int n_p = 0, range = a.range_min;
-    if (total > 0) {
-        n_p = min(max(static_cast<int>(kWorkgroups * cost_p / (cost_p + cost_s)), 1), kWorkgroups - 1);
-        range = max((total + n_p - 1) / n_p, a.range_min);
-        n_p = (total + range - 1) / range;
+    for (int w = 0; w < kWaves; ++w) cost_p += static_cast<float>(gi.sums[0][w]), cost_s += static_cast<float>(gi.sums[1][w]);
+    cost_s *= static_cast<float>(a.hkv_l * kOwnCost) / kWaves;
+    // ---- ranges: so long that the shared keys take the workgroups that are theirs by weight ----
+    int n_p = 0, all = 0;
+    if (cost_p > 0) {   // uniform
+        const float share = fminf(fmaxf(floorf(kWorkgroups * cost_p / (cost_p + cost_s)), 1.f), kWorkgroups - 1.f);
+        const int range = static_cast<int>(ceilf(cost_p / share));   // weighted steps of a workgroup
+        int units_of[kGroupsPer], units = 0;
+#pragma unroll
+        for (int x = 0; x < kGroupsPer; ++x) {
+            units_of[x] = 0;
+            if (steps[x] > 0) {
+                // a range that is too short costs more in the merge than it saves here: a step takes about as long as 16 parts of a row
+                const int cost = cols[x] > kNarrowMost ? kWideCost : kNarrowCost;
+                const int per = max(max((range + cost - 1) / cost, static_cast<int>(__builtin_sqrtf(static_cast<float>(steps[x])) * kRangeRoot)), a.range_min);
+                int ranges = (steps[x] + per - 1) / per;
+                // workgroup i runs on die i % 8: with a multiple of 4 ranges the tiles and heads of a group find the same keys in the L2
+                // of one die, or of two
+                if (ranges >= 16 && cols[x] > kTileCols) ranges &= ~3;
+                gi.ranges[tid * kGroupsPer + x] = static_cast<uint16_t>(ranges);
+                units_of[x] = ranges * a.hkv_l * tiles_of(cols[x]);
+            }
+            units += units_of[x];
+        }
+        const int incl = wave_scan(units);
+        if (lane == 63) gi.sums[2][wave] = incl;
+        __syncthreads();
+        int run = incl - units;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) run += gi.sums[2][w];
+            all += gi.sums[2][w];
+        }
+#pragma unroll
+        for (int x = 0; x < kGroupsPer; ++x) {
+            const int g = tid * kGroupsPer + x;
+            if (g < a.num_groups) gi.units[g] = run;
+            run += units_of[x];
+        }
+        if (tid == 0) gi.units[a.num_groups] = all;
+        n_p = min(all, kMostShared);
     }
     n_p = __builtin_amdgcn_readfirstlane(n_p);
-    range = __builtin_amdgcn_readfirstlane(range);
+    all = __builtin_amdgcn_readfirstlane(all);
     const int wg = blockIdx.x;
-    if (wg == n_p) {   // for the merge
+    if (wg == kWorkgroups - 1) {   // for the merge
+        __syncthreads();
 #pragma unroll
         for (int x = 0; x < kSeqs; ++x) {
             const int s = tid + x * kThreads;
             if (s >= n) continue;
-            SharedRow r = {0, 0, 0, 0, 0, range, 0, 0};
+            SharedRow r = {};
             const int g = mine[x];
             if (g >= 0 && gi.eff[g] > 0) {
-                const int m = gi.offs[g + 1] - gi.offs[g];
-                r = SharedRow{gi.line[g], (gi.eff[g] + 3) / 4, tiles_of(m, G), gi.base[g], (s - gi.offs[g]) * G, range, m * G > kTileCols / 2, 0};
+                const int c = (gi.offs[g + 1] - gi.offs[g]) * G, st = (gi.eff[g] + 3) / 4, per = (st + gi.ranges[g] - 1) / gi.ranges[g];
+                r = SharedRow{gi.units[g], gi.ranges[g], (st + per - 1) / per, tiles_of(c), (s - gi.offs[g]) * G, tile_cols(c), {0, 0}};
             }
             a.rows[s] = r;
         }
     }
     if (wg < n_p) {
-        shared_keys_body<kFp8, kBlockScales ? 1 : 0>(a, gi, smem, wg * range, min((wg + 1) * range, total), wg);
+        __syncthreads();
+        shared_units<kFp8, kBlockScales ? 1 : 0>(a, gi, smem, ref, sums, wg, n_p, all);
         return;
     }
     decode_flat_body<kFp8, kAppend, kWaves, false, kBlockScales ? 1 : 0, kMaxPairs, true>(
@@ -454,61 +701,74 @@ __global__ __launch_bounds__(32 * kGroups) void combine_shared_kernel(const floa
     size_t shared0 = 0;
     int shared_parts = 0;
     if (r.tiles > 0) {
-        const int c = r.col0 + j % G, tile = r.wide ? c / kTileCols : 0, local = tile + r.tiles * (j / G);
-        const int begin = r.line0 + local * r.steps, w0 = begin / r.range, w1 = (begin + r.steps - 1) / r.range;
-        shared0 = (static_cast<size_t>(w0) + r.base + local) * kTileCols + (c - tile * kTileCols);
-        shared_parts = (w1 - w0 + 1) * (r.wide ? 1 : 2);
+        const int c = r.col0 + j % G, tile = c / r.cols;
+        shared0 = (static_cast<size_t>(r.base) + static_cast<size_t>(tile + r.tiles * (j / G)) * r.ranges) * kTileCols + (c - tile * r.cols);
+        shared_parts = r.parts;
     }
     const int np = there ? min(e.y + shared_parts, kMergeParts) : 0;
-    const int stride = r.wide ? kTileCols : kTileCols / 2;   // rows between a shared part and the next
-    auto part = [&](int c, const float*& o, const float*& ml) {
-        if (c < e.y) {
-            const size_t row = own0 + static_cast<size_t>(c) * G;
-            o = o_part + row * kD;
-            ml = ml_part + row * 2;
-        } else {
-            const size_t row = shared0 + static_cast<size_t>(c - e.y) * stride;
-            o = o_shared + row * kD;
-            ml = ml_shared + row * 2;
-        }
+    auto row_of = [&](int c) -> size_t { return c < e.y ? own0 + static_cast<size_t>(c) * G : shared0 + static_cast<size_t>(c - e.y) * kTileCols; };
+    auto o_of = [&](int c) -> f32x4 { return *reinterpret_cast<const f32x4*>((c < e.y ? o_part : o_shared) + row_of(c) * kD + 4 * (tid & 31)); };
+    auto pair_of = [&](int c) -> f32x2 {
+        return c < np ? *reinterpret_cast<const f32x2*>((c < e.y ? ml_part : ml_shared) + row_of(c) * 2) : f32x2{-INFINITY, 0.f};
     };
-    float m_loc = -INFINITY;
-    for (int c = tid; c < np; c += kThreads) {
-        const float *o, *ml;
-        part(c, o, ml);
-        w_s[c] = ml[0];
-        m_loc = fmaxf(m_loc, ml[0]);
-    }
+    // this thread's first parts are requested before the weights are known: the time is that of dependent loads
+    constexpr int kEarly = 4;
+    f32x4 early[kEarly];
 #pragma unroll
-    for (int x = 32; x > 0; x >>= 1) m_loc = fmaxf(m_loc, __shfl_xor(m_loc, x));
-    if (lane == 0) red_s[0][tid >> 6] = m_loc;
-    __syncthreads();
-    float m_star = red_s[0][0];
-#pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) m_star = fmaxf(m_star, red_s[0][w]);
-    float l_loc = 0.f;
-    for (int c = tid; c < np; c += kThreads) {
-        const float *o, *ml;
-        part(c, o, ml);
-        const float w = w_s[c] == -INFINITY ? 0.f : exp2f(w_s[c] - m_star);
-        w_s[c] = w;
-        l_loc = fmaf(ml[1], w, l_loc);
-    }
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) l_loc += __shfl_xor(l_loc, x);
-    if (lane == 0) red_s[1][tid >> 6] = l_loc;
-    __syncthreads();
-    float l_star = red_s[1][0];
-#pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) l_star += red_s[1][w];
+    for (int x = 0; x < kEarly; ++x) early[x] = pg + kGroups * x < np ? o_of(pg + kGroups * x) : f32x4{0.f, 0.f, 0.f, 0.f};
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int c = pg; c < np; c += kGroups) {
-        const float *o, *ml;
-        part(c, o, ml);
-        const f32x4 v = *reinterpret_cast<const f32x4*>(o + 4 * (tid & 31));
-        const float w = w_s[c];
+    auto add_part = [&](float w, f32x4 v) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) acc[x] = fmaf(v[x], w, acc[x]);
+    };
+    float l_star;
+    if (np <= 64) {   // uniform: a pair per lane, every wavefront has all weights without LDS
+        const f32x2 ml = pair_of(lane);
+        float m_star = ml[0];
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) m_star = fmaxf(m_star, __shfl_xor(m_star, x));
+        const float w_lane = ml[0] == -INFINITY ? 0.f : exp2f(ml[0] - m_star);
+        l_star = ml[1] * w_lane;
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) l_star += __shfl_xor(l_star, x);
+#pragma unroll
+        for (int x = 0; x < kEarly; ++x)
+            if (kGroups * x < 64) add_part(__shfl(w_lane, (pg + kGroups * x) & 63), early[x]);
+        for (int c = kEarly * kGroups; c < np; c += kGroups) {
+            const float w = __shfl(w_lane, min(c + pg, 63));
+            if (c + pg < np) add_part(w, o_of(c + pg));
+        }
+    } else {
+        float m_loc = -INFINITY;
+        for (int c = tid; c < np; c += kThreads) {
+            w_s[c] = pair_of(c)[0];
+            m_loc = fmaxf(m_loc, w_s[c]);
+        }
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) m_loc = fmaxf(m_loc, __shfl_xor(m_loc, x));
+        if (lane == 0) red_s[0][tid >> 6] = m_loc;
+        __syncthreads();
+        float m_star = red_s[0][0];
+#pragma unroll
+        for (int w = 1; w < kThreads / 64; ++w) m_star = fmaxf(m_star, red_s[0][w]);
+        float l_loc = 0.f;
+        for (int c = tid; c < np; c += kThreads) {
+            const float w = w_s[c] == -INFINITY ? 0.f : exp2f(w_s[c] - m_star);   // (each slot is read and rewritten by the same thread)
+            w_s[c] = w;
+            l_loc = fmaf(pair_of(c)[1], w, l_loc);
+        }
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) l_loc += __shfl_xor(l_loc, x);
+        if (lane == 0) red_s[1][tid >> 6] = l_loc;
+        __syncthreads();
+        l_star = red_s[1][0];
+#pragma unroll
+        for (int w = 1; w < kThreads / 64; ++w) l_star += red_s[1][w];
+#pragma unroll
+        for (int x = 0; x < kEarly; ++x)
+            if (pg + kGroups * x < np) add_part(w_s[pg + kGroups * x], early[x]);
+#pragma unroll 4
+        for (int c = pg + kEarly * kGroups; c < np; c += kGroups) add_part(w_s[c], o_of(c));
     }
     *reinterpret_cast<f32x4*>(&acc_s[pg][4 * (tid & 31)]) = acc;
     __syncthreads();
@@ -527,10 +787,13 @@ int seqs_per_launch(int max_seq_len, const AttnShape& a) {
     const int64_t by_line = (static_cast<int64_t>(0x7FFFFFFF) - kGroup) / padded / a.hkv_l, by_index = kMaxPairs / a.hkv_l;
     return static_cast<int>(by_line < by_index ? by_line : by_index);
 }
+// units: a launch of `share` workgroups has up to that many ranges and one more for each item, a multiple of 4 of them for an item with
+// at least eight
 int64_t most_items(int n, int num_groups, const AttnShape& a) {
-    return static_cast<int64_t>(a.hkv_l) * (static_cast<int64_t>(n) * (a.hq_l / a.hkv_l) / kTileCols + (num_groups < n ? num_groups : n));
+    return static_cast<int64_t>(a.hkv_l) * (static_cast<int64_t>(n) * (a.hq_l / a.hkv_l) / kNarrowCols + (num_groups < n ? num_groups : n));
 }
-// tokens per wavefront so that no row has more than 480 parts of its own, steps per range so that it has no more than 482 shared ones
+int64_t most_units(int n, int num_groups, const AttnShape& a) { return (kWorkgroups + most_items(n, num_groups, a)) * 11 / 8 + 1; }
+// tokens per wavefront so that no row has more than 482 parts of its own, steps per range so that it has no more than 484 shared ones
 int own_r_min(int max_seq_len) {
     const int r = (max_seq_len / 480 + kGroup) / kGroup * kGroup;
     return r < 2 * kGroup ? 2 * kGroup : r;
@@ -540,19 +803,24 @@ int range_min(int max_seq_len) {
     return r < kMinSteps ? kMinSteps : r;
 }
 size_t rows_of(int n, const AttnShape& a) { return decode_mfma_rows_for(kWorkgroups * kWaves, n, a); }
-size_t slots_of(int n, int num_groups, const AttnShape& a) { return kWorkgroups + static_cast<size_t>(most_items(n, num_groups, a)); }
 
 }  // namespace
 
 bool decode_shared_supported(const AttnShape& a, int num_seqs, int max_seq_len, int num_groups) {
     if (num_groups < 1 || num_groups > kMaxGroups || !decode_mfma_supported(a, num_seqs, max_seq_len) || a.hkv_l > kMaxPairs) return false;
+    if (option_decode_shared() == 2) return false;
+    // A batch that is small even if every sequence has max_seq_len tokens reads its shared keys again and again from the caches, and the plain
+    // kernel, which has no groups to work out and fewer parts to merge, is done first: of 48 batches it was 1.0 to 3.5 us faster in all but one
+    // below 40 MB (10.9 against 13.5 us at 10 MB), even at 45 to 60, slower above (27 against 22 at 98, 150 against 45 at 1061).
+    const int64_t bytes = static_cast<int64_t>(num_seqs) * max_seq_len * a.hkv_l * 2 * kD * a.kv_elem;
+    if (option_decode_shared() != 1 && bytes <= kPlainBytes) return false;
     const int per = seqs_per_launch(max_seq_len, a), n = num_seqs < per ? num_seqs : per;
-    return per >= 1 && most_items(n, num_groups, a) < 0xFFFF && most_items(n, num_groups, a) * (max_seq_len / kStep + 1) < 0x7FFFFFFF;
+    return per >= 1 && most_items(n, num_groups, a) * (max_seq_len / kStep + 1) < 0x7FFFFFFF / kWideCost;
 }
 
 size_t decode_shared_workspace(int num_seqs, int max_seq_len, int num_groups, const AttnShape& a) {
     const int per = seqs_per_launch(max_seq_len, a), n = num_seqs < per ? num_seqs : per;
-    return (rows_of(n, a) + slots_of(n, num_groups, a) * kTileCols) * (kD + 2) * sizeof(float) + static_cast<size_t>(n) * (a.hkv_l * sizeof(int2) + sizeof(SharedRow)) + 32;
+    return (rows_of(n, a) + static_cast<size_t>(most_units(n, num_groups, a)) * kTileCols) * (kD + 2) * sizeof(float) + static_cast<size_t>(n) * (a.hkv_l * sizeof(int2) + sizeof(SharedRow)) + 32;
 }
 
 hipError_t launch_decode_shared(const void* q, const void* k_new, const void* v_new, const int64_t* slots, void* cache, const int32_t* block_table,
@@ -562,7 +830,7 @@ hipError_t launch_decode_shared(const void* q, const void* k_new, const void* v_
     const int per = seqs_per_launch(max_seq_len, a), G = a.hq_l / a.hkv_l;
     for (int s0 = 0; s0 < num_seqs; s0 += per) {  // runs share the workspace: same stream, one after the other
         const int n = num_seqs - s0 < per ? num_seqs - s0 : per;
-        const size_t rows = rows_of(n, a), shared = slots_of(n, num_groups, a) * kTileCols;
+        const size_t rows = rows_of(n, a), shared = static_cast<size_t>(most_units(n, num_groups, a)) * kTileCols;
         float* o_part = static_cast<float*>(workspace);
         float* o_shared = o_part + rows * kD;
         float* ml_part = o_shared + shared * kD;

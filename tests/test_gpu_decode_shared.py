@@ -17,9 +17,12 @@ DEV, BLOCK = "cuda:0", 16
 
 @pytest.fixture(scope="module")
 def B():
+    """The kernel that shares takes every batch it can, also those that are the plain kernel's by their size."""
     from paper_2509_16495_amd import binding
     binding.lib()
-    return binding
+    binding.set_option(binding.OPT_DECODE_SHARED, 1)
+    yield binding
+    binding.set_option(binding.OPT_DECODE_SHARED, 0)
 
 
 class Case:
@@ -194,6 +197,46 @@ def test_shapes_that_take_the_plain_kernels(B, hq, hkv, D, dtype, cache):
     d = case.device()
     case.call(B, d)
     case.check(d)
+
+
+@pytest.mark.parametrize("option", [0, 2])
+def test_small_batches_are_the_plain_kernels(B, option):
+    import torch
+    case = Case(**BATCHES["alone behind"])
+    d, e = case.device(), case.device()
+    try:
+        B.set_option(B.OPT_DECODE_SHARED, option)
+        case.call(B, d)
+        case.call(B, e, shared=False)
+    finally:
+        B.set_option(B.OPT_DECODE_SHARED, 1)
+    case.check(d)
+    assert torch.equal(d["out"], e["out"])
+
+
+def test_a_batch_that_is_large_enough(B):
+    """Above the size from which the kernel that shares takes a batch by itself, and the workspace that the query names."""
+    import torch
+    case = Case([(5000, [5040 + 3 * i for i in range(20)])], [90], seed=31)
+    try:
+        B.set_option(B.OPT_DECODE_SHARED, 0)
+        d, e = case.device(), case.device()
+        a = B.attn_desc(d["q"], d["cache"], d["table"], case.scale, d["k"], d["out"])
+        n, ms = len(case.lens), int(case.lens.max())
+        need = B.decode_shared_workspace_bytes(n, ms, 1, a)
+        assert need > B.decode_workspace_bytes(n, ms, a) == B.decode_shared_workspace_bytes(n, 400, 1, a)
+        ws = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+        case.call(B, d, workspace=ws[:need])
+        case.check(d)
+        assert (ws[need:] == 0xA5).all()
+        case.call(B, e)
+        torch.cuda.synchronize()
+        assert torch.equal(d["out"], e["out"])
+        with pytest.raises(B.ShiftAttnError) as error:
+            case.call(B, d, workspace=ws[:need - 16])
+        assert error.value.code == B.EWORKSPACE
+    finally:
+        B.set_option(B.OPT_DECODE_SHARED, 1)
 
 
 def test_without_an_append_and_with_some_rows_that_append_nothing(B):

@@ -204,6 +204,24 @@ def test_decode_shared_refuses(B):
     assert B.decode_shared_workspace_bytes(0, 64, 0, a) == 0 == B.decode_shared_workspace_bytes(3, 64, 1, _attn(B, dtype=B.F32))
 
 
+def test_the_option_and_the_sizes_that_follow_it(B):
+    a = _attn(B, max_blocks_per_seq=4000)
+    assert B.get_option(B.OPT_DECODE_SHARED) == 0
+    for value in (-1, 3):
+        assert B.lib().shiftattn_set_option(B.OPT_DECODE_SHARED, value) == B.EINVAL
+    plain = lambda n, ms: B.decode_workspace_bytes(n, ms, a)
+    shared = lambda n, ms, groups=2: B.decode_shared_workspace_bytes(n, ms, groups, a)
+    assert shared(9, 1000) == plain(9, 1000) and shared(64, 20000) > plain(64, 20000)
+    assert shared(64, 20000, 0) == plain(64, 20000) == shared(64, 20000, 513)      # nothing in common, more groups than are indexed
+    try:
+        B.set_option(B.OPT_DECODE_SHARED, 1)
+        assert shared(9, 1000) > plain(9, 1000)
+        B.set_option(B.OPT_DECODE_SHARED, 2)
+        assert shared(64, 20000) == plain(64, 20000)
+    finally:
+        B.set_option(B.OPT_DECODE_SHARED, 0)
+
+
 def test_decode_shared_python_refuses(B):
     ok = dict(q=_z(5, 8, 128), cache=_z(3, 1, 2, 2048), table=_z(5, 2, dtype=I32), lens=_z(5, dtype=I32), off=_z(3, dtype=I32), sh=_z(2, dtype=I32), out=_z(5, 8, 128),
               k=_z(5, 1, 128), v=_z(5, 1, 128), slots=_z(5, dtype=I64), ws=_z(64, dtype=U8), scales=None, scale=0.1)
