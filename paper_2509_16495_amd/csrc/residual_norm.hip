@@ -62,7 +62,18 @@ __device__ inline void store8(void* base, int64_t at, const float (&f)[8]) {
     }
 }
 
+// 1 / sqrt(x) rounded from an error of a few 2^-53 (two Newton steps on the hardware's estimate); 0 for an infinity
+__device__ inline float inverse_root(double x) {
+    double r = __builtin_amdgcn_rsq(x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = fma(r, fma(-0.5 * x * r, r, 0.5), r);
+    return x < __builtin_inf() ? static_cast<float>(r) : x > 0.0 ? 0.f : static_cast<float>(x);
+}
+
 // One workgroup per row, kPieces stretches of eight elements per thread, held in registers from the load to the store.
+// Bound: a row's bytes through HBM once (x and the residual in, the residual and the output out).  Threads for two stretches each: with one, a
+// row of 8192 took a workgroup of 16 wavefronts that waits at two barriers with nothing beside it on its compute unit (16384 rows, int8: 208
+// us), with four there are too few loads in flight (180; with two 170, 5.5 TB/s, what a copy reaches).
 template <bool kXF32, bool kResF32, int kPieces>
 __global__ __launch_bounds__(kMaxWaves * 64) void add_rms_norm_kernel(NormArgs a) {
     __shared__ double sums[kMaxWaves];
@@ -100,11 +111,11 @@ __global__ __launch_bounds__(kMaxWaves * 64) void add_rms_norm_kernel(NormArgs a
     sum = sums[0];
     for (int w = 1; w < waves; ++w) sum += sums[w];
     const double mean = sum / a.cols + a.eps;
-    const float inv = static_cast<float>(1.0 / sqrt(mean));
+    const float inv = inverse_root(mean);
 
-    uint32_t top = 0;     // largest |y| that is a number (FP8: infinities too), as bits
     const bool codes = a.out_kind >= SHIFTATTN_CODES_FP8;
     const uint32_t below = a.out_kind == SHIFTATTN_CODES_FP8 ? 0x7F800001u : 0x7F800000u;
+    uint32_t all = 0;     // largest |y|, as bits (NaN is above everything)
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
         const int col = (threadIdx.x + i * blockDim.x) * 8;
@@ -116,23 +127,65 @@ __global__ __launch_bounds__(kMaxWaves * 64) void add_rms_norm_kernel(NormArgs a
         for (int j = 0; j < 8; ++j) {
             h[i][j] = (h[i][j] * inv) * (w[j] + a.offset);
             const uint32_t b = __float_as_uint(h[i][j]) & 0x7FFFFFFFu;
-            top = max(top, b < below ? b : 0u);
+            all = max(all, b);
         }
         if (a.out_kind == SHIFTATTN_BF16) store8<false>(a.out, row * a.out_stride + col, h[i]);
         else if (a.out_kind == SHIFTATTN_F32) store8<true>(a.out, row * a.out_stride + col, h[i]);
     }
     if (!codes) return;
+    auto over_row = [&](uint32_t v) -> uint32_t {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o)));
-    if (lane == 0) tops[wave] = top;
-    __syncthreads();
-    top = tops[0];
-    for (int w = 1; w < waves; ++w) top = max(top, tops[w]);
+        for (int o = 32; o > 0; o >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), o)));
+        if (lane == 0) tops[wave] = v;
+        __syncthreads();
+        v = tops[0];
+        for (int w = 1; w < waves; ++w) v = max(v, tops[w]);
+        return v;
+    };
+    uint32_t top = over_row(all);   // largest |y| as bits
+    const bool numbers = top < 0x7F800000u;
+    if (!numbers) {   // (uniform, rare) of those that are numbers (FP8: infinities too)
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t b = __float_as_uint(h[i][j]) & 0x7FFFFFFFu;
+                if ((threadIdx.x + i * blockDim.x) * 8 < a.cols) m = max(m, b < below ? b : 0u);
+            }
+        __syncthreads();
+        top = over_row(m);
+    }
     const float amax = __uint_as_float(top);
     uint8_t* out = static_cast<uint8_t*>(a.out) + row * a.out_stride;
     if (a.out_kind == SHIFTATTN_CODES_FP8) {
         const float scale = amax > 0.f ? amax / 448.f : 1.f;
         if (threadIdx.x == 0) a.scales[row] = scale;
+        // The quotient correctly rounded, as a division gives it, in five instructions instead of ten: with y the rounded reciprocal, two steps
+        // q += (v - q scale) y, whose remainders are exact (Markstein's theorem; it needs a reciprocal whose divisor's
+        // mantissa is not all ones, and a range without underflow: below 2^-11 a quotient's code is 0 whatever its last bits).
+        if (numbers && scale > 0x1p-60f && scale < 0x1p60f && (__float_as_uint(scale) & 0x7FFFFFu) != 0x7FFFFFu) {
+            const float y = 1.f / scale;
+            auto quotient = [&](float v) {
+                float q = v * y;
+                q = fmaf(fmaf(-q, scale, v), y, q);
+                return copysignf(fmaf(fmaf(-q, scale, v), y, q), v);   // (-0 keeps its sign) at most 448 (1 + 2^-23): rounds to a code without a clamp
+            };
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int col = (threadIdx.x + i * blockDim.x) * 8;
+                if (col >= a.cols) continue;
+                u32x2 r;
+#pragma unroll
+                for (int h2 = 0; h2 < 2; ++h2) {
+                    int w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(h[i][4 * h2]), quotient(h[i][4 * h2 + 1]), 0, false);
+                    w = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(h[i][4 * h2 + 2]), quotient(h[i][4 * h2 + 3]), w, true);
+                    r[h2] = static_cast<uint32_t>(w);
+                }
+                *reinterpret_cast<u32x2*>(out + col) = r;
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int col = (threadIdx.x + i * blockDim.x) * 8;
@@ -148,7 +201,7 @@ __global__ __launch_bounds__(kMaxWaves * 64) void add_rms_norm_kernel(NormArgs a
     auto code = [&](float v) -> uint32_t {
         // adding 1.5 * 2^23 rounds the exact product to an integer, ties to even; its low byte is the code
         const uint32_t c = __float_as_uint(fmaf(v, to_code, 12582912.f)) & 0xFFu;
-        return fabsf(v) < INFINITY ? c : v != v ? 0u : v > 0.f ? 127u : 129u;
+        return numbers || fabsf(v) < INFINITY ? c : v != v ? 0u : v > 0.f ? 127u : 129u;
     };
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
@@ -168,8 +221,8 @@ hipError_t launch_add_rms_norm(const void* x, void* residual, const void* weight
                                hipStream_t st) {
     if (rows == 0) return hipSuccess;
     const int pieces = s.cols / 8;
-    int threads = 64;
-    while (threads < kMaxWaves * 64 && threads * 2 <= pieces) threads *= 2;
+    int threads = (pieces + 127) / 128 * 64;
+    threads = threads < kMaxWaves * 64 ? threads : kMaxWaves * 64;
     const int per = (pieces + threads - 1) / threads;
     NormArgs a{x, residual, weight, out, scales, s.x_stride, s.res_stride, s.out_stride, rows, s.cols, s.w_f32, s.out_kind, s.offset,
                static_cast<double>(s.eps)};
