@@ -12,6 +12,8 @@ namespace shiftattn {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBatch = 2;         // heads of a lane whose loads are in flight together
+constexpr int kMostPairs = 128;   // head_dim up to 256
 
 struct RotaryArgs {
     void* heads[2];                 // queries, keys
@@ -22,7 +24,7 @@ struct RotaryArgs {
     const int32_t* seq_lens;
     const double* frequencies;
     int64_t first, rows;            // those of this launch
-    int num_prefill, total_prefill_q, head_dim, half, slices;
+    int num_prefill, total_prefill_q, head_dim, half;
     float magnitude;
 };
 
@@ -45,39 +47,51 @@ __device__ inline void angle_of(int position, double frequency, float& sin_t, fl
     cos_t = n == 1 || n == 2 ? -b : b;
 }
 
-// A thread takes one 16-byte piece of a head's first elements (kPer pairs) and its partners, computes their angles once and goes through
-// its share of the row's heads; heads are dealt to `slices` threads where rows are few.
+// A wavefront takes a row.  Its lanes compute the angles, a pair (or two) each, and hand them round through LDS; then a lane owns one
+// 16-byte piece of a head's first elements (kPer pairs) and its partners, and the lanes lie side by side in memory over several heads.
+// What bounds it is HBM, where it counts that neighbouring lanes' places lie side by side and that instructions are few: threads that went down a
+// row's heads one by one touched 128 bytes here and there (65536 rows of 18 heads 124 us), and with the heads side by side but the angles
+// worked out by every thread batches that fit the caches were bound by those (8192 rows of 9 heads 9.9 us).  This takes 115 (5.2 TB/s
+// read + written) and 8.1.
 template <typename Elem, bool kPairs>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
     constexpr int kPer = 16 / sizeof(Elem);
-    const int chunks = a.half / kPer;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int chunk = static_cast<int>(item % chunks);
-    const int64_t rest = item / chunks;
-    if (rest >= a.rows * a.slices) return;
-    const int row = static_cast<int>(a.first + rest / a.slices), slice = static_cast<int>(rest % a.slices);
+    __shared__ float angles[kThreads / 64][2][kMostPairs];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + wave;
+    if (at >= a.rows) return;   // (a wavefront as a whole; there is no barrier)
+    const int row = static_cast<int>(a.first + at);
     int pos;
     if (a.positions) pos = a.positions[row];
     else if (row >= a.total_prefill_q) pos = a.seq_lens[a.num_prefill + row - a.total_prefill_q] - 1;
     else pos = a.num_prefill > 0 ? query_row(a.cu_seqlens_q, a.seq_lens, a.num_prefill, row).pos : -1;
     if (pos < 0) return;   // no token
+    for (int i = lane; i < a.half; i += 64) {
+        float sin_i, cos_i;
+        angle_of(pos, a.frequencies[i], sin_i, cos_i);
+        angles[wave][0][i] = sin_i * a.magnitude;
+        angles[wave][1][i] = cos_i * a.magnitude;
+    }
+    __builtin_amdgcn_wave_barrier();
+    const int chunks = a.half / kPer;                       // pieces of a head
+    const int beside = 64 / chunks;                         // heads that the wavefront takes at once
+    const int chunk = lane % chunks, slice = lane / chunks;
+    if (slice >= beside) return;
     float sin_t[kPer], cos_t[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        angle_of(pos, a.frequencies[chunk * kPer + j], sin_t[j], cos_t[j]);
-        sin_t[j] *= a.magnitude;
-        cos_t[j] *= a.magnitude;
+        sin_t[j] = angles[wave][0][chunk * kPer + j];
+        cos_t[j] = angles[wave][1][chunk * kPer + j];
     }
     union Piece { u32x4 v; Elem e[kPer]; };
     const int total = a.num_heads[0] + a.num_heads[1];
-    for (int head = slice; head < total; head += a.slices) {
+    auto place = [&](int head) -> u32x4* {
         const int which = head < a.num_heads[0] ? 0 : 1;
-        Elem* p = static_cast<Elem*>(a.heads[which]) + row * a.stride[which] + static_cast<int64_t>(head - (which ? a.num_heads[0] : 0)) * a.head_dim;
-        u32x4* lo = reinterpret_cast<u32x4*>(p + (kPairs ? 2 * chunk : chunk) * kPer);
-        u32x4* hi = kPairs ? lo + 1 : reinterpret_cast<u32x4*>(p + a.half + chunk * kPer);
-        Piece x, y;
-        x.v = *lo;
-        y.v = *hi;
+        return reinterpret_cast<u32x4*>(static_cast<Elem*>(a.heads[which]) + row * a.stride[which] + static_cast<int64_t>(head - (which ? a.num_heads[0] : 0)) * a.head_dim +
+                                        (kPairs ? 2 * chunk : chunk) * kPer);
+    };
+    const int partner = kPairs ? 1 : chunks;   // 16-byte pieces from the first to the second
+    auto turn = [&](Piece& x, Piece& y) {
         if constexpr (kPairs) {
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
@@ -95,8 +109,29 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a) {
                 set(y.e[j], v * cos_t[j] + u * sin_t[j]);
             }
         }
-        *lo = x.v;
-        *hi = y.v;
+    };
+    // heads in batches, all of a batch's loads in front of its stores (in place, the compiler cannot move a load up by itself)
+    for (int first = slice; first < total; first += kBatch * beside) {
+        Piece x[kBatch], y[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int head = first + i * beside;
+            if (head < total) {
+                const u32x4* p = place(head);
+                x[i].v = p[0];
+                y[i].v = p[partner];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int head = first + i * beside;
+            if (head < total) {
+                turn(x[i], y[i]);
+                u32x4* p = place(head);
+                p[0] = x[i].v;
+                p[partner] = y[i].v;
+            }
+        }
     }
 }
 
@@ -107,17 +142,13 @@ hipError_t launch_rotary(const RotaryShape& s, void* q, void* k, const int32_t* 
     const int heads = (q ? s.hq : 0) + (k ? s.hkv : 0);
     if (rows == 0 || heads == 0) return hipSuccess;
     RotaryArgs a{{q, k}, {q ? s.hq : 0, k ? s.hkv : 0}, {s.q_stride, s.k_stride}, positions, cu_seqlens_q, seq_lens, frequencies, 0, 0,
-                 num_prefill, total_prefill_q, s.head_dim, s.rot_dim / 2, 1, s.magnitude};
-    const int chunks = a.half * s.elem / 16;
-    // enough threads for every compute unit; beyond that a thread's angles serve all heads of its row
-    while (a.slices < heads && static_cast<int64_t>(rows) * chunks * a.slices < 256 * 256) a.slices *= 2;
-    a.slices = a.slices < heads ? a.slices : heads;
+                 num_prefill, total_prefill_q, s.head_dim, s.rot_dim / 2, s.magnitude};
     // rows beyond the threads of one launch go into further ones
-    const int64_t per_row = static_cast<int64_t>(chunks) * a.slices, most = most_workgroups(kThreads) * kThreads / per_row;
+    constexpr int64_t kRows = kThreads / 64, kMost = most_workgroups(kThreads) * kRows;
     auto run = [&](auto kernel) -> hipError_t {
-        for (a.first = 0; a.first < rows; a.first += most) {
-            a.rows = rows - a.first < most ? rows - a.first : most;
-            kernel<<<static_cast<unsigned>((a.rows * per_row + kThreads - 1) / kThreads), kThreads, 0, st>>>(a);
+        for (a.first = 0; a.first < rows; a.first += kMost) {
+            a.rows = rows - a.first < kMost ? rows - a.first : kMost;
+            kernel<<<static_cast<unsigned>((a.rows + kRows - 1) / kRows), kThreads, 0, st>>>(a);
             if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         }
         return hipSuccess;
