@@ -712,7 +712,7 @@ __global__ __launch_bounds__(32 * kGroups) void combine_shared_kernel(const floa
         return c < np ? *reinterpret_cast<const f32x2*>((c < e.y ? ml_part : ml_shared) + row_of(c) * 2) : f32x2{-INFINITY, 0.f};
     };
     // this thread's first parts are requested before the weights are known: the time is that of dependent loads
-    constexpr int kEarly = 4;
+    constexpr int kEarly = kGroups == 4 ? 4 : 8;
     f32x4 early[kEarly];
 #pragma unroll
     for (int x = 0; x < kEarly; ++x) early[x] = pg + kGroups * x < np ? o_of(pg + kGroups * x) : f32x4{0.f, 0.f, 0.f, 0.f};
@@ -858,10 +858,14 @@ hipError_t launch_decode_shared(const void* q, const void* k_new, const void* v_
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         const unsigned grid = static_cast<unsigned>(n) * a.hq_l;
         uint16_t* out_run = static_cast<uint16_t*>(out) + static_cast<size_t>(s0) * a.out_stride;
-        if (grid >= 1024)
-            combine_shared_kernel<4><<<grid, 128, 0, st>>>(o_part, ml_part, plan, o_shared, ml_shared, info, seq_lens + s0, a.hq_l, G, out_run, a.out_stride, a.v_scale);
-        else
-            combine_shared_kernel<16><<<grid, 512, 0, st>>>(o_part, ml_part, plan, o_shared, ml_shared, info, seq_lens + s0, a.hq_l, G, out_run, a.out_stride, a.v_scale);
+        auto merge = [&](auto kernel, int threads) {
+            kernel<<<grid, threads, 0, st>>>(o_part, ml_part, plan, o_shared, ml_shared, info, seq_lens + s0, a.hq_l, G, out_run, a.out_stride, a.v_scale);
+        };
+        // many rows have few parts and fill the chip by themselves (4032 rows of four parts: 17.5 us with four groups, 20.1 with eight); few rows
+        // have many, all of which should be on their way at once (1520 rows: 44.3 us with four, 42.6 with eight)
+        if (grid >= 2048) merge(combine_shared_kernel<4>, 128);
+        else if (grid >= 1024) merge(combine_shared_kernel<8>, 256);
+        else merge(combine_shared_kernel<16>, 512);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
