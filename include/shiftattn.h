@@ -272,7 +272,7 @@ int shiftattn_unpack_o_proj_int8_ws(const void *recv_codes, const float *a_scale
  *   x (device, in)               : [rows][cols], bf16 or float32, row stride x_stride
  *   residual (device, in/out)    : [rows][cols], bf16 or float32, row stride residual_stride, or NULL
  *   weight (device, in)          : [cols], bf16 or float32; weight_offset 1 is for weights stored as their difference from 1
- *   out (device, out)            : [rows][cols] in out_format, row stride out_stride.  May be x itself where type and stride are the same
+ *   out (device, out)            : [rows][cols] in out_format, row stride out_stride.  May be x itself where type and stride are the same (the residual too)
  *   scales (device, out)         : float32 [rows] for codes, else NULL
  * A NaN in h makes all of the row's y NaN, an infinity makes them 0 but for a NaN in its own place (scale 1 in both cases).
  * cols: a multiple of 8 up to 65536 (else EUNSUPPORTED); eps > 0.  Pointers 16-byte aligned (scales: 4), row strides multiples of 16 bytes (codes: 8).  0 as a stride stands for dense rows. */

@@ -817,6 +817,8 @@ int shiftattn_add_rms_norm(const void* x, void* residual, const void* weight, vo
     if (rows == 0) return SHIFTATTN_OK;
     if (!x || !weight || !out || (codes && !scales)) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
     if (out == residual) return fail(SHIFTATTN_EINVAL, "out and residual are the same rows");
+    if ((out == x && (n->out_format != n->x_dtype || s.out_stride != s.x_stride)) || (residual == x && (n->residual_dtype != n->x_dtype || s.res_stride != s.x_stride)))
+        return fail(SHIFTATTN_EINVAL, "out or residual is x in another type or with another stride");
     if (!codes && scales) return fail(SHIFTATTN_EINVAL, "scales belong to codes: must be NULL for values");
     if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned_to(out, codes ? 8 : 16) || !aligned_to(scales, 4))
         return fail(SHIFTATTN_EINVAL, "x / residual / weight / out must be 16-byte aligned (codes: 8), scales 4-byte");
@@ -848,6 +850,7 @@ int check_rotary(const shiftattn_rotary_desc* r, const void* q, const void* k, i
     if (rows > 0x7FFFFFFF) return fail(SHIFTATTN_EUNSUPPORTED, "more than 2^31-1 rows");
     if (rows == 0) return 0;
     if ((!q && !k) || !frequencies) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
+    if (q == k) return fail(SHIFTATTN_EINVAL, "q and k are the same rows");
     if (!aligned16(q) || !aligned16(k) || !aligned_to(frequencies, 8)) return fail(SHIFTATTN_EINVAL, "q / k must be 16-byte aligned, frequencies 8-byte");
     return 0;
 }

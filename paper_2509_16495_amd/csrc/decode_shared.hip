@@ -11,7 +11,7 @@ constexpr int kWaves = 4;
 constexpr int kWorkgroups = 512;      // two resident per compute unit
 constexpr int kMaxPairs = 1024;       // (sequence, KV head) pairs of a launch
 constexpr int kMaxGroups = 512;
-constexpr int64_t kPlainBytes = 40000000;   // cache up to which a batch is the plain kernel's
+constexpr double kPlainBytes = 40.0e6;   // cache up to which a batch is the plain kernel's
 constexpr int kMostShared = 508;      // of which take shared keys at most
 constexpr int kStep = 64;             // keys that shared ranges are counted in
 constexpr int kTileCols = 128;        // (sequence, head) columns of a tile whose keys a workgroup's wavefronts share
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
                     const int mid = (lo + hi) >> 1;
                     if (gi.offs[mid] <= s) lo = mid; else hi = mid;
                 }
-                if (gi.offs[lo + 1] - gi.offs[lo] >= 2) {   // (a group of one shares nothing)
+                if (s < gi.offs[lo + 1] && gi.offs[lo + 1] - gi.offs[lo] >= 2) {   // (a group of one shares nothing)
                     mine[x] = lo;
                     atomicMin(&gi.eff[lo], (len[x] - 1) / kBlockSize);
                     atomicMin(&gi.units[lo], s);
@@ -812,7 +812,7 @@ bool decode_shared_supported(const AttnShape& a, int num_seqs, int max_seq_len, 
     // A batch that is small even if every sequence has max_seq_len tokens reads its shared keys again and again from the caches, and the plain
     // kernel, which has no groups to work out and fewer parts to merge, is done first: of 48 batches it was 1.0 to 3.5 us faster in all but one
     // below 40 MB (10.9 against 13.5 us at 10 MB), even at 45 to 60, slower above (27 against 22 at 98, 150 against 45 at 1061).
-    const int64_t bytes = static_cast<int64_t>(num_seqs) * max_seq_len * a.hkv_l * 2 * kD * a.kv_elem;
+    const double bytes = 2.0 * kD * a.kv_elem * a.hkv_l * num_seqs * max_seq_len;
     if (option_decode_shared() != 1 && bytes <= kPlainBytes) return false;
     const int per = seqs_per_launch(max_seq_len, a), n = num_seqs < per ? num_seqs : per;
     return per >= 1 && most_items(n, num_groups, a) * (max_seq_len / kStep + 1) < 0x7FFFFFFF / kWideCost;

@@ -23,7 +23,6 @@ struct NormArgs {
     void* out;
     float* scales;
     int64_t x_stride, res_stride, out_stride;
-    int64_t rows;
     int cols;
     bool w_f32;
     int out_kind;         // SHIFTATTN_BF16, SHIFTATTN_F32, SHIFTATTN_CODES_FP8, SHIFTATTN_CODES_INT8
@@ -224,7 +223,7 @@ hipError_t launch_add_rms_norm(const void* x, void* residual, const void* weight
     int threads = (pieces + 127) / 128 * 64;
     threads = threads < kMaxWaves * 64 ? threads : kMaxWaves * 64;
     const int per = (pieces + threads - 1) / threads;
-    NormArgs a{x, residual, weight, out, scales, s.x_stride, s.res_stride, s.out_stride, rows, s.cols, s.w_f32, s.out_kind, s.offset,
+    NormArgs a{x, residual, weight, out, scales, s.x_stride, s.res_stride, s.out_stride, s.cols, s.w_f32, s.out_kind, s.offset,
                static_cast<double>(s.eps)};
     auto run = [&](auto kernel) -> hipError_t {
         const int64_t piece = most_workgroups(threads);

@@ -45,21 +45,20 @@ class Case:
         self.offsets = first + np.concatenate([[0], np.cumsum(sizes)]).astype(np.int64)
         n = len(lens)
         self.wide = max(1, max((max(l, 0) + BLOCK - 1) // BLOCK for l in lens)) + loose
-        need = sum((max(l, 0) + BLOCK - 1) // BLOCK for l in lens) + 3
+        # blocks in common: those of the group's first sequence that is no padding, as far as both have tokens in front of their last block
+        leader, common = list(range(n)), [0] * n
+        for g, pre in enumerate(shared):
+            members = [s for s in range(self.offsets[g], self.offsets[g + 1]) if lens[s] > 0]
+            for s in members[1:]:
+                leader[s], common[s] = members[0], max(min(pre // BLOCK, (lens[members[0]] - 1) // BLOCK, (lens[s] - 1) // BLOCK), 0)
+        need = sum((max(l, 0) + BLOCK - 1) // BLOCK - c for l, c in zip(lens, common)) + 3
         order = list(rng.permutation(need))
         self.num_blocks = need
         self.table = rng.integers(0, need, (n, self.wide))
         for s, l in enumerate(lens):
-            for i in range((max(l, 0) + BLOCK - 1) // BLOCK):
+            self.table[s, :common[s]] = self.table[leader[s], :common[s]]
+            for i in range(common[s], (max(l, 0) + BLOCK - 1) // BLOCK):
                 self.table[s, i] = order.pop()
-        for g, pre in enumerate(shared):
-            members = [s for s in range(self.offsets[g], self.offsets[g + 1]) if lens[s] > 0]
-            for s in members[1:]:
-                most = min(pre // BLOCK, (lens[members[0]] - 1) // BLOCK, (lens[s] - 1) // BLOCK)
-                self.table[s, :max(most, 0)] = self.table[members[0], :max(most, 0)]
-                # (a longer member than the first: the rest of the common blocks are its own, so the call's claim ends where the shortest does)
-            if members:
-                assert min(lens[s] for s in members) > 0
         for s, l in enumerate(lens):
             if l <= 0:
                 self.table[s] = -(10 ** 6)      # never read
@@ -258,6 +257,19 @@ def test_more_pairs_than_one_launch_takes(B, cache):
     groups = [(48, [60 + (i + g) % 9 for i in range(40 + 37 * (g % 3))]) for g in range(9)]
     case = Case(groups, [33] * 11, 8, 4, cache=cache, seed=7)
     assert len(case.lens) > 512
+    d = case.device()
+    case.call(B, d)
+    case.check(d)
+
+
+@pytest.mark.parametrize("cache", ["same", "fp8"])
+def test_more_units_than_workgroups(B, cache):
+    """Heads of 23 groups that make 560 units, narrow and wide ones, for at most 508 workgroups: some take two, one kind behind the other."""
+    case = Case([(768, [770, 775])] * 10 + [(1280, [1281 + i for i in range(17)])] * 3 + [(768, [769, 790])] * 10, [40], 64, 8, cache=cache, seed=41)
+    d = case.device()
+    case.call(B, d)
+    case.check(d)
+    case = Case([(48, [49, 50])] * 128, [], 8, 4, cache=cache, seed=42)          # 512 units of a few tokens
     d = case.device()
     case.call(B, d)
     case.check(d)

@@ -31,7 +31,7 @@ def _accepted():
 
 
 # ---- add_rms_norm ------------------------------------------------------------------------------------------------------
-def _norm(B, x=PTR, res=PTR, w=PTR, out=PTR + 64, scales=None, rows=4, **kw):
+def _norm(B, x=PTR, res=PTR, w=PTR + 128, out=PTR + 64, scales=None, rows=4, **kw):
     n = B.Norm(cols=64, x_dtype=B.BF16, residual_dtype=B.BF16, weight_dtype=B.BF16, out_format=B.BF16, eps=1e-5)
     for k, v in kw.items():
         setattr(n, k, v)
@@ -45,7 +45,10 @@ def test_norm_refuses(B):
                dict(x_stride=56), dict(residual_stride=56), dict(out_stride=56), dict(x_stride=68), dict(residual_stride=68), dict(out_stride=68), dict(x_stride=-64),
                dict(x=None), dict(w=None), dict(out=None), dict(x=PTR + 8), dict(res=PTR + 8), dict(w=PTR + 8), dict(out=PTR + 8), dict(scales=PTR),
                dict(out_format=B.CODES_INT8), dict(out_format=B.CODES_FP8, scales=PTR + 2), dict(out_format=B.CODES_FP8, scales=PTR, out=PTR + 4),
-               dict(out_format=B.CODES_INT8, scales=PTR, out_stride=68), dict(out=PTR)):
+               dict(out_format=B.CODES_INT8, scales=PTR, out_stride=68),
+               dict(out=PTR),                                                                          # the residual's rows
+               dict(res=None, out=PTR, out_format=B.F32), dict(res=None, out=PTR, out_stride=128), dict(res=None, out=PTR, out_format=B.CODES_FP8, scales=PTR),
+               dict(residual_dtype=B.F32), dict(residual_stride=128)):                                 # x in another type or with another stride
         assert _norm(B, **kw) == B.EINVAL, kw
         assert B.last_error()
     for cols in (4, 63, 65544, 1 << 30):
@@ -81,9 +84,14 @@ def _desc(B, **kw):
     return ctypes.byref(r)
 
 
-def _both(B, q=PTR, k=PTR, f=PTR, rows=4, pos=PTR, cu=PTR, lens=PTR, chunks=1, **kw):
+def _both(B, q=PTR, k=PTR + 2048, f=PTR, rows=4, pos=PTR, cu=PTR, lens=PTR, chunks=1, **kw):
     L, r = B.lib(), _desc(B, **kw)
     return [L.shiftattn_rotary(q, k, pos, rows, f, r, None), L.shiftattn_rotary_mixed(q, k, cu, lens, chunks, rows, 0, f, r, None)]
+
+
+def test_struct_layouts_match_header(B):
+    assert ctypes.sizeof(B.Norm) == 8 * 4 + 3 * 8 and B.Norm.x_stride.offset == 32 and B.Norm.eps.offset == 20
+    assert ctypes.sizeof(B.Rotary) == 8 * 4 + 2 * 8 and B.Rotary.magnitude.offset == 24 and B.Rotary.q_stride.offset == 32
 
 
 def test_rotary_refuses(B):
@@ -91,7 +99,7 @@ def test_rotary_refuses(B):
     assert L.shiftattn_rotary(PTR, PTR, PTR, 1, PTR, None, None) == B.EINVAL and L.shiftattn_rotary_mixed(PTR, PTR, PTR, PTR, 1, 1, 1, PTR, None, None) == B.EINVAL
     for kw in (dict(dtype=2), dict(layout=2), dict(layout=-1), dict(reserved=1), dict(num_q_heads=0), dict(num_kv_heads=-1), dict(num_q_heads=65537), dict(head_dim=0),
                dict(rot_dim=0), dict(rot_dim=144), dict(magnitude=math.nan), dict(magnitude=-math.inf), dict(q_stride=1016), dict(k_stride=120), dict(q_stride=1028),
-               dict(k_stride=132), dict(rows=-1), dict(f=None), dict(f=PTR + 4), dict(q=None, k=None), dict(q=PTR + 8), dict(k=PTR + 8)):
+               dict(k_stride=132), dict(rows=-1), dict(f=None), dict(f=PTR + 4), dict(q=None, k=None), dict(q=PTR + 8), dict(k=PTR + 8), dict(k=PTR)):
         assert _both(B, **kw) == [B.EINVAL] * 2, kw
     for kw in (dict(rot_dim=24), dict(rot_dim=8), dict(head_dim=132), dict(head_dim=264, rot_dim=256), dict(rot_dim=2)):
         assert _both(B, **kw) == [B.EUNSUPPORTED] * 2, kw
