@@ -1,4 +1,20 @@
 // Decode attention of a batch whose groups of sequences have the first blocks of their tables in common (shiftattn_decode_shared).
+//
+// The keys of a sequence are two ranges: S, the blocks in common, and E, its own.  With a reference m_R for each range (any finite number;
+// the result does not depend on it) and
+//     l_R = sum_{t in R} 2^(c z_t - m_R),   o_R = sum_{t in R} 2^(c z_t - m_R) v_t,   m = max m_R,
+// the row is  sum_R 2^(m_R - m) o_R / sum_R 2^(m_R - m) l_R.  o_S needs keys and values of S once for all (sequence, head) pairs of a group,
+// which are then columns of a matrix product (S^T = K Q^T, O^T = V^T P^T) like the heads of one sequence are in the plain kernel.
+//
+// One launch takes both kinds of ranges, a second one joins them.  Every workgroup works out the same plan from lengths and offsets, about
+// 3 us of which most is dependent loads; a launch of its own for the plan took 4 us more.  Workgroups are dealt out by the work that either
+// kind weighs; a unit of shared keys is (tile of columns, KV head, range of keys), a workgroup's own keys are the plain kernel's.
+//
+// What bounds it: the bytes read once are few (256 sequences of 8 heads behind 32768 tokens: 160 MB, 29 us at the copy rate), but each 32
+// tokens cost a tile of 128 columns 128 matrix instructions of 16.4 clocks and 4096 exponentials, and what the vector units do and what the
+// matrix units do adds up on a SIMD: 0.85 us a group of 32 tokens for one workgroup of a compute unit, 1.05 for each of two.  There the main
+// kernel is at 55 % of the rate of a large matrix product.  Few sequences are bounded by the fixed parts: plan 3 us, first loads 3, partial
+// results 2, the merge 4 to 9.  256 sequences behind 32768 tokens: 66 us, where the plain kernel reads 17 GB in 607.
 #include "decode_body.h"
 
 namespace shiftattn {
@@ -12,15 +28,23 @@ constexpr int kWorkgroups = 512;      // two resident per compute unit
 constexpr int kMaxPairs = 1024;       // (sequence, KV head) pairs of a launch
 constexpr int kMaxGroups = 512;
 constexpr double kPlainBytes = 40.0e6;   // cache up to which a batch is the plain kernel's
-constexpr int kMostShared = 508;      // of which take shared keys at most
+constexpr int kMostShared = 508;      // workgroups that take shared keys at most
 constexpr int kStep = 64;             // keys that shared ranges are counted in
 constexpr int kTileCols = 128;        // (sequence, head) columns of a tile whose keys a workgroup's wavefronts share
-constexpr int kNarrowCols = 32;       // and of one that every wavefront takes with keys of its own, where a group has no more than kNarrowMost
-constexpr int kNarrowMost = 64;
+// Columns of a tile that every wavefront takes with keys of its own, where a group has no more: 32 columns of one group of 20000 tokens 16.4
+// us against 17.2 with a wide tile, 16 columns of 24 groups in FP8 27.1 against 29.9, in bf16 27.3 against 25.0.  With narrow tiles up to 64
+// columns, 10 groups of 40 columns took 27.0 us against 25.4 with wide ones, one of 40 18.1 against 17.4, one of 64 18.9 against 17.9.
+constexpr int kNarrowCols = 32;
 constexpr int kMaxRanges = 480;       // ranges that the shared keys of a tile are cut into
 constexpr int kMinSteps = 2;          // steps of a range
-constexpr float kRangeRoot = 0.25f;   // least steps of a range, by the square root of a group's steps
-constexpr int kWideCost = 3, kNarrowCost = 1, kOwnCost = 2;   // time of a step of either kind of tile, and of 32 tokens for each of a workgroup's wavefronts
+// Least steps of a range, by the square root of a group's steps: a range that is too short costs more in the merge than it saves here (a step
+// takes about as long as 16 parts of a row).  Between 0.12 and 0.6 no batch changes by more than 3 %.
+constexpr float kRangeRoot = 0.25f;
+// time of a step of either kind of tile, and of 32 tokens for each of a workgroup's wavefronts (2 instead of 1 for narrow ones: within 1 %)
+constexpr int kWideCost = 3, kNarrowCost = 1, kOwnCost = 2;
+// Sum of a lane's eight weights from which a column's reference moves.  Up to it they stay as they are: a product with values below 2^96
+// cannot overflow.  At 2^8 tiles of 128 columns were 2 % slower, at 2^40 no faster.
+constexpr float kMostSum = 0x1p16f;
 
 // the shared part of a sequence, for the merge: `parts` partial results in units base + (tile + tiles * head) * ranges and on
 struct alignas(32) SharedRow {
@@ -64,7 +88,7 @@ __device__ inline int wave_scan(int v) {   // inclusive
 }
 
 // columns of a tile of a group that has so many, and its tiles
-__device__ inline int tile_cols(int cols) { return cols > kNarrowMost ? kTileCols : kNarrowCols; }
+__device__ inline int tile_cols(int cols) { return cols > kNarrowCols ? kTileCols : kNarrowCols; }
 __device__ inline int tiles_of(int cols) { return (cols + tile_cols(cols) - 1) / tile_cols(cols); }
 
 // One unit: the keys of blocks [first_block, end_block) of a group's table for one KV head, met by the columns [col_first, col_end) of
@@ -159,7 +183,7 @@ struct Columns {
         }
         add_up(0);
         add_up(1);
-        if (there < kGroup || __builtin_amdgcn_ballot_w64(!(sum[0] < 0x1p40f) || !(sum[1] < 0x1p40f))) [[unlikely]] {
+        if (there < kGroup || __builtin_amdgcn_ballot_w64(!(sum[0] < kMostSum) || !(sum[1] < kMostSum))) [[unlikely]] {
             // the unit's first tokens, a reference that is too low, NaN, or a block that does not exist
             const int grp = (threadIdx.x & 63) >> 4;
             const float least = -3.4e38f / fmaxf(c, 1.f);   // the reference stays finite (times c too) where all logits are minus infinity
@@ -528,7 +552,7 @@ __device__ __attribute__((always_inline)) inline void shared_units(const SharedA
         Unit u = {a.block_table + static_cast<size_t>(uniform(gi.leader[g])) * a.max_blocks, range * per, min((range + 1) * per, eff), head, col_first,
                   min(col_first + tile_cols(cols), cols), seq_first, unit};
         if (u.first_block >= eff) continue;   // (uniform) the last ranges of a group may have no keys
-        if (cols > kNarrowMost) wide_unit<kFp8, kScales>(a, u, smem);
+        if (cols > kNarrowCols) wide_unit<kFp8, kScales>(a, u, smem);
         else narrow_unit<kFp8, kScales>(a, u, smem, ref, sums);
     }
 }
@@ -595,7 +619,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
                 cols[x] = (gi.offs[g + 1] - gi.offs[g]) * G;
                 steps[x] = (gi.eff[g] + 3) / 4;
             }
-            weight += steps[x] * a.hkv_l * tiles_of(cols[x]) * (cols[x] > kNarrowMost ? kWideCost : kNarrowCost);
+            weight += steps[x] * a.hkv_l * tiles_of(cols[x]) * (cols[x] > kNarrowCols ? kWideCost : kNarrowCost);
         }
     }
 #pragma unroll
@@ -622,12 +646,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
         for (int x = 0; x < kGroupsPer; ++x) {
             units_of[x] = 0;
             if (steps[x] > 0) {
-                // a range that is too short costs more in the merge than it saves here: a step takes about as long as 16 parts of a row
-                const int cost = cols[x] > kNarrowMost ? kWideCost : kNarrowCost;
+                const int cost = cols[x] > kNarrowCols ? kWideCost : kNarrowCost;
                 const int per = max(max((range + cost - 1) / cost, static_cast<int>(__builtin_sqrtf(static_cast<float>(steps[x])) * kRangeRoot)), a.range_min);
                 int ranges = (steps[x] + per - 1) / per;
                 // workgroup i runs on die i % 8: with a multiple of 4 ranges the tiles and heads of a group find the same keys in the L2
-                // of one die, or of two
+                // of one die, or of two (135 MB read from memory become 20 where 2048 columns meet 32768 tokens)
                 if (ranges >= 16 && cols[x] > kTileCols) ranges &= ~3;
                 gi.ranges[tid * kGroupsPer + x] = static_cast<uint16_t>(ranges);
                 units_of[x] = ranges * a.hkv_l * tiles_of(cols[x]);
@@ -787,12 +810,11 @@ int seqs_per_launch(int max_seq_len, const AttnShape& a) {
     const int64_t by_line = (static_cast<int64_t>(0x7FFFFFFF) - kGroup) / padded / a.hkv_l, by_index = kMaxPairs / a.hkv_l;
     return static_cast<int>(by_line < by_index ? by_line : by_index);
 }
-// units: a launch of `share` workgroups has up to that many ranges and one more for each item, a multiple of 4 of them for an item with
-// at least eight
+// units: a launch of `share` workgroups has up to that many ranges and one more for each item (tile, KV head); the work is summed in float32
 int64_t most_items(int n, int num_groups, const AttnShape& a) {
     return static_cast<int64_t>(a.hkv_l) * (static_cast<int64_t>(n) * (a.hq_l / a.hkv_l) / kNarrowCols + (num_groups < n ? num_groups : n));
 }
-int64_t most_units(int n, int num_groups, const AttnShape& a) { return (kWorkgroups + most_items(n, num_groups, a)) * 11 / 8 + 1; }
+int64_t most_units(int n, int num_groups, const AttnShape& a) { return (kWorkgroups + most_items(n, num_groups, a)) * 9 / 8; }
 // tokens per wavefront so that no row has more than 482 parts of its own, steps per range so that it has no more than 484 shared ones
 int own_r_min(int max_seq_len) {
     const int r = (max_seq_len / 480 + kGroup) / kGroup * kGroup;

@@ -326,6 +326,22 @@ def test_logits_of_minus_infinity_and_far_apart(B):
         assert torch.equal(d["out"], e["out"])
 
 
+@pytest.mark.parametrize("members", [2, 20])
+def test_values_near_the_end_of_the_range(B, members):
+    """Values of 2^100 whose keys weigh 2^39 times what the first ones of every range do: the sums stay in float32 (2^16 * 2^100 * a range)."""
+    case = Case([(640, [650 + i for i in range(members)])], seed=13)
+    case.q[...] = 1
+    case.pages[:, :, 0] = 0
+    for i in range(40):
+        if i // 2 % 2:                        # the second 32 tokens of every 64
+            case.pages[case.table[0, i], :, 0] = P.bf16(np.float32(39 * math.log(2) / math.sqrt(128)))
+    case.pages[:, :, 1] *= np.float32(2.0 ** 100)
+    d = case.device()
+    case.call(B, d)
+    case.check(d)
+    assert np.isfinite(d["out"].float().cpu().numpy()).all()
+
+
 def test_strided_rows_of_any_kind(B):
     import torch
     case = Case([(128, [130, 150, 140])], [20], 8, 2, seed=13)
