@@ -139,6 +139,26 @@ def test_rotary_python_refuses(B):
             calls(**kw)[1]()
 
 
+def test_rows_that_share_memory(B):
+    """Rows that cross, found on the host where their distance is the same; rows side by side, between each other and behind each other are not."""
+    row = 64 * 2
+    norm = lambda **kw: _norm(B, **{**dict(x=PTR, res=None, out=PTR + 8192, w=PTR + 0x8000), **kw})
+    for at in (16, row - 16, row, 3 * row, 4 * row - 16, -16, -row, -4 * row + 16):
+        assert norm(out=PTR + at) == B.EINVAL and "share memory" in B.last_error()
+        assert norm(res=PTR + at) == B.EINVAL and norm(res=PTR + 8192 + at) == B.EINVAL
+        assert norm(out=PTR + at, x_stride=32 + 64, out_stride=32 + 64) == B.EINVAL
+    assert norm(out=PTR + 16, rows=1, out_stride=128) == B.EINVAL and norm(out=PTR + 16, out_format=B.F32, out_stride=64, x_stride=128) == B.EINVAL
+    # heads 0 .. 7 and 8 of rows of ten are apart, heads 0 .. 7 and 7 are not, nor heads 9 .. 16 of rows of ten and 7 (the first of the next row)
+    fused = dict(q_stride=1280, k_stride=1280)
+    for k in (7, -9, 10 - 1 - 9, 37, 30):
+        assert _both(B, k=PTR + 256 * k, **fused) == [B.EINVAL] * 2 and "heads" in B.last_error(), k
+    assert _both(B, k=PTR + 1024, rows=1) == [B.EINVAL] * 2
+    # side by side: refused for what comes behind in the order of the checks
+    for k in (8, 9, -1, -2, 40, 38):
+        assert _both(B, k=PTR + 256 * k, pos=PTR + 2, lens=PTR + 2, **fused) == [B.EINVAL] * 2 and "heads" not in B.last_error(), k
+    assert _both(B, k=PTR + 2048, rows=1, pos=None, lens=None) == [B.EINVAL] * 2 and "heads" not in B.last_error()
+
+
 def test_frequencies(B):
     """Each scaling from its definition, and at the ends where it changes nothing or divides by the factor."""
     i = np.arange(64)
