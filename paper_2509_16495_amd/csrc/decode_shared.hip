@@ -12,9 +12,14 @@
 //
 // What bounds it: the bytes read once are few (256 sequences of 8 heads behind 32768 tokens: 160 MB, 29 us at the copy rate), but each 32
 // tokens cost a tile of 128 columns 128 matrix instructions of 16.4 clocks and 4096 exponentials, and what the vector units do and what the
-// matrix units do adds up on a SIMD: 0.85 us a group of 32 tokens for one workgroup of a compute unit, 1.05 for each of two.  There the main
-// kernel is at 55 % of the rate of a large matrix product.  Few sequences are bounded by the fixed parts: plan 3 us, first loads 3, partial
-// results 2, the merge 4 to 9.  256 sequences behind 32768 tokens: 66 us, where the plain kernel reads 17 GB in 607.
+// matrix units do adds up on a SIMD: 0.85 us a group of 32 tokens for one workgroup of a compute unit, 0.8 to 1.0 for each of two, where the
+// matrix units are busy half of the time.  Neither the barrier (1 us of 55 without it), nor keys out of a hot L2, nor 32x32x16 instructions
+// (4 % less for one workgroup, 5 % more for two), nor exponentials in front of the first matrix instructions change that.  Few sequences are
+// bounded by the fixed parts: plan 3 us, first loads 3, partial results 2, the merge 4 to 9.  256 sequences behind 32768 tokens: 67 us, where the
+// plain kernel reads 17 GB in 607.
+// Workgroups of eight wavefronts whose halves take every other group and add their sums in LDS write half as many parts (64 sequences behind
+// 32768 tokens 28.1 us against 31.7), but a compute unit draws only so many bytes, and those with the sequences' own keys are then fewer (256 with
+// up to 2000 of their own 84 to 113 us against 67): not taken.
 #include "decode_body.h"
 
 namespace shiftattn {
@@ -40,8 +45,10 @@ constexpr int kMinSteps = 2;          // steps of a range
 // Least steps of a range, by the square root of a group's steps: a range that is too short costs more in the merge than it saves here (a step
 // takes about as long as 16 parts of a row).  Between 0.12 and 0.6 no batch changes by more than 3 %.
 constexpr float kRangeRoot = 0.25f;
-// time of a step of either kind of tile, and of 32 tokens for each of a workgroup's wavefronts (2 instead of 1 for narrow ones: within 1 %)
-constexpr int kWideCost = 3, kNarrowCost = 1, kOwnCost = 2;
+// Time of a step of either kind of tile, and of 32 tokens for each of a workgroup's wavefronts, which have one group of 32 on its way each: 2 us
+// in bf16 as in FP8.  With 2 for those, 180 sequences of up to 600 tokens behind 20000 took 55.0 us (39.6 with 4; FP8 50.9 and 42.7), 10 groups
+// of 8 behind 6000 28.5 (24.5; 26.1 and 23.2), 8 groups over an FP8 cache 44.0 (44.1 to 45.5); with 6 these took 47.0.  Narrow steps at 2: within 1 %.
+constexpr int kWideCost = 3, kNarrowCost = 1, kOwnCost = 4;
 // Sum of a lane's eight weights from which a column's reference moves.  Up to it they stay as they are: a product with values below 2^96
 // cannot overflow.  At 2^8 tiles of 128 columns were 2 % slower, at 2^40 no faster.
 constexpr float kMostSum = 0x1p16f;
