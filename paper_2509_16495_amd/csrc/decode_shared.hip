@@ -379,7 +379,7 @@ __device__ __attribute__((always_inline)) inline void wide_unit(const SharedArgs
                              "global_load_lds_dwordx4 %1, %5\n\t"
                              "global_load_lds_dwordx4 %2, %5 offset:1024\n\t"
                              "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
-                             "global_load_lds_dwordx4 %4, %5 offset:3072"
+                             "global_load_lds_dwordx4 %4, %5 offset:0xc00"
                              :: "s"(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem)) + (g & 3) * kStageBytes + zero_at), "v"(place[0]), "v"(place[1]), "v"(place[2]),
                                 "v"(place[3]), "s"(a.cache + from) : "memory");
             }
