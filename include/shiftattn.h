@@ -419,7 +419,8 @@ int shiftattn_decode_static(const void *q, const void *k_new, const void *v_new,
  *   shared_lens (device, in)  : int32 [num_groups]: so many first tokens the sequences of a group have in common.  Of those the whole blocks
  *                 are shared: entries 0 .. shared_lens[i] / 16 - 1 of the sequences' rows of block_table name the same blocks
  *                 (as far as a sequence has tokens; entries of padding rows are not read).  What remains of shared_lens[i] / 16 lies in blocks of
- *                 each sequence's own.  <= 0: nothing in common
+ *                 each sequence's own.  <= 0: nothing in common.  A group shares what the shortest of its sequences has in front of its last
+                 token's block, and nothing where that would save less than it takes
  *   kv_scales: the scales of a cache with block scales (a->kv_format = SHIFTATTN_KV_FP8_E4M3_BLOCKS), NULL for any other
  *   All else as in shiftattn_decode; a token that is appended must lie behind the blocks in common.
  * bf16 rows with head_dim 128 and up to 16 query heads per KV head, and up to 512 groups, take the kernel that shares; any other call is
@@ -562,7 +563,7 @@ int32_t shiftattn_use_base_config(int32_t n_tokens, int32_t threshold);
  *                                can land one bf16 step from the correctly rounded value.  Tiles whose softmax
  *                                sums leave [2^-40, 2^40] are recomputed on Q as given.  Off by default
  *   SHIFTATTN_OPT_DECODE_SHARED  1 | 2: shiftattn_decode_shared takes the kernel that shares wherever it can (1), or never (2),
- *                                whatever the size of the batch
+ *                                whatever the size of the batch and however little its groups have in common
  *   set returns EINVAL for an unknown option or value; get returns -1 for an unknown option. */
 enum { SHIFTATTN_OPT_PREFILL_TILE = 0, SHIFTATTN_OPT_PREFILL_SPLITS = 1, SHIFTATTN_OPT_GENERIC_ONLY = 2,
        SHIFTATTN_OPT_PREFILL_PAIRING = 3, SHIFTATTN_OPT_PREFILL_SCALED_Q = 4, SHIFTATTN_OPT_DECODE_SHARED = 5, SHIFTATTN_OPT_COUNT = 6 };

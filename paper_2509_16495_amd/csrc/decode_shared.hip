@@ -21,34 +21,21 @@
 // 32768 tokens 28.1 us against 31.7), but a compute unit draws only so many bytes, and those with the sequences' own keys are then fewer (256 with
 // up to 2000 of their own 84 to 113 us against 67): not taken.
 #include "decode_body.h"
+#include "shared_deal.h"
 
 namespace shiftattn {
 
 namespace {
 
 using namespace decode_flat;
+using namespace shared_deal;
 
 constexpr int kWaves = 4;
-constexpr int kWorkgroups = 512;      // two resident per compute unit
 constexpr int kMaxPairs = 1024;       // (sequence, KV head) pairs of a launch
 constexpr int kMaxGroups = 512;
 constexpr double kPlainBytes = 40.0e6;   // cache up to which a batch is the plain kernel's
-constexpr int kMostShared = 508;      // workgroups that take shared keys at most
-constexpr int kStep = 64;             // keys that shared ranges are counted in
-constexpr int kTileCols = 128;        // (sequence, head) columns of a tile whose keys a workgroup's wavefronts share
-// Columns of a tile that every wavefront takes with keys of its own, where a group has no more: 32 columns of one group of 20000 tokens 16.4
-// us against 17.2 with a wide tile, 16 columns of 24 groups in FP8 27.1 against 29.9, in bf16 27.3 against 25.0.  With narrow tiles up to 64
-// columns, 10 groups of 40 columns took 27.0 us against 25.4 with wide ones, one of 40 18.1 against 17.4, one of 64 18.9 against 17.9.
-constexpr int kNarrowCols = 32;
 constexpr int kMaxRanges = 480;       // ranges that the shared keys of a tile are cut into
 constexpr int kMinSteps = 2;          // steps of a range
-// Least steps of a range, by the square root of a group's steps: a range that is too short costs more in the merge than it saves here (a step
-// takes about as long as 16 parts of a row).  Between 0.12 and 0.6 no batch changes by more than 3 %.
-constexpr float kRangeRoot = 0.25f;
-// Time of a step of either kind of tile, and of 32 tokens for each of a workgroup's wavefronts, which have one group of 32 on its way each: 2 us
-// in bf16 as in FP8.  With 2 for those, 180 sequences of up to 600 tokens behind 20000 took 55.0 us (39.6 with 4; FP8 50.9 and 42.7), 10 groups
-// of 8 behind 6000 28.5 (24.5; 26.1 and 23.2), 8 groups over an FP8 cache 44.0 (44.1 to 45.5); with 6 these took 47.0.  Narrow steps at 2: within 1 %.
-constexpr int kWideCost = 3, kNarrowCost = 1, kOwnCost = 4;
 // Sum of a lane's eight weights from which a column's reference moves.  Up to it they stay as they are: a product with values below 2^96
 // cannot overflow.  At 2^8 tiles of 128 columns were 2 % slower, at 2^40 no faster.
 constexpr float kMostSum = 0x1p16f;
@@ -81,6 +68,7 @@ struct SharedArgs {
     SharedRow* rows;
     int64_t q_stride;
     int num_groups, first_seq, num_seqs, max_blocks, hq_l, hkv_l, r_min, range_min;
+    bool always;          // groups share whatever that costs
     float c;
 };
 
@@ -93,10 +81,6 @@ __device__ inline int wave_scan(int v) {   // inclusive
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 into rows 2 and 3
     return v;
 }
-
-// columns of a tile of a group that has so many, and its tiles
-__device__ inline int tile_cols(int cols) { return cols > kNarrowCols ? kTileCols : kNarrowCols; }
-__device__ inline int tiles_of(int cols) { return (cols + tile_cols(cols) - 1) / tile_cols(cols); }
 
 // One unit: the keys of blocks [first_block, end_block) of a group's table for one KV head, met by the columns [col_first, col_end) of
 // the group ((sequence, head) pairs of that KV head's heads), up to 128, or up to 32 (kNarrow).
@@ -535,15 +519,31 @@ __device__ __attribute__((always_inline)) inline void narrow_unit(const SharedAr
     __syncthreads();   // (a next unit writes where this one reads)
 }
 
-// units [first, all) in strides of n_wg
+// the first unit that begins at weight x of the line or behind it (weights: where each group's units begin; uniform)
+__device__ inline int first_unit(const SharedArgs& a, const GroupIndex& gi, const int* weights, uint32_t x) {
+    const int lane = threadIdx.x & 63;
+    for (int at = 0; at < a.num_groups; at += 64) {
+        const int i = min(at + lane, a.num_groups - 1);
+        const uint64_t m = __builtin_amdgcn_ballot_w64(static_cast<uint32_t>(weights[i]) < x && static_cast<uint32_t>(weights[i + 1]) >= x);
+        if (m) {
+            const int g = __builtin_amdgcn_readfirstlane(at + __builtin_ctzll(m));
+            const uint32_t from = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(weights[g])), to = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(weights[g + 1]));
+            const int first = __builtin_amdgcn_readfirstlane(gi.units[g]), n = __builtin_amdgcn_readfirstlane(gi.units[g + 1]) - first;
+            return first + units_before(x, from, (to - from) / n, n);
+        }
+    }
+    return 0;   // x = 0
+}
+
+// units [first, end)
 template <bool kFp8, int kScales>
 __device__ __attribute__((always_inline)) inline void shared_units(const SharedArgs& a, const GroupIndex& gi, unsigned char* smem, float (&ref)[kWaves][kNarrowCols],
-                                                                  float (&sums)[kWaves][kNarrowCols], int first, int n_wg, int all) {
+                                                                  float (&sums)[kWaves][kNarrowCols], int first, int end) {
     const int lane = threadIdx.x & 63;
     const int G = a.hq_l / a.hkv_l;
     auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
 #pragma unroll 1
-    for (int unit = first; unit < all; unit += n_wg) {
+    for (int unit = first; unit < end; ++unit) {
         int g = 0;
         for (int at = 0; at < a.num_groups; at += 64) {   // the group that the unit belongs to
             const int i = min(at + lane, a.num_groups - 1);
@@ -555,7 +555,7 @@ __device__ __attribute__((always_inline)) inline void shared_units(const SharedA
         }
         const int eff = uniform(gi.eff[g]), ranges = uniform(gi.ranges[g]), seq_first = uniform(gi.offs[g]), cols = (uniform(gi.offs[g + 1]) - seq_first) * G;
         const int local = unit - uniform(gi.units[g]), item = uniform(local / ranges), range = local - item * ranges, tiles = tiles_of(cols);
-        const int per = uniform(((eff + 3) / 4 + ranges - 1) / ranges) * 4, head = uniform(item / tiles), col_first = (item - head * tiles) * tile_cols(cols);
+        const int per = uniform(range_steps(steps_of(eff), ranges)) * 4, head = uniform(item / tiles), col_first = (item - head * tiles) * tile_cols(cols);
         Unit u = {a.block_table + static_cast<size_t>(uniform(gi.leader[g])) * a.max_blocks, range * per, min((range + 1) * per, eff), head, col_first,
                   min(col_first + tile_cols(cols), cols), seq_first, unit};
         if (u.first_block >= eff) continue;   // (uniform) the last ranges of a group may have no keys
@@ -613,6 +613,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
     }
     __syncthreads();
     // ---- what there is to do: steps of all tiles, weighted, and groups of 32 tokens that the sequences have to themselves ----
+    auto eff_of = [&](int g) -> int {
+        const int members = gi.offs[g + 1] - gi.offs[g];
+        return a.always || pays(gi.eff[g], members, members * G) ? gi.eff[g] : 0;
+    };
     int cols[kGroupsPer], steps[kGroupsPer];   // thread t owns groups kGroupsPer t and following
     int weight = 0, own = 0;
 #pragma unroll
@@ -624,14 +628,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
             gi.leader[g] = static_cast<uint16_t>(leader);
             if (leader < n) {
                 cols[x] = (gi.offs[g + 1] - gi.offs[g]) * G;
-                steps[x] = (gi.eff[g] + 3) / 4;
+                steps[x] = steps_of(eff_of(g));
             }
-            weight += steps[x] * a.hkv_l * tiles_of(cols[x]) * (cols[x] > kNarrowCols ? kWideCost : kNarrowCost);
+            weight += steps[x] * a.hkv_l * tiles_of(cols[x]) * cost_of(cols[x]);
         }
     }
 #pragma unroll
     for (int x = 0; x < kSeqs; ++x) {
-        const int f = mine[x] >= 0 ? gi.eff[mine[x]] : 0;
+        const int f = mine[x] >= 0 ? eff_of(mine[x]) : 0;
         from[tid + x * kThreads] = f;
         own += (max(len[x], 0) - f * kBlockSize + kGroup - 1) / kGroup;
     }
@@ -643,24 +647,24 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) cost_p += static_cast<float>(gi.sums[0][w]), cost_s += static_cast<float>(gi.sums[1][w]);
     cost_s *= static_cast<float>(a.hkv_l * kOwnCost) / kWaves;
+#pragma unroll
+    for (int x = 0; x < kGroupsPer; ++x)
+        if (steps[x] == 0 && tid * kGroupsPer + x < a.num_groups) gi.eff[tid * kGroupsPer + x] = 0;   // (all have read it)
     // ---- ranges: so long that the shared keys take the workgroups that are theirs by weight ----
+    const int wg = blockIdx.x;
     int n_p = 0, all = 0;
     if (cost_p > 0) {   // uniform
-        const float share = fminf(fmaxf(floorf(kWorkgroups * cost_p / (cost_p + cost_s)), 1.f), kWorkgroups - 1.f);
-        const int range = static_cast<int>(ceilf(cost_p / share));   // weighted steps of a workgroup
-        int units_of[kGroupsPer], units = 0;
+        const float share = share_of(cost_p, cost_s);
+        const int range = range_of(cost_p, cost_s);
+        int units_of[kGroupsPer], each_of[kGroupsPer], units = 0;
 #pragma unroll
         for (int x = 0; x < kGroupsPer; ++x) {
-            units_of[x] = 0;
+            units_of[x] = each_of[x] = 0;
             if (steps[x] > 0) {
-                const int cost = cols[x] > kNarrowCols ? kWideCost : kNarrowCost;
-                const int per = max(max((range + cost - 1) / cost, static_cast<int>(__builtin_sqrtf(static_cast<float>(steps[x])) * kRangeRoot)), a.range_min);
-                int ranges = (steps[x] + per - 1) / per;
-                // workgroup i runs on die i % 8: with a multiple of 4 ranges the tiles and heads of a group find the same keys in the L2
-                // of one die, or of two (135 MB read from memory become 20 where 2048 columns meet 32768 tokens)
-                if (ranges >= 16 && cols[x] > kTileCols) ranges &= ~3;
+                const int ranges = ranges_of(steps[x], cols[x], range, a.range_min);
                 gi.ranges[tid * kGroupsPer + x] = static_cast<uint16_t>(ranges);
                 units_of[x] = ranges * a.hkv_l * tiles_of(cols[x]);
+                each_of[x] = weight_of(steps[x], ranges, cols[x]);
             }
             units += units_of[x];
         }
@@ -680,11 +684,41 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
             run += units_of[x];
         }
         if (tid == 0) gi.units[a.num_groups] = all;
-        n_p = min(all, kMostShared);
+        n_p = all;
+        if (all > share || all > kMostShared) {   // uniform: more units than the shared keys' part of the workgroups
+            uint32_t weighs = 0, longest = 0;   // as the units are: their last ranges may be shorter
+#pragma unroll
+            for (int x = 0; x < kGroupsPer; ++x) {
+                weighs += static_cast<uint32_t>(units_of[x]) * each_of[x];
+                longest = max(longest, static_cast<uint32_t>(each_of[x]));
+            }
+            const uint32_t weighs_to = static_cast<uint32_t>(wave_scan(static_cast<int>(weighs)));
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) longest = max(longest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(longest), o)));
+            if (lane == 63) gi.sums[0][wave] = static_cast<int>(weighs_to), gi.sums[1][wave] = static_cast<int>(longest);
+            __syncthreads();
+            uint32_t line = 0, at = weighs_to - weighs;
+            longest = 0;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                if (w < wave) at += static_cast<uint32_t>(gi.sums[0][w]);
+                line += static_cast<uint32_t>(gi.sums[0][w]);
+                longest = max(longest, static_cast<uint32_t>(gi.sums[1][w]));
+            }
+            n_p = workgroups_of(all, static_cast<float>(line), static_cast<float>(longest), cost_s);
+            if (wg < n_p && n_p < all) {   // (a workgroup needs the weights or the sequences' first blocks)
+#pragma unroll
+                for (int x = 0; x < kGroupsPer; ++x) {
+                    const int g = tid * kGroupsPer + x;
+                    if (g <= a.num_groups) from[g] = static_cast<int>(at);
+                    at += static_cast<uint32_t>(units_of[x]) * each_of[x];
+                }
+                if (tid == 0) from[a.num_groups] = static_cast<int>(line);
+            }
+        }
     }
     n_p = __builtin_amdgcn_readfirstlane(n_p);
     all = __builtin_amdgcn_readfirstlane(all);
-    const int wg = blockIdx.x;
     if (wg == kWorkgroups - 1) {   // for the merge
         __syncthreads();
 #pragma unroll
@@ -694,7 +728,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
             SharedRow r = {};
             const int g = mine[x];
             if (g >= 0 && gi.eff[g] > 0) {
-                const int c = (gi.offs[g + 1] - gi.offs[g]) * G, st = (gi.eff[g] + 3) / 4, per = (st + gi.ranges[g] - 1) / gi.ranges[g];
+                const int c = (gi.offs[g + 1] - gi.offs[g]) * G, st = steps_of(gi.eff[g]), per = range_steps(st, gi.ranges[g]);
                 r = SharedRow{gi.units[g], gi.ranges[g], (st + per - 1) / per, tiles_of(c), (s - gi.offs[g]) * G, tile_cols(c), {0, 0}};
             }
             a.rows[s] = r;
@@ -702,7 +736,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
     }
     if (wg < n_p) {
         __syncthreads();
-        shared_units<kFp8, kBlockScales ? 1 : 0>(a, gi, smem, ref, sums, wg, n_p, all);
+        int first = wg, end = wg + 1;
+        if (n_p < all) {
+            const uint32_t line = static_cast<uint32_t>(from[a.num_groups]);
+            first = first_unit(a, gi, from, first_of(line, n_p, wg));
+            end = first_unit(a, gi, from, first_of(line, n_p, wg + 1));
+        }
+        shared_units<kFp8, kBlockScales ? 1 : 0>(a, gi, smem, ref, sums, first, end);
         return;
     }
     decode_flat_body<kFp8, kAppend, kWaves, false, kBlockScales ? 1 : 0, kMaxPairs, true>(
@@ -869,7 +909,7 @@ hipError_t launch_decode_shared(const void* q, const void* k_new, const void* v_
         const SharedArgs args = {static_cast<const uint16_t*>(q) + static_cast<size_t>(s0) * a.q_stride, static_cast<uint16_t*>(cache),
                                  block_table + static_cast<size_t>(s0) * a.max_blocks, seq_lens + s0, group_offsets, shared_lens, a.kv_scales, o_part, ml_part, plan,
                                  o_shared, ml_shared, info, a.q_stride, num_groups, s0, n, a.max_blocks, a.hq_l, a.hkv_l, own_r_min(max_seq_len),
-                                 range_min(max_seq_len), a.scale * a.k_scale * 1.4426950408889634f};
+                                 range_min(max_seq_len), option_decode_shared() == 1, a.scale * a.k_scale * 1.4426950408889634f};
         const AppendArgs ap = {append ? static_cast<const uint16_t*>(k_new) + static_cast<size_t>(s0) * a.kv_stride : nullptr,
                                append ? static_cast<const uint16_t*>(v_new) + static_cast<size_t>(s0) * a.kv_stride : nullptr,
                                append ? slots + s0 : nullptr, a.kv_stride, a.k_scale, a.v_scale, a.kv_scales};
