@@ -521,6 +521,7 @@ int shiftattn_tables_truncate(const shiftattn_tables *t, const int32_t *keep_len
 size_t shiftattn_prefill_workspace_bytes(int32_t num_seqs, int32_t total_q, int32_t max_q_len,
                                          int32_t max_seq_len, const shiftattn_attn *a);
 size_t shiftattn_decode_workspace_bytes(int32_t num_seqs, int32_t max_seq_len, const shiftattn_attn *a);
+/* ... holds, under the same options, every call of up to so many sequences, tokens and groups (num_groups up to num_seqs or 512) */
 size_t shiftattn_decode_shared_workspace_bytes(int32_t num_seqs, int32_t max_seq_len, int32_t num_groups, const shiftattn_attn *a);
 size_t shiftattn_mixed_workspace_bytes(int32_t num_prefill_seqs, int32_t total_prefill_q, int32_t max_q_len,
                                        int32_t max_prefill_seq_len, int32_t num_decode_seqs,

@@ -7,6 +7,7 @@
 #include <stdio.h>
 #include <stdlib.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <mutex>
@@ -960,8 +961,10 @@ int shiftattn_decode_shared(const void* q, const void* k_new, const void* v_new,
 size_t shiftattn_decode_shared_workspace_bytes(int32_t num_seqs, int32_t max_seq_len, int32_t num_groups, const shiftattn_attn* a) {
     AttnShape s;
     if (check_attn(a, &s) || num_seqs < 0 || max_seq_len < 0 || num_groups < 0) return SIZE_MAX;
-    if (num_seqs == 0 || !use_decode_shared(s, num_seqs, max_seq_len, num_groups)) return shiftattn_decode_workspace_bytes(num_seqs, max_seq_len, a);
-    return decode_shared_workspace(num_seqs, max_seq_len, num_groups, s);
+    // large enough for every smaller call: batches of more groups, or of longer sequences, may be those that need less
+    const size_t shared = num_seqs == 0 || force_generic() ? 0 : decode_shared_most_workspace(num_seqs, max_seq_len, num_groups, s);
+    const size_t plain = shiftattn_decode_workspace_bytes(num_seqs, max_seq_len, a), short_plain = shiftattn_decode_workspace_bytes(num_seqs, 0, a);
+    return std::max({shared, plain, short_plain});
 }
 
 int shiftattn_decode_static(const void* q, const void* k_new, const void* v_new, const int64_t* slot_mapping, void* kv_cache,

@@ -873,23 +873,39 @@ int range_min(int max_seq_len) {
 }
 size_t rows_of(int n, const AttnShape& a) { return decode_mfma_rows_for(kWorkgroups * kWaves, n, a); }
 
-}  // namespace
-
-bool decode_shared_supported(const AttnShape& a, int num_seqs, int max_seq_len, int num_groups) {
-    if (num_groups < 1 || num_groups > kMaxGroups || !decode_mfma_supported(a, num_seqs, max_seq_len) || a.hkv_l > kMaxPairs) return false;
-    if (option_decode_shared() == 2) return false;
+// is a batch the kernel's that shares?
+bool large_enough(int num_seqs, int max_seq_len, const AttnShape& a) {
+    if (option_decode_shared() != 0) return option_decode_shared() == 1;
     // A batch that is small even if every sequence has max_seq_len tokens reads its shared keys again and again from the caches, and the plain
     // kernel, which has no groups to work out and fewer parts to merge, is done first: of 48 batches it was 1.0 to 3.5 us faster in all but one
     // below 40 MB (10.9 against 13.5 us at 10 MB), even at 45 to 60, slower above (27 against 22 at 98, 150 against 45 at 1061).
     const double bytes = 2.0 * kD * a.kv_elem * a.hkv_l * num_seqs * max_seq_len;
-    if (option_decode_shared() != 1 && bytes <= kPlainBytes) return false;
+    return bytes > kPlainBytes;
+}
+size_t size_of(int n, int num_groups, const AttnShape& a) {
+    return (rows_of(n, a) + static_cast<size_t>(most_units(n, num_groups, a)) * kTileCols) * (kD + 2) * sizeof(float) + static_cast<size_t>(n) * (a.hkv_l * sizeof(int2) + sizeof(SharedRow)) + 32;
+}
+
+}  // namespace
+
+bool decode_shared_supported(const AttnShape& a, int num_seqs, int max_seq_len, int num_groups) {
+    if (num_groups < 1 || num_groups > kMaxGroups || !decode_mfma_supported(a, num_seqs, max_seq_len) || a.hkv_l > kMaxPairs) return false;
+    if (!large_enough(num_seqs, max_seq_len, a)) return false;
     const int per = seqs_per_launch(max_seq_len, a), n = num_seqs < per ? num_seqs : per;
     return per >= 1 && most_items(n, num_groups, a) * (max_seq_len / kStep + 1) < 0x7FFFFFFF / kWideCost;
 }
 
 size_t decode_shared_workspace(int num_seqs, int max_seq_len, int num_groups, const AttnShape& a) {
-    const int per = seqs_per_launch(max_seq_len, a), n = num_seqs < per ? num_seqs : per;
-    return (rows_of(n, a) + static_cast<size_t>(most_units(n, num_groups, a)) * kTileCols) * (kD + 2) * sizeof(float) + static_cast<size_t>(n) * (a.hkv_l * sizeof(int2) + sizeof(SharedRow)) + 32;
+    const int per = seqs_per_launch(max_seq_len, a);
+    return size_of(num_seqs < per ? num_seqs : per, num_groups, a);
+}
+
+size_t decode_shared_most_workspace(int num_seqs, int max_seq_len, int num_groups, const AttnShape& a) {
+    if (num_groups < 1 || (num_groups > kMaxGroups && num_groups > num_seqs) || !decode_mfma_supported(a, num_seqs, 0) || a.hkv_l > kMaxPairs ||
+        !large_enough(num_seqs, max_seq_len, a))
+        return 0;
+    const int per = seqs_per_launch(0, a);   // a launch of shorter sequences has more of them
+    return size_of(num_seqs < per ? num_seqs : per, num_groups < kMaxGroups ? num_groups : kMaxGroups, a);
 }
 
 hipError_t launch_decode_shared(const void* q, const void* k_new, const void* v_new, const int64_t* slots, void* cache, const int32_t* block_table,

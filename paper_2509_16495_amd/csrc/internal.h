@@ -128,7 +128,10 @@ hipError_t launch_decode_mfma(const void* q, const void* k_new, const void* v_ne
 
 // decode_shared.hip : the same operation where groups of sequences have the first blocks of their tables in common
 bool decode_shared_supported(const AttnShape& a, int num_seqs, int max_seq_len, int num_groups);
+// what a launch needs, and what every one of up to so many sequences, tokens and groups needs (0: none of them is this kernel's; more groups
+// than it indexes: num_groups > num_seqs is not asked for)
 size_t decode_shared_workspace(int num_seqs, int max_seq_len, int num_groups, const AttnShape& a);
+size_t decode_shared_most_workspace(int num_seqs, int max_seq_len, int num_groups, const AttnShape& a);
 hipError_t launch_decode_shared(const void* q, const void* k_new, const void* v_new, const int64_t* slots, void* cache, const int32_t* block_table,
                                 const int32_t* seq_lens, int num_seqs, int max_seq_len, const int32_t* group_offsets, const int32_t* shared_lens,
                                 int num_groups, void* out, void* workspace, const AttnShape& a, hipStream_t st);

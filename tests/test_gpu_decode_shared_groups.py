@@ -43,3 +43,15 @@ def test_groups_that_are_left_alone(B, groups, cache):
         case.check(d)
     finally:
         B.set_option(B.OPT_DECODE_SHARED, 1)
+
+
+def test_one_workspace_for_batches_of_any_number_of_groups(B):
+    """Sized for the most sequences, tokens and groups, which are the plain kernel's, and taken by every smaller batch."""
+    import torch
+    cases = [Case([(32, [33 + i % 3, 40]) for i in range(n)], [50], seed=n) for n in (600, 512, 300, 3)]
+    ds = [c.device() for c in cases]
+    a = B.attn_desc(ds[0]["q"], ds[0]["cache"], ds[0]["table"], cases[0].scale, ds[0]["k"], ds[0]["out"])
+    ws = torch.full((B.decode_shared_workspace_bytes(1201, 50, 600, a),), 0xFF, dtype=torch.uint8, device="cuda:0")
+    for c, d in zip(cases, ds):
+        c.call(B, d, workspace=ws)
+        c.check(d)
