@@ -273,7 +273,7 @@ int shiftattn_unpack_o_proj_int8_ws(const void *recv_codes, const float *a_scale
  *   residual (device, in/out)    : [rows][cols], bf16 or float32, row stride residual_stride, or NULL
  *   weight (device, in)          : [cols], bf16 or float32; weight_offset 1 is for weights stored as their difference from 1
  *   out (device, out)            : [rows][cols] in out_format, row stride out_stride.  x and out, or x and residual, may be the same rows (same type
- *                                  and stride); rows that share memory in any other way are not allowed
+ *                                  and stride); rows that share memory in any other way are refused (EINVAL)
  *   scales (device, out)         : float32 [rows] for codes, else NULL
  * A NaN in h makes all of the row's y NaN, an infinity makes them 0 but for a NaN in its own place (scale 1 in both cases).
  * cols: a multiple of 8 up to 65536 (else EUNSUPPORTED); eps > 0.  Pointers 16-byte aligned (scales: 4), row strides multiples of 16 bytes (codes: 8).  0 as a stride stands for dense rows. */
@@ -294,7 +294,7 @@ int shiftattn_add_rms_norm(const void *x, void *residual, const void *weight, vo
  * for pair i of a row at position p, m = magnitude, in float32, rounded once; t is reduced in 64 bits (exact to float32 at any
  * position).  Pair i is elements i and i + rot_dim / 2 (SHIFTATTN_ROTARY_HALVES) or 2 i and 2 i + 1 (SHIFTATTN_ROTARY_PAIRS).
  *   q, k (device, in/out)      : [rows][heads][head_dim], row strides q_stride, k_stride: views into one fused buffer as the attention
- *                                calls take them (K is cached turned).  Either may be NULL; no head may be in both.
+ *                                calls take them (K is cached turned).  Either may be NULL; heads that share memory are refused (EINVAL).
  *   frequencies (device, in)   : float64 [rot_dim / 2], radians per position (shiftattn_rotary_frequencies makes them)
  * rotary: positions (device, in): int32 [rows]; a negative one (padding) leaves the row as it is.
  * rotary_mixed: the rows of a unified batch, positions from what shiftattn_mixed takes: row cu_seqlens_q[s] + i is token i of the

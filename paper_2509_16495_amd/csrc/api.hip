@@ -13,6 +13,7 @@
 #include <mutex>
 
 #include "internal.h"
+#include "rows_touch.h"
 
 using namespace shiftattn;
 
@@ -221,15 +222,11 @@ int check_decode_args(const void* q, const void* kv_cache, const int32_t* block_
 
 bool aligned_to(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
-// `rows` rows of a_bytes from a and of b_bytes from b on, one behind the other at the same distance (or one row each): do they share bytes
-// without being the same rows?
-bool cross(const void* a, int64_t a_bytes, int64_t a_stride, const void* b, int64_t b_bytes, int64_t b_stride, int64_t rows) {
-    if (!a || !b || a == b || (rows > 1 && a_stride != b_stride)) return false;
-    const bool a_first = reinterpret_cast<uintptr_t>(a) < reinterpret_cast<uintptr_t>(b);
-    const uint64_t d = a_first ? reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a) : reinterpret_cast<uintptr_t>(a) - reinterpret_cast<uintptr_t>(b);
-    const uint64_t front = a_first ? a_bytes : b_bytes, back = a_first ? b_bytes : a_bytes;
-    const uint64_t stride = a_stride > b_stride ? a_stride : b_stride, n = d / stride, m = d % stride;
-    return n < static_cast<uint64_t>(rows) && (m < front || (m + back > stride && n + 1 < static_cast<uint64_t>(rows)));
+// `rows` rows of a_bytes, a_stride apart from a on, and of b_bytes from b on: do they share bytes without being the same rows?  (The same
+// start is the caller's to look at.)
+bool cross(const void* a, int64_t a_bytes, int64_t a_stride, const void* b, int64_t b_bytes, int64_t b_stride, int elem_a, int elem_b, int64_t rows) {
+    return a && b && a != b &&
+           rows_touch(reinterpret_cast<uintptr_t>(a), a_bytes, static_cast<__int128>(a_stride) * elem_a, reinterpret_cast<uintptr_t>(b), b_bytes, static_cast<__int128>(b_stride) * elem_b, rows);
 }
 
 int check_tables(const shiftattn_tables* t, const void* workspace, size_t workspace_bytes) {
@@ -832,8 +829,8 @@ int shiftattn_add_rms_norm(const void* x, void* residual, const void* weight, vo
     if ((out == x && (n->out_format != n->x_dtype || s.out_stride != s.x_stride)) || (residual == x && (n->residual_dtype != n->x_dtype || s.res_stride != s.x_stride)))
         return fail(SHIFTATTN_EINVAL, "out or residual is x in another type or with another stride");
     const int64_t bx = static_cast<int64_t>(s.cols) * ex, br = static_cast<int64_t>(s.cols) * er, bo = static_cast<int64_t>(s.cols) * eo;
-    if (cross(x, bx, s.x_stride * ex, out, bo, s.out_stride * eo, rows) || cross(x, bx, s.x_stride * ex, residual, br, s.res_stride * er, rows) ||
-        cross(out, bo, s.out_stride * eo, residual, br, s.res_stride * er, rows))
+    if (cross(x, bx, s.x_stride, out, bo, s.out_stride, ex, eo, rows) || cross(x, bx, s.x_stride, residual, br, s.res_stride, ex, er, rows) ||
+        cross(out, bo, s.out_stride, residual, br, s.res_stride, eo, er, rows))
         return fail(SHIFTATTN_EINVAL, "rows of x, residual and out share memory without being the same");
     if (!codes && scales) return fail(SHIFTATTN_EINVAL, "scales belong to codes: must be NULL for values");
     if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned_to(out, codes ? 8 : 16) || !aligned_to(scales, 4))
@@ -866,7 +863,7 @@ int check_rotary(const shiftattn_rotary_desc* r, const void* q, const void* k, i
     if (rows > 0x7FFFFFFF) return fail(SHIFTATTN_EUNSUPPORTED, "more than 2^31-1 rows");
     if (rows == 0) return 0;
     if ((!q && !k) || !frequencies) return fail(SHIFTATTN_EINVAL, "a required pointer is NULL");
-    if (q == k || cross(q, static_cast<int64_t>(s->hq) * s->head_dim * e, s->q_stride * e, k, static_cast<int64_t>(s->hkv) * s->head_dim * e, s->k_stride * e, rows))
+    if (q == k || cross(q, static_cast<int64_t>(s->hq) * s->head_dim * e, s->q_stride, k, static_cast<int64_t>(s->hkv) * s->head_dim * e, s->k_stride, e, e, rows))
         return fail(SHIFTATTN_EINVAL, "q and k have heads in common");
     if (!aligned16(q) || !aligned16(k) || !aligned_to(frequencies, 8)) return fail(SHIFTATTN_EINVAL, "q / k must be 16-byte aligned, frequencies 8-byte");
     return 0;
