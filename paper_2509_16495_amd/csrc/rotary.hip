@@ -2,7 +2,8 @@
 // angles that grow with the row's position, (a, b) -> m (a cos t - b sin t, b cos t + a sin t), t = position * frequency.
 //
 // The angle is reduced to a fraction of a turn in 64 bits: at position 10^6 a float32 product would have no fraction left that is worth
-// anything (2^20 radians have a last place of 2^-3).  A quarter of a turn around the nearest axis remains, where the Taylor series of
+// anything (2^20 radians have a last place of 2^-3).  Both products, by 1 / (2 pi) and by the position, keep what their rounding leaves off: at position
+// 2^31 that is up to 4e-7 radians for a frequency of 1, and more for higher ones.  A quarter of a turn around the nearest axis remains, where the Taylor series of
 // sine to the ninth and of cosine to the tenth power are exact to 2 * 10^-9, a thirtieth of float32's last place.
 #include "internal.h"
 #include "query_rows.h"
@@ -35,10 +36,18 @@ __device__ inline void set(float& p, float f) { p = f; }
 
 // sine and cosine of position * frequency radians
 __device__ inline void angle_of(int position, double frequency, float& sin_t, float& cos_t) {
-    double turns = position * (frequency * 0.15915494309189535);   // 1 / (2 pi)
-    turns -= rint(turns);                                          // [-1/2, 1/2]
-    const double quarter = rint(turns * 4.0);
-    const float t = static_cast<float>((turns - quarter * 0.25) * 6.283185307179586), u = t * t;
+    float t;
+    double quarter;
+    {
+#pragma clang fp contract(off)   // (a product that joined a sum would bring the part that is added below)
+        const double high = frequency * 0.15915494309189535;   // 1 / (2 pi), whose next 53 bits are those of -9.839338337591243e-18
+        const double low = fma(frequency, 0.15915494309189535, -high) + frequency * -9.839338337591243e-18;
+        const double turns = position * high, rest = fma(static_cast<double>(position), high, -turns) + position * low;
+        const double part = turns - rint(turns);   // [-1/2, 1/2], exact
+        quarter = rint(part * 4.0);
+        t = static_cast<float>(((part - quarter * 0.25) + rest) * 6.283185307179586);
+    }
+    const float u = t * t;
     const float s = t * fmaf(u, fmaf(u, fmaf(u, fmaf(u, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), 1.f);
     const float c = fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
     const int n = static_cast<int>(quarter) & 3;
