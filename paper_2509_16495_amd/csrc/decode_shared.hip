@@ -36,9 +36,10 @@ constexpr int kMaxGroups = 512;
 constexpr double kPlainBytes = 40.0e6;   // cache up to which a batch is the plain kernel's
 constexpr int kMaxRanges = 480;       // ranges that the shared keys of a tile are cut into
 constexpr int kMinSteps = 2;          // steps of a range
-// Sum of a lane's eight weights from which a column's reference moves.  Up to it they stay as they are: a product with values below 2^96
-// cannot overflow.  At 2^8 tiles of 128 columns were 2 % slower, at 2^40 no faster.
-constexpr float kMostSum = 0x1p16f;
+// A column's reference is set this much (in powers of two) above the largest logit so far, and moves from a sum of a lane's eight weights of kMostSum
+// on: weights may grow by 2^13 until it does, and are at most one in the mean, so that a product overflows where the plain kernel's would.  (Rounding
+// to bf16 does not depend on the exponent.)  On tiles of 128 columns a growth of 2^8 was 2 % slower, one of 2^40 no faster than one of 2^16.
+constexpr float kLead = 13.f, kMostSum = 8.f;
 
 // the shared part of a sequence, for the merge: `parts` partial results in units base + (tile + tiles * head) * ranges and on
 struct alignas(32) SharedRow {
@@ -50,6 +51,12 @@ struct GroupIndex {
     int units[kMaxGroups + 1];                                 // units (tile, KV head, range) of the groups in front
     uint16_t offs[kMaxGroups + 1], ranges[kMaxGroups], leader[kMaxGroups];   // first sequence, ranges of an item, the sequence whose table is read
     int sums[3][kWaves];
+};
+
+// logits become powers of two by c; how far above the largest one a reference is set, and the least one: it stays finite (times c too) where all
+// logits are minus infinity
+struct Reference {
+    float c, lead, least;
 };
 
 struct SharedArgs {
@@ -69,7 +76,7 @@ struct SharedArgs {
     int64_t q_stride;
     int num_groups, first_seq, num_seqs, max_blocks, hq_l, hkv_l, r_min, range_min;
     bool always;          // groups share whatever that costs
-    float c;
+    Reference ref;
 };
 
 __device__ inline int wave_scan(int v) {   // inclusive
@@ -135,9 +142,10 @@ struct Columns {
     // P and O += V^T P^T of those tokens, `there` of which exist: 16 or all (blocks that do not are zeros).  kAhead: and the logits of the
     // group parked at `ahead`, their matrix instructions one by one between those of the exponentials, which take about as long.
     template <bool kAhead>
-    __device__ __attribute__((always_inline)) void weigh(const unsigned char* my, int vr, f32x4 (&s)[4], int there, float c, const unsigned char* ahead = nullptr,
+    __device__ __attribute__((always_inline)) void weigh(const unsigned char* my, int vr, f32x4 (&s)[4], int there, const Reference& r, const unsigned char* ahead = nullptr,
                                                          const int* kr = nullptr, f32x4* next = nullptr) {
         u32x4 vf[8];
+        const float c = r.c;
         // P is taken against a reference that moves when a sum says that logits are far above it (rounding to bf16 does not depend on the
         // exponent): no maximum is looked for, which was a fifth of the instructions, and the sums are rarely scaled
         float p[4][4], sum[2];
@@ -177,32 +185,33 @@ struct Columns {
         if (there < kGroup || __builtin_amdgcn_ballot_w64(!(sum[0] < kMostSum) || !(sum[1] < kMostSum))) [[unlikely]] {
             // the unit's first tokens, a reference that is too low, NaN, or a block that does not exist
             const int grp = (threadIdx.x & 63) >> 4;
-            const float least = -3.4e38f / fmaxf(c, 1.f);   // the reference stays finite (times c too) where all logits are minus infinity
             const bool gone = 8 * grp >= there;             // a lane's eight tokens exist or do not
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 float mx = -INFINITY;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (gone) s[x][r] = s[2 + x][r] = -INFINITY;
-                    mx = fmaxf(mx, fmaxf(s[x][r], s[2 + x][r]));
+                for (int i = 0; i < 4; ++i) {
+                    if (gone) s[x][i] = s[2 + x][i] = -INFINITY;
+                    mx = fmaxf(mx, fmaxf(s[x][i], s[2 + x][i]));
                 }
                 mx = fmaxf(mx, __shfl_xor(mx, 16));
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
-                const float m_new = fmaxf(fmaxf(m[x], mx), least);
+                const float m_new = fmaxf(fmaxf(m[x], fminf(mx + r.lead, -r.least)), r.least);
                 const float alpha = __builtin_amdgcn_exp2f((m[x] - m_new) * c);
                 m[x] = m_new;
                 l[x] *= alpha;
 #pragma unroll
                 for (int mt = 0; mt < 8; ++mt) o[x][mt] *= alpha;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    p[x][r] = __builtin_amdgcn_exp2f(fmaf(s[x][r], c, -m_new * c));
-                    p[2 + x][r] = __builtin_amdgcn_exp2f(fmaf(s[2 + x][r], c, -m_new * c));
+                for (int i = 0; i < 4; ++i) {
+                    p[x][i] = __builtin_amdgcn_exp2f(fmaf(s[x][i], c, -m_new * c));
+                    p[2 + x][i] = __builtin_amdgcn_exp2f(fmaf(s[2 + x][i], c, -m_new * c));
                 }
                 add_up(x);
             }
         }
+        // P to bf16, off by at most 2^-8 of itself: what the matrix instructions take, as in every decode kernel here (float32 ones are 16 times slower).
+        // The sums l are of P as it is, in 32 bits.
         bf16x8 pf[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -425,7 +434,7 @@ __device__ __attribute__((always_inline)) inline void wide_unit(const SharedArgs
             if (g + 3 < n) fetch(g + 3, 0);
         }
         // (behind the last group: logits of whatever lies there, not used)
-        c.weigh<true>(smem + (g & 3) * kStageBytes, at.vr, now, (blocks - 2 * g) * kBlockSize, a.c, smem + ((g + 1) & 3) * kStageBytes, at.kr, next);
+        c.weigh<true>(smem + (g & 3) * kStageBytes, at.vr, now, (blocks - 2 * g) * kBlockSize, a.ref, smem + ((g + 1) & 3) * kStageBytes, at.kr, next);
     };
     int g = 0;
 #pragma unroll 1
@@ -443,7 +452,7 @@ __device__ __attribute__((always_inline)) inline void wide_unit(const SharedArgs
             float* dst = a.o_shared + row * kD + 4 * grp;
 #pragma unroll
             for (int mt = 0; mt < 8; ++mt) *reinterpret_cast<f32x4*>(dst + 16 * mt) = c.o[x][mt];
-            if (grp == 0) *reinterpret_cast<f32x2*>(a.ml_shared + row * 2) = f32x2{c.m[x] * a.c, c.l[x]};
+            if (grp == 0) *reinterpret_cast<f32x2*>(a.ml_shared + row * 2) = f32x2{c.m[x] * a.ref.c, c.l[x]};
         }
     }
     if constexpr (!kFp8) __builtin_amdgcn_s_waitcnt(0x0F70);   // (vmcnt(0): a next unit counts its own loads only)
@@ -477,7 +486,7 @@ __device__ __attribute__((always_inline)) inline void narrow_unit(const SharedAr
         if (i + kStride < u.end_block) load(i + kStride);
         f32x4 s[4];
         c.scores(my, at.kr, s);
-        c.weigh<false>(my, at.vr, s, (u.end_block - i) * kBlockSize, a.c);
+        c.weigh<false>(my, at.vr, s, (u.end_block - i) * kBlockSize, a.ref);
     }
     c.sum_lanes();
     if (grp == 0) ref[wave][col] = c.m[0], ref[wave][16 + col] = c.m[1];
@@ -488,7 +497,7 @@ __device__ __attribute__((always_inline)) inline void narrow_unit(const SharedAr
         float top = ref[0][16 * x + col];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ref[w][16 * x + col]);
-        const float f = c.m[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((c.m[x] - top) * a.c);
+        const float f = c.m[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((c.m[x] - top) * a.ref.c);
 #pragma unroll
         for (int mt = 0; mt < 8; ++mt) *reinterpret_cast<f32x4*>(mine + (16 * x + col) * kD + 4 * ((grp + 4 * mt) ^ (col & 7))) = c.o[x][mt] * f;
         if (grp == 0) sums[wave][16 * x + col] = c.l[x] * f;
@@ -512,7 +521,7 @@ __device__ __attribute__((always_inline)) inline void narrow_unit(const SharedAr
                 float top = ref[0][cc], l = sums[0][cc];
 #pragma unroll
                 for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ref[w][cc]), l += sums[w][cc];
-                *reinterpret_cast<f32x2*>(a.ml_shared + row * 2) = f32x2{top * a.c, l};
+                *reinterpret_cast<f32x2*>(a.ml_shared + row * 2) = f32x2{top * a.ref.c, l};
             }
         }
     }
@@ -746,7 +755,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
         return;
     }
     decode_flat_body<kFp8, kAppend, kWaves, false, kBlockScales ? 1 : 0, kMaxPairs, true>(
-        a.q, a.q_stride, a.cache, a.block_table, a.max_blocks, a.seq_lens, a.o_part, a.ml_part, a.plan, n, a.hq_l, a.hkv_l, a.c, a.r_min, ap, smem, index, wg - n_p,
+        a.q, a.q_stride, a.cache, a.block_table, a.max_blocks, a.seq_lens, a.o_part, a.ml_part, a.plan, n, a.hq_l, a.hkv_l, a.ref.c, a.r_min, ap, smem, index, wg - n_p,
         kWorkgroups - n_p, a.scales, from);
 }
 
@@ -913,6 +922,7 @@ hipError_t launch_decode_shared(const void* q, const void* k_new, const void* v_
                                 int num_groups, void* out, void* workspace, const AttnShape& a, hipStream_t st) {
     const bool append = k_new != nullptr;
     const int per = seqs_per_launch(max_seq_len, a), G = a.hq_l / a.hkv_l;
+    const float c = a.scale * a.k_scale * 1.4426950408889634f;
     for (int s0 = 0; s0 < num_seqs; s0 += per) {  // runs share the workspace: same stream, one after the other
         const int n = num_seqs - s0 < per ? num_seqs - s0 : per;
         const size_t rows = rows_of(n, a), shared = static_cast<size_t>(most_units(n, num_groups, a)) * kTileCols;
@@ -925,7 +935,7 @@ hipError_t launch_decode_shared(const void* q, const void* k_new, const void* v_
         const SharedArgs args = {static_cast<const uint16_t*>(q) + static_cast<size_t>(s0) * a.q_stride, static_cast<uint16_t*>(cache),
                                  block_table + static_cast<size_t>(s0) * a.max_blocks, seq_lens + s0, group_offsets, shared_lens, a.kv_scales, o_part, ml_part, plan,
                                  o_shared, ml_shared, info, a.q_stride, num_groups, s0, n, a.max_blocks, a.hq_l, a.hkv_l, own_r_min(max_seq_len),
-                                 range_min(max_seq_len), option_decode_shared() == 1, a.scale * a.k_scale * 1.4426950408889634f};
+                                 range_min(max_seq_len), option_decode_shared() == 1, {c, fminf(kLead / c, 3.4e38f / fmaxf(c, 1.f)), -3.4e38f / fmaxf(c, 1.f)}};
         const AppendArgs ap = {append ? static_cast<const uint16_t*>(k_new) + static_cast<size_t>(s0) * a.kv_stride : nullptr,
                                append ? static_cast<const uint16_t*>(v_new) + static_cast<size_t>(s0) * a.kv_stride : nullptr,
                                append ? slots + s0 : nullptr, a.kv_stride, a.k_scale, a.v_scale, a.kv_scales};

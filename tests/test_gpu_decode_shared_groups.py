@@ -1,8 +1,11 @@
 """decode_shared where units of shared keys are many and short beside the sequences' own keys: a workgroup takes several of them, of groups of
 different length and width, one behind the other (bounds as in test_gpu_decode_shared)."""
+import math
+
 import numpy as np
 import pytest
 
+import plain_8bit as P
 from test_gpu_decode_shared import B, Case
 
 pytestmark = pytest.mark.gpu
@@ -55,3 +58,28 @@ def test_one_workspace_for_batches_of_any_number_of_groups(B):
     for c, d in zip(cases, ds):
         c.call(B, d, workspace=ws)
         c.check(d)
+
+
+@pytest.mark.parametrize("members", [2, 20])
+@pytest.mark.parametrize("shared", [True, False])
+def test_values_of_any_magnitude(B, members, shared):
+    """Values times 2^e make outputs times 2^e, to the bit: nothing on the way overflows or loses places where the plain call's sums do not.
+    Half of the keys weigh 2^12 times the first ones of every range."""
+    import torch
+    outs = []
+    for e in (0, -100, 100, 115):
+        case = Case([(640, [650 + i for i in range(members)])], seed=17)
+        case.q[...] = 1
+        case.pages[:, :, 0] = 0
+        for i in range(40):
+            if i // 2 % 2:
+                case.pages[case.table[0, i], :, 0] = P.bf16(np.float32(12 * math.log(2) / math.sqrt(128)))
+        case.pages[:, :, 1] *= np.float32(2.0 ** e)
+        case.v_new *= np.float32(2.0 ** e)
+        d = case.device()
+        case.call(B, d, shared=shared)
+        torch.cuda.synchronize()
+        out = d["out"].double() * 2.0 ** -e
+        assert torch.isfinite(out).all(), e
+        outs.append(out)
+    assert all(torch.equal(o, outs[0]) for o in outs)
