@@ -663,7 +663,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
     const int wg = blockIdx.x;
     int n_p = 0, all = 0;
     if (cost_p > 0) {   // uniform
-        const float share = share_of(cost_p, cost_s);
         const int range = range_of(cost_p, cost_s);
         int units_of[kGroupsPer], each_of[kGroupsPer], units = 0;
 #pragma unroll
@@ -673,7 +672,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
                 const int ranges = ranges_of(steps[x], cols[x], range, a.range_min);
                 gi.ranges[tid * kGroupsPer + x] = static_cast<uint16_t>(ranges);
                 units_of[x] = ranges * a.hkv_l * tiles_of(cols[x]);
-                each_of[x] = weight_of(steps[x], ranges, cols[x]);
+                each_of[x] = among(range_steps(steps[x], ranges), cols[x]);
             }
             units += units_of[x];
         }
@@ -694,7 +693,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_shared_kernel(SharedArg
         }
         if (tid == 0) gi.units[a.num_groups] = all;
         n_p = all;
-        if (all > share || all > kMostShared) {   // uniform: more units than the shared keys' part of the workgroups
+        if (!one_each(all, cost_p, cost_s)) {   // uniform
             uint32_t weighs = 0, longest = 0;   // as the units are: their last ranges may be shorter
 #pragma unroll
             for (int x = 0; x < kGroupsPer; ++x) {

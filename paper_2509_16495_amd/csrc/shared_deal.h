@@ -31,10 +31,10 @@ constexpr float kRangeRoot = 0.25f;
 // in bf16 as in FP8.  With 2 for those, 180 sequences of up to 600 tokens behind 20000 took 55.0 us (39.6 with 4; FP8 50.9 and 42.7), 10 groups
 // of 8 behind 6000 28.5 (24.5; 26.1 and 23.2), 8 groups over an FP8 cache 44.0 (44.1 to 45.5); with 6 these took 47.0.  Narrow steps at 2: within 1 %.
 constexpr int kWideCost = 3, kNarrowCost = 1, kOwnCost = 4;
-// What a unit takes beside its keys (block ids, queries, the first keys, the parts it writes: a chain of loads).  It counts where a workgroup takes
-// several of them, and where it is asked if sharing pays.  64 prompts of 1000 tokens with two answers each, 8 KV heads: 166 us with 10 (FP8 91, the plain kernel
-// 98), 173 with 6 (99), 169 with 14 (94); 20 groups of 4 behind 512 tokens 88, 88, 93; 30 groups of 3 behind 3000 121, 120, 124.
-constexpr int kUnitCost = 10;
+// What a unit takes beside its keys (block ids, queries, the first keys, the parts it writes: a chain of loads), and a step of a narrow tile among
+// many, where memory sets the pace: half of the own keys' 128 tokens.  They count where workgroups take several units, and where it is asked if
+// sharing pays.
+constexpr int kUnitCost = 6, kNarrowAmong = 2;
 
 // columns of a tile of a group that has so many, and its tiles
 SHIFTATTN_BOTH int tile_cols(int cols) { return cols > kNarrowCols ? kTileCols : kNarrowCols; }
@@ -42,15 +42,16 @@ SHIFTATTN_BOTH int tiles_of(int cols) { return (cols + tile_cols(cols) - 1) / ti
 SHIFTATTN_BOTH int cost_of(int cols) { return cols > kNarrowCols ? kWideCost : kNarrowCost; }
 SHIFTATTN_BOTH int steps_of(int blocks) { return (blocks + 3) / 4; }
 
+// steps of a unit that is one of many, and the unit
+SHIFTATTN_BOTH int among(int steps, int cols) { return kUnitCost + steps * (cols > kNarrowCols ? kWideCost : kNarrowAmong); }
 // Do the tiles of a group with so many blocks in common take less than its members take with those blocks each for itself?  512 pairs with four
 // blocks in common: 212 us if they share those, 205 if they do not (the plain kernel 198).
 SHIFTATTN_BOTH bool pays(int blocks, int members, int cols) {
-    return static_cast<float>(tiles_of(cols)) * (kUnitCost + steps_of(blocks) * cost_of(cols)) < 0.25f * kOwnCost * members * blocks / 2;
+    return static_cast<float>(tiles_of(cols)) * among(steps_of(blocks), cols) < 0.25f * kOwnCost * members * blocks / 2;
 }
 
-// The shared keys' part of the workgroups by weight, and the weight of a range: an even part of all work.  (Shared keys over whole workgroups, at
-// least one, made 2000 tokens of 4 sequences one range that 60 others waited for: 43 us, where this takes 36.)
-SHIFTATTN_BOTH float share_of(float shared, float own) { return kWorkgroups * shared / (shared + own); }
+// The weight of a range: an even part of all work.  (Shared keys over whole workgroups, at least one, made 2000 tokens of 4 sequences one range that
+// 60 others waited for: 43 us, where this takes 36.)
 SHIFTATTN_BOTH int range_of(float shared, float own) { return static_cast<int>(__builtin_ceilf((shared + own) / kWorkgroups)); }
 
 // ranges that the keys of a tile are cut into (range_min: steps that a range has at least), and steps of one of them
@@ -61,28 +62,36 @@ SHIFTATTN_BOTH int ranges_of(int steps, int cols, int range, int range_min) {
     per = per > range_min ? per : range_min;
     const int ranges = (steps + per - 1) / per;
     // workgroup i runs on die i % 8: with a multiple of 4 ranges the tiles and heads of a group find the same keys in the L2 of one die, or of
-    // two (135 MB read from memory become 20 where 2048 columns meet 32768 tokens)
+    // two (210 MB fetched from memory become 41 where 2048 columns meet 32768 tokens, 17 MB of keys)
     return ranges >= 16 && cols > kTileCols ? ranges & ~3 : ranges;
 }
 SHIFTATTN_BOTH int range_steps(int steps, int ranges) { return (steps + ranges - 1) / ranges; }
 
-// what a unit that is one of several of a workgroup takes
-SHIFTATTN_BOTH uint32_t weight_of(int steps, int ranges, int cols) { return kUnitCost + range_steps(steps, ranges) * cost_of(cols); }
+// Is a workgroup for each of `all` units, whose steps weigh `shared`, the best there is?  Where the own keys take no longer than the mean unit.
+SHIFTATTN_BOTH bool one_each(int all, float shared, float own) {
+    return all <= kMostShared && own * all <= (shared + static_cast<float>(kUnitCost) * all) * (kWorkgroups - all);
+}
 
-// Workgroups for `all` units of shared keys of weight `shared`, the longest of weight `longest`.  As many as there are units: the shared part
-// takes `longest`.  Fewer, m, with units that follow each other: at most shared / m + longest; that meets the own keys' own / (kWorkgroups - m) at
-// the root of  longest m^2 + (shared + own - longest kWorkgroups) m - kWorkgroups shared = 0.  The faster of the two.
-// With a workgroup for every unit, however short, 64 prompts with two answers each of eight KV heads left four workgroups to the own keys: 2585 us,
-// where the plain kernel takes 182.
+// Workgroups for `all` units of shared keys that weigh `shared` together and `longest` at most (by `among`).  With m of them, and units that follow
+// each other, the shared part takes up to shared / m + longest, which meets the own keys' own / (kWorkgroups - m) at the root of
+//     longest m^2 + (shared + own - longest kWorkgroups) m - kWorkgroups shared = 0;
+// with a workgroup for one, two or three units it takes one, two or three times `longest`.  The fastest of these.
+// 64 prompts of 1000 tokens with two answers each, 8 KV heads: 165 us (FP8 91), where a workgroup for every unit, however short, left four to
+// the own keys and took 2585 (the plain kernel 182, 98); 30 groups of 3 behind 3000 tokens 106 (140, and 121 without the multiples of `longest`; plain 197).
 SHIFTATTN_BOTH int workgroups_of(int all, float shared, float longest, float own) {
     const float b = shared + own - longest * kWorkgroups, root = __builtin_sqrtf(b * b + 4.f * kWorkgroups * longest * shared);
     const float meet = b > 0.f ? 2.f * kWorkgroups * shared / (b + root) : (root - b) / (2.f * longest);
     const int most = all < kMostShared ? all : kMostShared;
-    int fewer = meet < 1.f ? 1 : meet < static_cast<float>(most) ? static_cast<int>(meet) : most;
-    if (all > kMostShared) return fewer;
-    const float own_each = own / (kWorkgroups - all), own_fewer = own / (kWorkgroups - fewer), shared_fewer = shared / fewer + longest;
-    const float each = own_each > longest ? own_each : longest, both = own_fewer > shared_fewer ? own_fewer : shared_fewer;
-    return each <= both ? all : fewer;
+    int best = meet < 1.f ? 1 : meet < static_cast<float>(most) ? static_cast<int>(meet) : most;
+    const float own_best = own / (kWorkgroups - best), shared_best = shared / best + longest;
+    float least = own_best > shared_best ? own_best : shared_best;
+    for (int k = 3; k > 0; --k) {
+        const int n = (all + k - 1) / k;
+        if (n > kMostShared) break;
+        const float own_n = own / (kWorkgroups - n), time = own_n > k * longest ? own_n : k * longest;
+        if (time <= least) best = n, least = time;
+    }
+    return best;
 }
 
 // Of n < all workgroups number i takes the units that begin at weights [first_of(i), first_of(i + 1)) of the line of all units.

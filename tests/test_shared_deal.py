@@ -23,20 +23,19 @@ using namespace shiftattn::shared_deal;
 extern "C" void walk(const int* steps, const int* cols, int groups, int hkv, float own, int range_min, int* out, double* times) {
     float shared = 0;
     for (int g = 0; g < groups; ++g) shared += static_cast<float>(steps[g]) * hkv * tiles_of(cols[g]) * cost_of(cols[g]);
-    const float share = share_of(shared, own);
     const int range = range_of(shared, own);
     std::vector<int> units(groups + 1, 0);
     std::vector<uint32_t> line(groups + 1, 0), each(groups, 0);
     uint32_t longest = 0;
     for (int g = 0; g < groups; ++g) {
         const int ranges = steps[g] > 0 ? ranges_of(steps[g], cols[g], range, range_min) : 0, n = ranges * hkv * tiles_of(cols[g]);
-        if (n) each[g] = weight_of(steps[g], ranges, cols[g]);
+        if (n) each[g] = among(range_steps(steps[g], ranges), cols[g]);
         longest = std::max(longest, each[g]);
         units[g + 1] = units[g] + n, line[g + 1] = line[g] + n * each[g];
     }
     const int all = units[groups];
     int n_p = all;
-    if (all > share || all > kMostShared) n_p = workgroups_of(all, static_cast<float>(line[groups]), static_cast<float>(longest), own);
+    if (!one_each(all, shared, own)) n_p = workgroups_of(all, static_cast<float>(line[groups]), static_cast<float>(longest), own);
     std::vector<int> taken(all, 0);
     double most = 0;
     auto unit_at = [&](uint32_t x) {
