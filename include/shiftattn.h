@@ -268,7 +268,8 @@ int shiftattn_unpack_o_proj_int8_ws(const void *recv_codes, const float *a_scale
  * inv = 1 / sqrt(sum_k h[k]^2 / cols + eps), the sum in 64 bits, rounded once to float32; y[k] = (h[k] * inv) * (weight[k] + weight_offset),
  * each operation in float32.  Written as y rounded to bf16 or as it is (out_format SHIFTATTN_BF16 / _F32), or as the codes and the scale
  * that shiftattn_quantize_rows_fp8 / _int8 name for the row y (SHIFTATTN_CODES_FP8 / _INT8), from y's float32 values: what the
- * projections over 8-bit operands take.  The results do not depend on how rows are shared out: they are those bits.
+ * projections over 8-bit operands take.  The results are those bits, the same for a row wherever it stands; where 1 / sqrt lies within a few 2^-53
+ * (relative) of a border between two float32 values, about one row in 2^27, inv may be the value next to it.
  *   x (device, in)               : [rows][cols], bf16 or float32, row stride x_stride
  *   residual (device, in/out)    : [rows][cols], bf16 or float32, row stride residual_stride, or NULL
  *   weight (device, in)          : [cols], bf16 or float32; weight_offset 1 is for weights stored as their difference from 1
@@ -424,7 +425,9 @@ int shiftattn_decode_static(const void *q, const void *k_new, const void *v_new,
  *   kv_scales: the scales of a cache with block scales (a->kv_format = SHIFTATTN_KV_FP8_E4M3_BLOCKS), NULL for any other
  *   All else as in shiftattn_decode; a token that is appended must lie behind the blocks in common.
  * bf16 rows with head_dim 128 and up to 16 query heads per KV head, and up to 512 groups, take the kernel that shares; any other call is
- * served as the plain one, and so is a small batch (num_seqs * max_seq_len tokens of up to 40 MB of cache), where the plain one is faster.  workspace: shiftattn_decode_shared_workspace_bytes(...) bytes, 16-byte aligned. */
+ * served as the plain one, and so is a small batch (num_seqs * max_seq_len tokens of up to 40 MB of cache), where the plain one is faster.  That is asked of the upper
+ * bounds, on the host: a call that is captured for long sequences and replayed on short ones, or a batch with little in common, takes the kernel that
+ * shares and pays 1.5 to 7 us for its plan and its merge.  workspace: shiftattn_decode_shared_workspace_bytes(...) bytes, 16-byte aligned. */
 int shiftattn_decode_shared(const void *q, const void *k_new, const void *v_new, const int64_t *slot_mapping, void *kv_cache,
                             float *kv_scales, const int32_t *block_table, const int32_t *seq_lens, int32_t num_seqs,
                             int32_t max_seq_len, const int32_t *group_offsets, const int32_t *shared_lens, int32_t num_groups,

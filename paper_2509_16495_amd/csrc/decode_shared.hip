@@ -8,15 +8,17 @@
 //
 // One launch takes both kinds of ranges, a second one joins them.  Every workgroup works out the same plan from lengths and offsets, about
 // 3 us of which most is dependent loads; a launch of its own for the plan took 4 us more.  Workgroups are dealt out by the work that either
-// kind weighs; a unit of shared keys is (tile of columns, KV head, range of keys), a workgroup's own keys are the plain kernel's.
+// kind weighs (shared_deal.h); a unit of shared keys is (tile of columns, KV head, range of keys), a workgroup's own keys are the plain kernel's.
 //
 // What bounds it: the bytes read once are few (256 sequences of 8 heads behind 32768 tokens: 160 MB, 29 us at the copy rate), but each 32
-// tokens cost a tile of 128 columns 128 matrix instructions of 16.4 clocks and 4096 exponentials, and what the vector units do and what the
-// matrix units do adds up on a SIMD: 0.85 us a group of 32 tokens for one workgroup of a compute unit, 0.8 to 1.0 for each of two, where the
-// matrix units are busy half of the time.  Neither the barrier (1 us of 55 without it), nor keys out of a hot L2, nor 32x32x16 instructions
-// (4 % less for one workgroup, 5 % more for two), nor exponentials in front of the first matrix instructions change that.  Few sequences are
-// bounded by the fixed parts: plan 3 us, first loads 3, partial results 2, the merge 4 to 9.  256 sequences behind 32768 tokens: 67 us, where the
-// plain kernel reads 17 GB in 607.
+// tokens cost a tile of 128 columns 128 matrix instructions of 16.4 clocks and 4096 exponentials: a wavefront's share of the matrix and of the
+// vector instructions takes about 880 clocks of a SIMD (0.37 us).  Two tiles on a compute unit, a wavefront of each on a SIMD, take 0.8 to 1.0 us for
+// a group of both: that sum and a tenth to a third on top of it.  A lone tile takes 0.85 us for its group, twice its sum: it waits (for operands out of LDS, for the
+// products that its exponentials need, for the other wavefronts), with nothing beside it that would fill the time.  A launch has both, and wavefronts
+// that read the sequences' own keys: over all of 256 sequences behind 32768 tokens the matrix units are busy for a quarter of the time, and so is LDS.
+// Neither the barrier (1 us of 55 without it), nor keys out of a hot L2, nor 32x32x16 instructions (4 % less for one workgroup, 5 % more for two), nor
+// exponentials in front of the first matrix instructions change that.  Few sequences are bounded by the fixed parts: plan 3 us, first loads 3, partial
+// results 2, the merge 4 to 9.  256 sequences behind 32768 tokens: 67 us, where the plain kernel reads 17 GB in 607.
 // Workgroups of eight wavefronts whose halves take every other group and add their sums in LDS write half as many parts (64 sequences behind
 // 32768 tokens 28.1 us against 31.7), but a compute unit draws only so many bytes, and those with the sequences' own keys are then fewer (256 with
 // up to 2000 of their own 84 to 113 us against 67): not taken.
@@ -287,7 +289,8 @@ struct Block {
 };
 
 // A unit's block ids, 64 at a time, one per lane: ids that came one by one through scalar loads made every wait for LDS data wait for them
-// too (they share a counter), 1 us a step.
+// too (they share a counter), 1 us a step.  (As built, the load of the window behind is waited for where it is made, with everything else that
+// is on its way: once in 32 groups.)
 struct BlockIds {
     const int32_t* table;
     int last, at, now, next;   // the window from block `at` on, and the one behind it
@@ -336,7 +339,7 @@ struct Places {
 // logits of group g + 1 are (matrix instructions between the vector ones), and groups g + 2 and g + 3 are on their way: straight into LDS, or
 // in two sets of registers where codes are widened.  One barrier per group: behind it group g + 1 is there for all, and all are done with
 // group g - 1, whose place the next load takes.
-// What bounds it: LDS, 64 KiB read for each group by the four wavefronts (512 clocks of a compute unit), two workgroups on a unit.
+// What bounds it stands at the head of this file; LDS, 64 KiB read for each group by the four wavefronts (512 clocks of a compute unit), is not it.
 template <bool kFp8, int kScales>
 __device__ __attribute__((always_inline)) inline void wide_unit(const SharedArgs& a, const Unit& u, unsigned char* smem) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;

@@ -3,9 +3,10 @@
 //
 //   h = x + residual, rounded to the residual's type and stored there;  inv = 1 / sqrt(sum h^2 / cols + eps);  y = (h * inv) * (w + offset)
 //
-// The squares are summed in 64 bits (a bf16 value's square is exact in 32, a float32 value's in 64) and inv is rounded once to float32,
-// so that y, and with it every code and scale, does not depend on the order of the sum: the codes of a row are the same whichever of the
-// instances below took it.
+// The squares are summed in 64 bits (a bf16 value's square is exact in 32, a float32 value's in 64) and inv is rounded once to float32, so
+// that y, and with it every code and scale, is what the definition says in any order of the sum, unless 1 / sqrt lies within the sum's and the root's few
+// 2^-53 of a border between two float32 values: about one row in 2^27, whose inv may be the neighbouring value.  A row's instance follows from
+// `cols` alone, so the same row gives the same bits in every call.
 #include "internal.h"
 
 namespace shiftattn {
