@@ -29,7 +29,8 @@ constexpr int kNarrowCols = 32;
 constexpr float kRangeRoot = 0.25f;
 // Time of a step of either kind of tile, and of 32 tokens for each of a workgroup's wavefronts, which have one group of 32 on its way each: 2 us
 // in bf16 as in FP8.  With 2 for those, 180 sequences of up to 600 tokens behind 20000 took 55.0 us (39.6 with 4; FP8 50.9 and 42.7), 10 groups
-// of 8 behind 6000 28.5 (24.5; 26.1 and 23.2), 8 groups over an FP8 cache 44.0 (44.1 to 45.5); with 6 these took 47.0.  Narrow steps at 2: within 1 %.
+// of 8 behind 6000 28.5 (24.5; 26.1 and 23.2), 8 groups over an FP8 cache 44.0 (44.1 to 45.5); with 6 these took 47.0.  Narrow steps at 2: within
+// 1 % in those batches, 30 groups of 3 behind 3000 tokens 134 us against 121.
 constexpr int kWideCost = 3, kNarrowCost = 1, kOwnCost = 4;
 // What a unit takes beside its keys (block ids, queries, the first keys, the parts it writes: a chain of loads), and a step of a narrow tile among
 // many, where memory sets the pace: half of the own keys' 128 tokens.  They count where workgroups take several units, and where it is asked if
